@@ -334,6 +334,129 @@ int dbf_stack_gemv(const dbf_stack* stack, const void* x_dev, void* y_dev, int b
 int dbf_stack_sync_timeouts(const dbf_stack* stack, int* timeouts); /* as dbf_sync_timeouts */
 void dbf_stack_free(dbf_stack* stack); /* NULL is allowed */
 
+/* ---- between the layer products of a token pass -------------------------------------------
+ * What a decoder does with the outputs of its query, key and value layers, and with its logits: places in a paged cache for new
+ * tokens (dbf_block_tables), norms and position rotation of the heads (dbf_qk_norm_rope), the write to a cache held in 4 bits
+ * (dbf_cache_append), attention over it (dbf_cache_attend), and log probabilities of given tokens (dbf_token_logprobs).  The paper
+ * compresses the linear layers only and times them alone; these are the rest of the pass that they run in.
+ * All are asynchronous on hip_stream, allocate nothing, do not synchronise and may be captured into a graph; results do not depend
+ * on scheduling.  Arguments are host values and device pointers; lengths, tables, positions and slots are read on the device, so a
+ * pass needs no copy to the host.  What the device finds out of range there is never followed: each entry point says what comes out.
+ *
+ * Element types of tensors: */
+enum { DBF_F16 = 0, DBF_BF16 = 1, DBF_F32 = 2 };
+
+/* The cache: pages of page_tokens (32, 64, 128 or 256) tokens, n_kv_heads heads of head_dim (64, 128 or 256) keys and values each, in
+ * one block of dbf_cache_bytes bytes (16-byte aligned, caller's).  `slot` = page * page_tokens + place in the page.
+ * A value is s (c - z): a code c of 4 bits, and for each group of 64 values of a token and head a scale s and an integer z in 0..15.
+ * Group of value d: (d / 16) mod (head_dim / 64).  s is the range of the group's values and zero, over 15, rounded up to 7 significant
+ * bits and to a multiple of 2^-24, so that every value held is exact in fp16; z = rint(-lo / s), c = clamp(rint(x / s) + z, 0, 15),
+ * ties to even.  Values beyond +-57344 are held as that.  4.5 bits a value in all.
+ * Layout: records of 32 tokens, 36 * head_dim bytes, in the order [page][head][page_tokens / 32]:
+ *   keys    at 0:             token t: head_dim / 2 bytes, values 2 i and 2 i + 1 in the low and the high half of byte i
+ *   values  at 16 head_dim:   group p: 1024 bytes; byte 16 (16 g + l) + 4 (2 q + h) + i holds token 16 h + 4 g + i, values
+ *                             16 (p + (head_dim / 64) 2 q) + l (low half) and 16 (p + (head_dim / 64) (2 q + 1)) + l (high half)
+ *   keys' groups at 32 head_dim, values' groups at 34 head_dim: [group][token] of two fp16: s, -s z
+ * A token whose keys or values of a head are not all finite is held with -s z of its keys no number and s = 0 of its values:
+ * attention rows of that head which see the token come out as no numbers, others are not touched. */
+typedef struct dbf_cache {
+    void* data;
+    int n_pages, page_tokens, n_kv_heads, head_dim;
+} dbf_cache;
+#define DBF_CACHE_BLOCK 32  /* tokens of a record */
+#define DBF_CACHE_GROUP 64  /* values that share a scale */
+size_t dbf_cache_bytes(int n_pages, int page_tokens, int n_kv_heads, int head_dim); /* 0 if one is out of range */
+
+/* dbf_block_tables: pages and slots for the new tokens of n_seq requests.  Request i holds cached_len[i] tokens, in the pages
+ * block_table[i][0 ..] (table_stride entries a request), and gets new_len[i] more (negative counts as 0).  The pages that
+ * takes, ceil((cached + new) / page_tokens) - ceil(cached / page_tokens), come from free_pages[0 .. n_free) in the order of the
+ * requests and are entered in the table; nothing else of it changes.  Out:
+ *   q_start  [n_seq + 1]: requests' first new tokens in their common order, and the number of all
+ *   kv_len   [n_seq]: cached + new         positions [max_tokens]: each new token's place in its request
+ *   slots    [max_tokens]: its slot in the cache; -1 where free_pages or the table has no page for it
+ *   status   [2]: pages taken; pages that were missing
+ * Entries of positions and slots behind the last token are 0 and -1 (tokens beyond max_tokens get none).  All arrays are device
+ * int32, 4-byte aligned; free_pages may be NULL if n_free is 0, positions and slots if max_tokens is 0.
+ * Errors: DBF_EINVAL (null, misaligned, n_seq < 1 or > DBF_MAX_DIM, n_free or max_tokens < 0, table_stride < 1, page_tokens), DBF_EHIP. */
+int dbf_block_tables(const int32_t* cached_len, const int32_t* new_len, int n_seq, int page_tokens, const int32_t* free_pages, int n_free,
+                     int32_t* block_table, int table_stride, int max_tokens, int32_t* q_start, int32_t* kv_len, int32_t* positions,
+                     int32_t* slots, int32_t* status, void* hip_stream);
+
+/* The heads of a pass's tokens, and what is done to them.  Rows are strides apart, counted in values: [n_tokens][heads][head_dim] with
+ * whatever between the rows.  Pointers need the element type's alignment only.
+ *   norm:     x <- x / sqrt(mean of x^2 over the head + eps) * weight            (weight: [head_dim] of dtype; NULL: no norm)
+ *   rotation: the first rot_dim values of a head in pairs (a, b) <- (a cos - b sin, b cos + a sin); pairs are (i, i + rot_dim / 2), or
+ *             neighbours (2 i, 2 i + 1) if interleaved; rope: device fp32 [rope_len][rot_dim], the cosines, then the sines of a
+ *             position's pairs; positions: device int32 [n_tokens].  rope NULL: no rotation.  A token whose position is not in
+ *             [0, rope_len) gets no numbers for its rotated values.
+ * In fp32, rounded once at the end. */
+typedef struct dbf_heads {
+    const void *q, *k, *v;
+    long long q_stride, k_stride, v_stride;
+    void *q_out, *k_out;
+    long long q_out_stride, k_out_stride;
+    const void *q_weight, *k_weight;
+    const void* rope;
+    const int32_t* positions;
+    int dtype, n_tokens, n_q_heads, n_kv_heads, head_dim;
+    int rope_len, rot_dim, interleaved;
+    float eps;
+} dbf_heads;
+
+/* dbf_qk_norm_rope: q -> q_out and k -> k_out (each may be its input; a NULL q or k leaves that out).  head_dim: even, 2 .. 1024; dtype
+ * DBF_F16 or DBF_BF16.  n_tokens 0 does nothing.  v is not used.
+ * Errors: DBF_EINVAL (null, misaligned, strides below a row's length, counts, rot_dim odd or above head_dim, eps < 0), DBF_ESHAPE
+ * (head_dim), DBF_EHIP. */
+int dbf_qk_norm_rope(const dbf_heads* heads, void* hip_stream);
+
+/* dbf_cache_append: the same in one launch with the write to the cache: q -> q_out (if q is not NULL), and the token's k, after norm
+ * and rotation, and v into slot slots[t] (device int32 [n_tokens]; a token whose slot is not one of the cache's is left out).  k_out is
+ * not used: keys go from fp32 to 4 bits.  No two tokens may have one slot.  head_dim and n_kv_heads are the cache's (DBF_ESHAPE). */
+int dbf_cache_append(const dbf_heads* heads, const dbf_cache* cache, const int32_t* slots, void* hip_stream);
+
+/* dbf_cache_read: what the cache holds in the given slots, as k_out and v_out [n_tokens][n_kv_heads][head_dim] of dtype (DBF_F16: exact,
+ * DBF_BF16: rounded, DBF_F32); a slot that is not one of the cache's reads as zeros, a token held as no number as no numbers (k_out). */
+int dbf_cache_read(const dbf_cache* cache, const int32_t* slots, int n_tokens, void* k_out, void* v_out, int dtype, void* hip_stream);
+
+/* dbf_cache_attend: out = softmax(scale q k^T) v over the tokens that the cache holds for a request.
+ *   q, out:     device [n_tokens][n_q_heads][head_dim] of dtype (DBF_F16, DBF_BF16), rows q_stride / out_stride values apart; n_q_heads is a multiple
+ *               of the cache's heads, query head h reads head h / (n_q_heads / n_kv_heads)
+ *   q_start:    device int32 [n_seq + 1]: request i's rows; NULL: one row a request (row i)
+ *   kv_len:     device int32 [n_seq]: tokens held for the request, the new ones (its rows) among them
+ *   block_table device int32 [n_seq][table_stride]: pages of a request in the order of its tokens
+ *   causal:     row t of n sees the first kv_len - n + t + 1 tokens; 0: all rows see all
+ *   max_q, max_kv: no request has more rows or tokens (they choose the launch; a request that has more of either, or a kv_len that is
+ *               negative or beyond its table, comes out as no numbers in the rows below max_q; rows from max_q on are not written)
+ * A row that sees nothing is zero.  A page that the cache does not have makes the rows that see it no numbers.  Scores, statistics and sums are fp32;
+ * probabilities are rounded to fp16 relative to a row's largest for the product with the values.
+ * workspace_dev: 256-byte aligned, dbf_cache_attend_workspace_bytes(attend, cache) bytes (may be 0), which depends on dtype, n_seq,
+ * n_q_heads, max_q, max_kv and the cache's sizes only; contents need not be anything.
+ * Errors: DBF_EINVAL, DBF_ESHAPE (head_dim, heads that do not divide), DBF_EWORKSPACE, DBF_EHIP. */
+typedef struct dbf_attend {
+    const void* q;
+    void* out;
+    long long q_stride, out_stride;
+    const int32_t *q_start, *kv_len, *block_table;
+    int dtype, n_tokens, n_seq, n_q_heads, max_q, max_kv, table_stride, causal;
+    float scale;
+} dbf_attend;
+size_t dbf_cache_attend_workspace_bytes(const dbf_attend* attend, const dbf_cache* cache);
+int dbf_cache_attend(const dbf_attend* attend, const dbf_cache* cache, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+
+/* dbf_token_logprobs: of rows of logits x [n_rows][vocab] (dtype DBF_F16, DBF_BF16, DBF_F32; row_stride values apart)
+ *   logprob[row] = x[target] - log sum exp x            (targets: device int32; a negative target: 0, one beyond the row: no number)
+ *   entropy[row] = - sum p log p, of p = softmax x      (NULL: left out)
+ *   top_ids, top_logprobs [n_rows][n_top]: the n_top (0 .. 64, at most vocab) likeliest tokens in order, ties to the lowest index
+ * logprob, entropy, top_logprobs: device fp32; top_ids: device int32.  A logit of -infinity is a token that cannot be: it counts for
+ * nothing.  A row of nothing else, or with a logit that is no number or +infinity, has no distribution: its logprob, entropy and
+ * top_logprobs are no numbers; its top_ids are still in order (no numbers before all others).
+ * targets and logprob may both be NULL.  workspace_dev: 256-byte aligned, dbf_token_logprobs_workspace_bytes bytes (may be 0).
+ * Errors: DBF_EINVAL, DBF_ESHAPE (vocab), DBF_EWORKSPACE, DBF_EHIP. */
+size_t dbf_token_logprobs_workspace_bytes(int n_rows, int vocab, int n_top); /* 0 if one is out of range, or none is needed */
+int dbf_token_logprobs(const void* logits, int dtype, long long row_stride, int n_rows, int vocab, const int32_t* targets, int n_top,
+                       float* logprob, float* entropy, int32_t* top_ids, float* top_logprobs, void* workspace_dev, size_t workspace_bytes,
+                       void* hip_stream);
+
 /* Measurement aid: dbf_stack_gemv with HIP events recorded on `hip_stream` around its
  * launches.  Blocks until the last launch has finished.  *ms_first is the elapsed time of the
  * first kernel (the whole pass for DBF_GEMV_MFMA, the B stage for the two-launch kinds),

@@ -26,6 +26,7 @@ GEMM_AUTO, GEMM_I8 = 0, 2
  TUNE_FP4_MAX_ITEMS) = range(16)
 MAX_BATCH = 16
 GEMM_STATIC_BYTES = 32 << 20  # DBF_GEMM_STATIC_BYTES
+F16, BF16, F32 = 0, 1, 2  # element types (DBF_F16, ...)
 
 EXPORTS = [
     "dbf_pack", "dbf_pack_bits", "dbf_unpack_bits", "dbf_dims", "dbf_free",
@@ -35,10 +36,45 @@ EXPORTS = [
     "dbf_stack_create", "dbf_stack_create_grouped", "dbf_stack_offsets", "dbf_stack_gemv", "dbf_stack_gemv_timed",
     "dbf_stack_sync_timeouts", "dbf_stack_free",
     "dbf_prune_middle", "dbf_svid_workspace_bytes", "dbf_svid", "dbf_admm_workspace_bytes", "dbf_admm_step", "dbf_admm_prepare_workspace_bytes", "dbf_admm_prepare", "dbf_probe_read", "dbf_probe_mfma", "dbf_strerror",
+    "dbf_cache_bytes", "dbf_block_tables", "dbf_qk_norm_rope", "dbf_cache_append", "dbf_cache_read",
+    "dbf_cache_attend_workspace_bytes", "dbf_cache_attend", "dbf_token_logprobs_workspace_bytes", "dbf_token_logprobs",
     "dbf_tuning_set", "dbf_tuning_get", "dbf_tuning_reset",
 ]
 
 _lib = None
+
+
+class _Described(C.Structure):
+    """A descriptor of the C ABI: made once from keyword arguments (an unknown one is an error), passed to calls as it is."""
+
+    def __init__(self, **fields):
+        unknown = set(fields) - {name for name, _ in self._fields_}
+        if unknown:
+            raise TypeError("%s has no %s" % (type(self).__name__, ", ".join(sorted(unknown))))
+        super().__init__(**fields)
+
+
+class Cache(_Described):
+    """dbf_cache: pages of keys and values in 4 bits, in device memory of the caller's."""
+    _fields_ = [("data", C.c_void_p), ("n_pages", C.c_int), ("page_tokens", C.c_int), ("n_kv_heads", C.c_int), ("head_dim", C.c_int)]
+
+
+class Heads(_Described):
+    """dbf_heads: the query, key and value heads of a pass's tokens, and what norm and rotation they get."""
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("q_stride", C.c_longlong), ("k_stride", C.c_longlong), ("v_stride", C.c_longlong),
+                ("q_out", C.c_void_p), ("k_out", C.c_void_p), ("q_out_stride", C.c_longlong), ("k_out_stride", C.c_longlong),
+                ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("rope", C.c_void_p), ("positions", C.c_void_p),
+                ("dtype", C.c_int), ("n_tokens", C.c_int), ("n_q_heads", C.c_int), ("n_kv_heads", C.c_int), ("head_dim", C.c_int),
+                ("rope_len", C.c_int), ("rot_dim", C.c_int), ("interleaved", C.c_int), ("eps", C.c_float)]
+
+
+class Attend(_Described):
+    """dbf_attend: query rows, requests and their tables."""
+    _fields_ = [("q", C.c_void_p), ("out", C.c_void_p), ("q_stride", C.c_longlong), ("out_stride", C.c_longlong),
+                ("q_start", C.c_void_p), ("kv_len", C.c_void_p), ("block_table", C.c_void_p),
+                ("dtype", C.c_int), ("n_tokens", C.c_int), ("n_seq", C.c_int), ("n_q_heads", C.c_int), ("max_q", C.c_int),
+                ("max_kv", C.c_int), ("table_stride", C.c_int), ("causal", C.c_int), ("scale", C.c_float)]
 
 
 class DbfError(RuntimeError):
@@ -97,6 +133,18 @@ def lib() -> C.CDLL:
     L.dbf_admm_prepare.argtypes = [vp, vp, vp, vp, i32, i32, i32, C.c_float, vp, vp, vp, sz, vp, vp]
     L.dbf_probe_read.argtypes = [vp, sz, vp, vp]
     L.dbf_probe_mfma.argtypes = [i32, i32, i32, i32, vp, vp, C.POINTER(C.c_double)]
+    L.dbf_cache_bytes.argtypes = [i32, i32, i32, i32]
+    L.dbf_cache_bytes.restype = sz
+    L.dbf_block_tables.argtypes = [vp, vp, i32, i32, vp, i32, vp, i32, i32, vp, vp, vp, vp, vp, vp]
+    L.dbf_qk_norm_rope.argtypes = [C.POINTER(Heads), vp]
+    L.dbf_cache_append.argtypes = [C.POINTER(Heads), C.POINTER(Cache), vp, vp]
+    L.dbf_cache_read.argtypes = [C.POINTER(Cache), vp, i32, vp, vp, i32, vp]
+    L.dbf_cache_attend_workspace_bytes.argtypes = [C.POINTER(Attend), C.POINTER(Cache)]
+    L.dbf_cache_attend_workspace_bytes.restype = sz
+    L.dbf_cache_attend.argtypes = [C.POINTER(Attend), C.POINTER(Cache), vp, sz, vp]
+    L.dbf_token_logprobs_workspace_bytes.argtypes = [i32, i32, i32]
+    L.dbf_token_logprobs_workspace_bytes.restype = sz
+    L.dbf_token_logprobs.argtypes = [vp, i32, C.c_longlong, i32, i32, vp, i32, vp, vp, vp, vp, vp, sz, vp]
     L.dbf_tuning_set.argtypes = [i32, i32]
     L.dbf_tuning_get.argtypes = [i32]
     L.dbf_tuning_reset.argtypes = []
@@ -344,6 +392,50 @@ def dbf_stack_gemv_timed(stack: Stack, x_ptr: int, y_ptr: int, batch: int, strea
     _check(lib().dbf_stack_gemv_timed(stack.handle, x_ptr, y_ptr, batch, kind, stream, C.byref(mb), C.byref(ma)),
            "dbf_stack_gemv_timed")
     return float(mb.value), float(ma.value)
+
+
+# ---- between the layer products of a token pass ---------------------------------------------------------
+
+
+def dbf_cache_bytes(n_pages: int, page_tokens: int, n_kv_heads: int, head_dim: int) -> int:
+    return int(lib().dbf_cache_bytes(n_pages, page_tokens, n_kv_heads, head_dim))
+
+
+def dbf_block_tables(cached_len_ptr: int, new_len_ptr: int, n_seq: int, page_tokens: int, free_pages_ptr: int, n_free: int, block_table_ptr: int,
+                     table_stride: int, max_tokens: int, q_start_ptr: int, kv_len_ptr: int, positions_ptr: int, slots_ptr: int, status_ptr: int,
+                     stream: int = 0) -> None:
+    _check(lib().dbf_block_tables(cached_len_ptr, new_len_ptr, n_seq, page_tokens, free_pages_ptr, n_free, block_table_ptr, table_stride, max_tokens,
+                                  q_start_ptr, kv_len_ptr, positions_ptr, slots_ptr, status_ptr, stream), "dbf_block_tables")
+
+
+def dbf_qk_norm_rope(heads: Heads, stream: int = 0) -> None:
+    _check(lib().dbf_qk_norm_rope(heads, stream), "dbf_qk_norm_rope")
+
+
+def dbf_cache_append(heads: Heads, cache: Cache, slots_ptr: int, stream: int = 0) -> None:
+    _check(lib().dbf_cache_append(heads, cache, slots_ptr, stream), "dbf_cache_append")
+
+
+def dbf_cache_read(cache: Cache, slots_ptr: int, n_tokens: int, k_ptr: int, v_ptr: int, dtype: int = F16, stream: int = 0) -> None:
+    _check(lib().dbf_cache_read(cache, slots_ptr, n_tokens, k_ptr, v_ptr, dtype, stream), "dbf_cache_read")
+
+
+def dbf_cache_attend_workspace_bytes(attend: Attend, cache: Cache) -> int:
+    return int(lib().dbf_cache_attend_workspace_bytes(attend, cache))
+
+
+def dbf_cache_attend(attend: Attend, cache: Cache, ws_ptr: int, ws_bytes: int, stream: int = 0) -> None:
+    _check(lib().dbf_cache_attend(attend, cache, ws_ptr, ws_bytes, stream), "dbf_cache_attend")
+
+
+def dbf_token_logprobs_workspace_bytes(n_rows: int, vocab: int, n_top: int) -> int:
+    return int(lib().dbf_token_logprobs_workspace_bytes(n_rows, vocab, n_top))
+
+
+def dbf_token_logprobs(logits_ptr: int, dtype: int, row_stride: int, n_rows: int, vocab: int, targets_ptr: int, n_top: int, logprob_ptr: int,
+                       entropy_ptr: int, top_ids_ptr: int, top_logprobs_ptr: int, ws_ptr: int, ws_bytes: int, stream: int = 0) -> None:
+    _check(lib().dbf_token_logprobs(logits_ptr, dtype, row_stride, n_rows, vocab, targets_ptr, n_top, logprob_ptr, entropy_ptr, top_ids_ptr,
+                                    top_logprobs_ptr, ws_ptr, ws_bytes, stream), "dbf_token_logprobs")
 
 
 def dbf_probe_read(src_ptr: int, nbytes: int, sink_ptr: int = 0, stream: int = 0) -> None:

@@ -29,6 +29,10 @@ SOURCES = [
     "dbf_prune.hip",
     "dbf_svid.hip",
     "dbf_admm.hip",
+    "dbf_tables.hip",
+    "dbf_heads.hip",
+    "dbf_attend.hip",
+    "dbf_logprobs.hip",
 ]
 
 FLAGS = [
