@@ -13,8 +13,13 @@ struct AttendArgs {
     const int *q_start, *kv_len, *table;
     const uint8_t* cache;
     int n_tokens, n_seq, n_q, n_kv, max_q, max_kv, table_stride, causal, n_pages, page_shift, dim;
+    int group;             // query heads of a key head
+    int chunk, parts;      // tokens of a part of the long axis; parts of the longest request
     float scale;
+    float *part_out, *part_stat;   // of parts: sums [request][head][part][row][head_dim], maximum and sum of the row [..][2]
 };
+constexpr float LOWEST = -3.0e38f;   // of a running maximum: below all scores, and its difference from one is a number
+constexpr int FEW = 16;              // rows (tokens times heads) of a request and key head that are few
 
 // A request's rows and tokens; ok: they are what the call allows.
 struct Request {
@@ -29,6 +34,313 @@ __device__ __forceinline__ Request request(const AttendArgs& a, int i) {
     r.kv = a.kv_len[i];
     r.ok = r.kv >= 0 && r.kv <= a.max_kv && r.kv <= (long long)a.table_stride << a.page_shift && r.rows <= a.max_q;
     return r;
+}
+
+// The wavefront's lanes l, l + 16, l + 32, l + 48 hold parts of one column: their maximum or sum, in all of them.
+__device__ __forceinline__ float column_max(float v) {
+    const unsigned b = __builtin_bit_cast(unsigned, v);
+    const auto r = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+    const unsigned c = __builtin_bit_cast(unsigned, fmaxf(__builtin_bit_cast(float, (unsigned)r[0]), __builtin_bit_cast(float, (unsigned)r[1])));
+    const auto t = __builtin_amdgcn_permlane32_swap(c, c, false, false);
+    return fmaxf(__builtin_bit_cast(float, (unsigned)t[0]), __builtin_bit_cast(float, (unsigned)t[1]));
+}
+__device__ __forceinline__ float column_sum(float v) {
+    const unsigned b = __builtin_bit_cast(unsigned, v);
+    const auto r = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+    const unsigned c = __builtin_bit_cast(unsigned, __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]));
+    const auto t = __builtin_amdgcn_permlane32_swap(c, c, false, false);
+    return __builtin_bit_cast(float, (unsigned)t[0]) + __builtin_bit_cast(float, (unsigned)t[1]);
+}
+
+template <typename T>
+__device__ __forceinline__ void load8(const T* at, float (&v)[8]) {   // of any alignment
+    const dbf_u4 w = *reinterpret_cast<const dbf_u4_any*>(at);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = dbf_to_float(__builtin_bit_cast(T, (uint16_t)(w[e >> 1] >> 16 * (e & 1))));
+}
+
+// The 16 codes of a lane's 8 bytes as two operands of the 16x16x32 product, the even and the odd ones.  A code is left where it lies in an fp16: as the
+// subnormal number c 2^-24, or 16 c 2^-24 for the odd ones, which the matrix cores take as they are.
+__device__ __forceinline__ void operands(unsigned w0, unsigned w1, dbf_h8& even, dbf_h8& odd) {
+    const dbf_u4 e = {w0 & 0x000F000Fu, w0 >> 8 & 0x000F000Fu, w1 & 0x000F000Fu, w1 >> 8 & 0x000F000Fu};
+    const dbf_u4 o = {w0 & 0x00F000F0u, w0 >> 8 & 0x00F000F0u, w1 & 0x00F000F0u, w1 >> 8 & 0x00F000F0u};
+    even = __builtin_bit_cast(dbf_h8, e);
+    odd = __builtin_bit_cast(dbf_h8, o);
+}
+
+// Four codes' bytes of a word, tokens 0 .. 3 with a value in the low and one in the high half of a byte, as fp16 values s c - s z (exact: 7 bits times 4), the
+// pairs of tokens 0, 2 and 1, 3 of the low value and of the high one.  s and b: the pairs' scales and zeros.  (1024 + c is fp16's 1024 with c in its last bits.)
+__device__ __forceinline__ void values(unsigned u, dbf_h2 s02, dbf_h2 b02, dbf_h2 s13, dbf_h2 b13, unsigned& lo02, unsigned& lo13, unsigned& hi02, unsigned& hi13) {
+    const dbf_h2 less = {(_Float16)-1024.f, (_Float16)-1024.f}, part = {(_Float16)0.0625f, (_Float16)0.0625f}, less_part = {(_Float16)-64.f, (_Float16)-64.f};
+    auto code = [](unsigned v) { return __builtin_bit_cast(dbf_h2, v | 0x64006400u); };
+    auto value = [](dbf_h2 c, dbf_h2 s, dbf_h2 b) { return __builtin_bit_cast(unsigned, __builtin_elementwise_fma(c, s, b)); };
+    lo02 = value(code(u & 0x000F000Fu) + less, s02, b02);
+    lo13 = value(code(u >> 8 & 0x000F000Fu) + less, s13, b13);
+    hi02 = value(__builtin_elementwise_fma(code(u & 0x00F000F0u), part, less_part), s02, b02);
+    hi13 = value(__builtin_elementwise_fma(code(u >> 8 & 0x00F000F0u), part, less_part), s13, b13);
+}
+// The low or the high halves of two words.
+__device__ __forceinline__ dbf_h2 lows(unsigned a, unsigned b) { return __builtin_bit_cast(dbf_h2, __builtin_amdgcn_perm(b, a, 0x05040100u)); }
+__device__ __forceinline__ dbf_h2 highs(unsigned a, unsigned b) { return __builtin_bit_cast(dbf_h2, __builtin_amdgcn_perm(b, a, 0x07060302u)); }
+
+// What a lane holds of a record of 32 tokens: of tokens 16 t + (lane & 15), the keys' bytes of its 16 N values; of the group's words, those of tokens
+// 16 t + 4 (lane >> 4) ..; of the values, both runs of 16 tokens of its place.
+template <int N>
+struct Record {
+    unsigned k[2][2 * N];
+    dbf_u4 kw[2][N], v[N], vw[2][N];
+    __device__ __forceinline__ void load(const uint8_t* rec, int lane) {
+        const int g = lane >> 4, r = lane & 15;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const uint8_t* at = rec + (16 * t + r) * 32 * N + 8 * N * g;
+            if constexpr (N == 1) {
+                const dbf_u2 w = *reinterpret_cast<const dbf_u2*>(at);
+                k[t][0] = w[0], k[t][1] = w[1];
+            } else {
+#pragma unroll
+                for (int e = 0; e < N / 2; ++e) {
+                    const dbf_u4 w = *reinterpret_cast<const dbf_u4*>(at + 16 * e);
+#pragma unroll
+                    for (int f = 0; f < 4; ++f) k[t][4 * e + f] = w[f];
+                }
+            }
+#pragma unroll
+            for (int p = 0; p < N; ++p) {
+                const uint8_t* words = rec + 2048 * N + 128 * p + 64 * t + 16 * g;
+                kw[t][p] = *reinterpret_cast<const dbf_u4*>(words);
+                vw[t][p] = *reinterpret_cast<const dbf_u4*>(words + 128 * N);
+            }
+        }
+#pragma unroll
+        for (int p = 0; p < N; ++p) v[p] = *reinterpret_cast<const dbf_u4*>(rec + 1024 * N + 1024 * p + 16 * lane);
+    }
+};
+__device__ __forceinline__ dbf_h2 word(unsigned w) { return __builtin_bit_cast(dbf_h2, w); }
+
+// Few rows: those of a request and key head are columns of one 16-wide product (the rows' tokens times the heads that share the keys), the long axis is cut
+// into parts, a workgroup's part goes by records of 32 tokens to its four wavefronts, each with statistics of its own.
+//   scores:  K q^T, 16 tokens x 16 columns x the 64 values of a group; x = sum over groups of s (c . q) - s z sum q: the scale and the zero come on the sums,
+//            so codes go to the matrix cores as they are.  q is scaled by a power of two to the top of fp16's range, and exact there.
+//   weights: e^(x - m) with m a maximum that may lag: it is raised when some score is more than 2^8 above it, so that a step that raises none
+//            (nearly all) joins no lanes and touches no sums.  Rounded to fp16 for the product, times 2^7: a weight 2^-21 of the largest still has all its bits.
+//   output:  V^T p^T, 16 values of a group x 16 columns x 32 tokens, of values made exact in fp16.  (Scales on the weights instead of the values were fewer
+//            instructions, but their rounding does not cancel between c and z: values near zero lost three bits.)
+template <typename T, int N>
+__global__ __launch_bounds__(256) void dbf_attend_few_kernel(const AttendArgs a) {
+    constexpr int D = 64 * N;
+    __shared__ float sums[4][FEW][N == 1 ? 64 : 128], stats[4][2][FEW];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
+    const int part = blockIdx.x, head = blockIdx.y, req = blockIdx.z, G = a.group;
+    const Request r = request(a, req);
+    const int cols = min(r.rows, a.max_q) * G;
+    if (!cols) return;
+    const int begin = part * a.chunk, end = r.ok ? min(begin + a.chunk, r.kv) : 0;
+    if (part > 0 && begin >= end) return;
+    // the column's query, by groups
+    dbf_h8 qe[N], qo[N];
+    float Q[N], kappa;
+    {
+        const bool live = c < cols;
+        const T* at = static_cast<const T*>(a.q) + (long long)(r.row0 + (live ? c / G : 0)) * a.q_stride + (long long)(head * G + (live ? c % G : 0)) * D + 16 * N * g;
+        float v[N][16], most = 0.f;
+#pragma unroll
+        for (int p = 0; p < N; ++p) {
+            float x[2][8];
+            load8(at + 16 * p, x[0]);
+            load8(at + 16 * p + 8, x[1]);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                v[p][e] = live ? x[e >> 3][e & 7] : 0.f;
+                most = fmaxf(most, fabsf(v[p][e]));
+            }
+        }
+        most = column_max(most);
+        const int up = most > 0.f && most < __builtin_inff() ? 14 - __builtin_amdgcn_frexp_expf(most) : 0;
+        kappa = ldexpf(a.scale * 1.44269504089f, 24 - up);
+#pragma unroll
+        for (int p = 0; p < N; ++p) {
+            float sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int d = 8 * (e >> 2) + 4 * (e & 1) + (e & 2);
+                const _Float16 lo = (_Float16)ldexpf(v[p][d], up), hi = (_Float16)ldexpf(v[p][d + 1], up);
+                qe[p][e] = lo;
+                qo[p][e] = hi * (_Float16)0.0625f;
+                sum += (float)lo + (float)hi;
+            }
+            Q[p] = column_sum(sum) * 0x1p-24f;
+        }
+    }
+    const int seen = a.causal ? r.kv - r.rows + c / G + 1 : r.kv;   // tokens that the column sees
+    const int all_see = a.causal ? r.kv - r.rows + 1 : r.kv;        // ... that all columns see
+    float m = LOWEST, l = 0.f;
+    dbf_f4 o[4 * N] = {};
+    const int* table = a.table + (long long)req * a.table_stride;
+    const int first = begin / 32 + wave, last = (end + 31) / 32 - 1, per_page = a.page_shift - 5;
+    bool known, known_next;
+    auto at = [&](int b, bool& is) {
+        const int page = table[b >> per_page];
+        is = (unsigned)page < (unsigned)a.n_pages;
+        return a.cache + ((((long long)(is ? page : 0) * a.n_kv + head) << per_page) + (b & ((1 << per_page) - 1))) * dbf_record_bytes(D);
+    };
+    Record<N> now, next;
+    if (first <= last) now.load(at(first, known), lane);
+    for (int b = first; b <= last; b += 4) {
+        next.load(at(min(b + 4, last), known_next), lane);
+        float x[2][4] = {};
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+#pragma unroll
+            for (int p = 0; p < N; ++p) {
+                dbf_h8 even, odd;
+                operands(now.k[t][2 * p], now.k[t][2 * p + 1], even, odd);
+                dbf_f4 acc = {0.f, 0.f, 0.f, 0.f};
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(even, qe[p], acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(odd, qo[p], acc, 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const dbf_h2 sb = word(now.kw[t][p][i]);
+                    x[t][i] = fmaf((float)sb[0], acc[i], x[t][i]);
+                    x[t][i] = fmaf((float)sb[1], Q[p], x[t][i]);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[t][i] *= kappa;
+        }
+        if (32 * b + 32 > all_see || !known) {   // tokens that are not there for all: no scores, and no words (what lies there may be no number)
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int j = 32 * b + 16 * t + 4 * g + i;
+                    x[t][i] = j < seen ? (known ? x[t][i] : __builtin_nanf("")) : -__builtin_inff();
+#pragma unroll
+                    for (int p = 0; p < N; ++p) now.vw[t][p][i] = known && j < r.kv ? now.vw[t][p][i] : 0u;
+                }
+        }
+        float most = LOWEST;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) most = fmaxf(most, x[t][i]);
+        if (__any(most > m + 8.f)) {
+            const float to = fmaxf(m, column_max(most)), keep = __builtin_amdgcn_exp2f(m - to);
+            m = to;
+            l *= keep;
+#pragma unroll
+            for (int j = 0; j < 4 * N; ++j) o[j] *= keep;
+        }
+        dbf_h8 weights;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float w = __builtin_amdgcn_exp2f(x[t][i] - m + 7.f);
+                l += w;
+                weights[4 * t + 2 * (i & 1) + (i >> 1)] = (_Float16)w;
+            }
+#pragma unroll
+        for (int p = 0; p < N; ++p) {
+            dbf_h2 s02[2], s13[2], b02[2], b13[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const dbf_u4 w = now.vw[t][p];
+                s02[t] = lows(w[0], w[2]);
+                s13[t] = lows(w[1], w[3]);
+                b02[t] = highs(w[0], w[2]);
+                b13[t] = highs(w[1], w[3]);
+            }
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                unsigned lo[4], hi[4];
+#pragma unroll
+                for (int t = 0; t < 2; ++t) values(now.v[p][2 * q + t], s02[t], b02[t], s13[t], b13[t], lo[2 * t], lo[2 * t + 1], hi[2 * t], hi[2 * t + 1]);
+                const dbf_h8 low = __builtin_bit_cast(dbf_h8, (dbf_u4){lo[0], lo[1], lo[2], lo[3]}), high = __builtin_bit_cast(dbf_h8, (dbf_u4){hi[0], hi[1], hi[2], hi[3]});
+                o[p + N * (2 * q)] = __builtin_amdgcn_mfma_f32_16x16x32_f16(low, weights, o[p + N * (2 * q)], 0, 0, 0);
+                o[p + N * (2 * q + 1)] = __builtin_amdgcn_mfma_f32_16x16x32_f16(high, weights, o[p + N * (2 * q + 1)], 0, 0, 0);
+            }
+        }
+        now = next;
+        known = known_next;
+    }
+    // the four wavefronts' sums
+    l = column_sum(l);
+    if (g == 0) {
+        stats[wave][0][c] = m;
+        stats[wave][1][c] = l;
+    }
+    constexpr int SPAN = N == 1 ? 64 : 128;
+    for (int d0 = 0; d0 < D; d0 += SPAN) {
+        if (d0) __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 4 * N; ++j)
+            if (16 * j >= d0 && 16 * j < d0 + SPAN) *reinterpret_cast<dbf_f4*>(&sums[wave][c][16 * j - d0 + 4 * g]) = o[j];
+        __syncthreads();
+        for (int e = threadIdx.x; e < cols * SPAN; e += 256) {
+            const int col = e / SPAN, d = e % SPAN;
+            float most = stats[0][0][col];
+            for (int w = 1; w < 4; ++w) most = fmaxf(most, stats[w][0][col]);
+            float y = 0.f, sum = 0.f;
+            for (int w = 0; w < 4; ++w) {
+                const float keep = __builtin_amdgcn_exp2f(stats[w][0][col] - most);
+                y = fmaf(keep, sums[w][col][d], y);
+                sum = fmaf(keep, stats[w][1][col], sum);
+            }
+            if (a.parts == 1) {
+                T* out = static_cast<T*>(a.out) + (long long)(r.row0 + col / G) * a.out_stride + (long long)(head * G + col % G) * D + d0 + d;
+                *out = dbf_from_float<T>(!r.ok ? __builtin_nanf("") : sum == 0.f ? 0.f : y / sum);
+            } else {
+                const long long at = (((long long)req * a.n_kv + head) * a.parts + part) * (a.max_q * G) + col;
+                a.part_out[at * D + d0 + d] = y;
+                if (d0 + d == 0) {
+                    a.part_stat[2 * at] = most;
+                    a.part_stat[2 * at + 1] = sum;
+                }
+            }
+        }
+    }
+}
+
+// The parts of a row, joined in their order: a workgroup to a row and head.
+template <typename T>
+__global__ __launch_bounds__(256) void dbf_attend_join_kernel(const AttendArgs a) {
+    __shared__ float sums[256][4], total[4];
+    const int tid = threadIdx.x, req = blockIdx.z, head = blockIdx.y, col = blockIdx.x, D = a.dim, G = a.group, per = D / 4, lanes = 256 / per;
+    const Request r = request(a, req);
+    if (col >= min(r.rows, a.max_q) * G) return;
+    const int parts = r.ok ? (r.kv + a.chunk - 1) / a.chunk : 0, d = tid % per, turn = tid / per;
+    const long long step = a.max_q * G, first = ((long long)req * a.n_kv + head) * a.parts * step + col;
+    float most = LOWEST;
+    for (int p = tid; p < parts; p += 256) most = fmaxf(most, a.part_stat[2 * (first + p * step)]);
+    most = dbf_wave_max(most);
+    if ((tid & 63) == 0) total[tid >> 6] = most;
+    __syncthreads();
+    most = fmaxf(fmaxf(total[0], total[1]), fmaxf(total[2], total[3]));
+    dbf_f4 y = {0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f;
+    for (int p = turn; p < parts; p += lanes) {
+        const long long at = first + p * step;
+        const float keep = __builtin_amdgcn_exp2f(a.part_stat[2 * at] - most);
+        const dbf_f4 x = *reinterpret_cast<const dbf_f4*>(a.part_out + at * D + 4 * d);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = fmaf(keep, x[i], y[i]);
+        sum = fmaf(keep, a.part_stat[2 * at + 1], sum);
+    }
+    __syncthreads();
+    *reinterpret_cast<dbf_f4*>(sums[tid]) = y;
+    __shared__ float of[256];
+    of[tid] = sum;
+    __syncthreads();
+    if (turn) return;
+    for (int k = 1; k < lanes; ++k) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] += sums[k * per + d][i];
+        sum += of[k * per + d];
+    }
+    T* out = static_cast<T*>(a.out) + (long long)(r.row0 + col / G) * a.out_stride + (long long)(head * G + col % G) * D + 4 * d;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[i] = dbf_from_float<T>(!r.ok ? __builtin_nanf("") : sum == 0.f ? 0.f : y[i] / sum);
 }
 
 // A workgroup to a row and head.
@@ -109,11 +421,54 @@ int check_attend(const dbf_attend* a, const dbf_cache* c) {
     return DBF_OK;
 }
 
+// How a call is cut: tokens of a part, parts of the longest request, bytes of their sums.
+struct Cut {
+    bool few;
+    int chunk, parts;
+    size_t out_bytes, stat_bytes;
+};
+Cut cut_of(const dbf_attend* a, const dbf_cache* c) {
+    Cut k = {};
+    const int G = a->n_q_heads / c->n_kv_heads;
+    k.few = (long long)a->max_q * G <= FEW;
+    k.chunk = INT_MAX;
+    k.parts = 1;
+    if (k.few && a->max_kv > 0) {
+        const long long rows = (long long)a->n_seq * c->n_kv_heads;
+        // parts: as many workgroups as the chip holds four times over, of 256 tokens at least
+        long long parts = (4096 + rows - 1) / rows, chunk = (a->max_kv + parts - 1) / parts;
+        chunk = (chunk + 127) / 128 * 128;
+        if (chunk < 512) chunk = 512;
+        k.chunk = (int)(chunk > INT_MAX / 2 ? INT_MAX / 2 : chunk);
+        k.parts = (int)((a->max_kv + (long long)k.chunk - 1) / k.chunk);
+        if (k.parts > 1) {
+            const size_t n = (size_t)rows * k.parts * (size_t)(a->max_q * G);
+            k.out_bytes = n * c->head_dim * 4;
+            k.stat_bytes = (n * 8 + 255) / 256 * 256;
+        }
+    }
+    return k;
+}
+
+template <typename T>
+int launch_attend(const AttendArgs& a, const Cut& cut, hipStream_t stream) {
+    if (!cut.few) {
+        hipLaunchKernelGGL(dbf_attend_simple_kernel<T>, dim3(a.max_q, a.n_q, a.n_seq), dim3(256), 0, stream, a);
+        return hipGetLastError() == hipSuccess ? DBF_OK : DBF_EHIP;
+    }
+    const auto kernel = a.dim == 64 ? dbf_attend_few_kernel<T, 1> : a.dim == 128 ? dbf_attend_few_kernel<T, 2> : dbf_attend_few_kernel<T, 4>;
+    hipLaunchKernelGGL(kernel, dim3(a.parts, a.n_kv, a.n_seq), dim3(256), 0, stream, a);
+    if (hipGetLastError() != hipSuccess) return DBF_EHIP;
+    if (a.parts > 1) hipLaunchKernelGGL(dbf_attend_join_kernel<T>, dim3(a.max_q * a.group, a.n_kv, a.n_seq), dim3(256), 0, stream, a);
+    return hipGetLastError() == hipSuccess ? DBF_OK : DBF_EHIP;
+}
+
 }  // namespace
 
 extern "C" size_t dbf_cache_attend_workspace_bytes(const dbf_attend* attend, const dbf_cache* cache) {
     if (check_attend(attend, cache)) return 0;
-    return 0;
+    const Cut cut = cut_of(attend, cache);
+    return cut.out_bytes + cut.stat_bytes;
 }
 
 extern "C" int dbf_cache_attend(const dbf_attend* attend, const dbf_cache* cache, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
@@ -131,7 +486,13 @@ extern "C" int dbf_cache_attend(const dbf_attend* attend, const dbf_cache* cache
     a.n_tokens = attend->n_tokens;  a.n_seq = attend->n_seq;  a.n_q = attend->n_q_heads;  a.n_kv = cache->n_kv_heads;
     a.max_q = attend->max_q;  a.max_kv = attend->max_kv;  a.table_stride = attend->table_stride;  a.causal = attend->causal;
     a.n_pages = cache->n_pages;  a.page_shift = dbf_page_shift(cache->page_tokens);  a.dim = cache->head_dim;  a.scale = attend->scale;
-    const auto kernel = attend->dtype == DBF_F16 ? dbf_attend_simple_kernel<_Float16> : dbf_attend_simple_kernel<dbf_bf16>;
-    hipLaunchKernelGGL(kernel, dim3(a.max_q, a.n_q, a.n_seq), dim3(256), 0, static_cast<hipStream_t>(hip_stream), a);
-    return hipGetLastError() == hipSuccess ? DBF_OK : DBF_EHIP;
+    const Cut cut = cut_of(attend, cache);
+    if (cut.out_bytes) {
+        if (!workspace_dev || dbf_misaligned(workspace_dev, 256) || workspace_bytes < cut.out_bytes + cut.stat_bytes) return DBF_EWORKSPACE;
+        a.part_stat = static_cast<float*>(workspace_dev);
+        a.part_out = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + cut.stat_bytes);
+    }
+    a.group = a.n_q / a.n_kv;  a.chunk = cut.chunk;  a.parts = cut.parts;
+    const auto stream = static_cast<hipStream_t>(hip_stream);
+    return attend->dtype == DBF_F16 ? launch_attend<_Float16>(a, cut, stream) : launch_attend<dbf_bf16>(a, cut, stream);
 }
