@@ -1,4 +1,5 @@
 // Attention over the cache in 4 bits (include/dbf.h, dbf_cache_attend).
+#include <algorithm>
 #include <initializer_list>
 
 #include "dbf_cache.h"
@@ -19,6 +20,7 @@ struct AttendArgs {
     float *part_out, *part_stat;   // of parts: sums [request][head][part][row][head_dim], maximum and sum of the row [..][2]
 };
 constexpr float LOWEST = -3.0e38f;   // of a running maximum: below all scores, and its difference from one is a number
+constexpr int MOST_PARTS = 512;      // of the long axis
 constexpr int FEW = 16;              // rows (tokens times heads) of a request and key head that are few
 
 // A request's rows and tokens; ok: they are what the call allows.
@@ -79,16 +81,16 @@ __device__ __forceinline__ void values(unsigned u, dbf_h2 s02, dbf_h2 b02, dbf_h
     hi02 = value(__builtin_elementwise_fma(code(u & 0x00F000F0u), part, less_part), s02, b02);
     hi13 = value(__builtin_elementwise_fma(code(u >> 8 & 0x00F000F0u), part, less_part), s13, b13);
 }
+__device__ __forceinline__ dbf_h2 word(unsigned w) { return __builtin_bit_cast(dbf_h2, w); }
 // The low or the high halves of two words.
 __device__ __forceinline__ dbf_h2 lows(unsigned a, unsigned b) { return __builtin_bit_cast(dbf_h2, __builtin_amdgcn_perm(b, a, 0x05040100u)); }
 __device__ __forceinline__ dbf_h2 highs(unsigned a, unsigned b) { return __builtin_bit_cast(dbf_h2, __builtin_amdgcn_perm(b, a, 0x07060302u)); }
 
-// What a lane holds of a record of 32 tokens: of tokens 16 t + (lane & 15), the keys' bytes of its 16 N values; of the group's words, those of tokens
-// 16 t + 4 (lane >> 4) ..; of the values, both runs of 16 tokens of its place.
+// What a lane holds of a record's keys: of tokens 16 t + (lane & 15), the bytes of its 16 N values; the groups' words of tokens 16 t + 4 (lane >> 4) ..
 template <int N>
-struct Record {
+struct Keys {
     unsigned k[2][2 * N];
-    dbf_u4 kw[2][N], v[N], vw[2][N];
+    dbf_u4 words[2][N];
     __device__ __forceinline__ void load(const uint8_t* rec, int lane) {
         const int g = lane >> 4, r = lane & 15;
 #pragma unroll
@@ -106,17 +108,117 @@ struct Record {
                 }
             }
 #pragma unroll
-            for (int p = 0; p < N; ++p) {
-                const uint8_t* words = rec + 2048 * N + 128 * p + 64 * t + 16 * g;
-                kw[t][p] = *reinterpret_cast<const dbf_u4*>(words);
-                vw[t][p] = *reinterpret_cast<const dbf_u4*>(words + 128 * N);
-            }
+            for (int p = 0; p < N; ++p) words[t][p] = *reinterpret_cast<const dbf_u4*>(rec + 2048 * N + 128 * p + 64 * t + 16 * g);
         }
-#pragma unroll
-        for (int p = 0; p < N; ++p) v[p] = *reinterpret_cast<const dbf_u4*>(rec + 1024 * N + 1024 * p + 16 * lane);
     }
 };
-__device__ __forceinline__ dbf_h2 word(unsigned w) { return __builtin_bit_cast(dbf_h2, w); }
+// ... and of its values: both runs of 16 tokens of its place in a group, and the words as above.
+template <int N>
+struct Values {
+    dbf_u4 v[N], words[2][N];
+    __device__ __forceinline__ void load(const uint8_t* rec, int lane) {
+        const int g = lane >> 4;
+#pragma unroll
+        for (int p = 0; p < N; ++p) v[p] = *reinterpret_cast<const dbf_u4*>(rec + 1024 * N + 1024 * p + 16 * lane);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int p = 0; p < N; ++p) words[t][p] = *reinterpret_cast<const dbf_u4*>(rec + 2176 * N + 128 * p + 64 * t + 16 * g);
+    }
+};
+
+// A wavefront's sums for its 16 columns, and a step over one record.
+template <int N>
+struct Columns {
+    dbf_h8 qe[N], qo[N];         // the queries' even and odd values, the odd ones over 16
+    float Q[N], kappa, m, l;     // their sums; from sums of products to scores in powers of two; largest score so far, or a little less; sum of the weights
+    dbf_f4 o[4 * N];
+    int seen, kv;                // tokens that the column sees, and that there are
+
+    // x: the scores of tokens 16 t + 4 g + i
+    __device__ __forceinline__ void scores(const Keys<N>& keys, float kappa, float (&x)[2][4]) const {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[t][i] = 0.f;
+#pragma unroll
+            for (int p = 0; p < N; ++p) {
+                dbf_h8 even, odd;
+                operands(keys.k[t][2 * p], keys.k[t][2 * p + 1], even, odd);
+                dbf_f4 acc = {0.f, 0.f, 0.f, 0.f};
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(even, qe[p], acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(odd, qo[p], acc, 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const dbf_h2 sb = word(keys.words[t][p][i]);
+                    x[t][i] = fmaf((float)sb[0], acc[i], x[t][i]);
+                    x[t][i] = fmaf((float)sb[1], Q[p], x[t][i]);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[t][i] *= kappa;
+        }
+    }
+    // Tokens from `first` on that are not there for all: no scores, and no words (what lies there may be no number).
+    __device__ __forceinline__ void mask(int first, bool known, float (&x)[2][4], Values<N>& values) const {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int j = first + 16 * t + i;
+                x[t][i] = j < seen ? (known ? x[t][i] : __builtin_nanf("")) : -__builtin_inff();
+#pragma unroll
+                for (int p = 0; p < N; ++p) values.words[t][p][i] = known && j < kv ? values.words[t][p][i] : 0u;
+            }
+    }
+    __device__ __forceinline__ void raise(const float (&x)[2][4]) {
+        float most = LOWEST;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) most = fmaxf(most, x[t][i]);
+        if (__any(most > m + 8.f)) {
+            const float to = fmaxf(m, column_max(most)), keep = __builtin_amdgcn_exp2f(m - to);
+            m = to;
+            l *= keep;
+#pragma unroll
+            for (int j = 0; j < 4 * N; ++j) o[j] *= keep;
+        }
+    }
+    __device__ __forceinline__ void add(const float (&x)[2][4], const Values<N>& in) {
+        dbf_h8 weights;
+        const float from = m - 7.f;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float w = __builtin_amdgcn_exp2f(x[t][i] - from);
+                l += w;
+                weights[4 * t + 2 * (i & 1) + (i >> 1)] = (_Float16)w;
+            }
+#pragma unroll
+        for (int p = 0; p < N; ++p) {
+            dbf_h2 s02[2], s13[2], b02[2], b13[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const dbf_u4 w = in.words[t][p];
+                s02[t] = lows(w[0], w[2]);
+                s13[t] = lows(w[1], w[3]);
+                b02[t] = highs(w[0], w[2]);
+                b13[t] = highs(w[1], w[3]);
+            }
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                unsigned lo[4], hi[4];
+#pragma unroll
+                for (int t = 0; t < 2; ++t) values(in.v[p][2 * q + t], s02[t], b02[t], s13[t], b13[t], lo[2 * t], lo[2 * t + 1], hi[2 * t], hi[2 * t + 1]);
+                const dbf_h8 low = __builtin_bit_cast(dbf_h8, (dbf_u4){lo[0], lo[1], lo[2], lo[3]}), high = __builtin_bit_cast(dbf_h8, (dbf_u4){hi[0], hi[1], hi[2], hi[3]});
+                o[p + N * (2 * q)] = __builtin_amdgcn_mfma_f32_16x16x32_f16(low, weights, o[p + N * (2 * q)], 0, 0, 0);
+                o[p + N * (2 * q + 1)] = __builtin_amdgcn_mfma_f32_16x16x32_f16(high, weights, o[p + N * (2 * q + 1)], 0, 0, 0);
+            }
+        }
+    }
+};
 
 // Few rows: those of a request and key head are columns of one 16-wide product (the rows' tokens times the heads that share the keys), the long axis is cut
 // into parts, a workgroup's part goes by records of 32 tokens to its four wavefronts, each with statistics of its own.
@@ -127,7 +229,7 @@ __device__ __forceinline__ dbf_h2 word(unsigned w) { return __builtin_bit_cast(d
 //   output:  V^T p^T, 16 values of a group x 16 columns x 32 tokens, of values made exact in fp16.  (Scales on the weights instead of the values were fewer
 //            instructions, but their rounding does not cancel between c and z: values near zero lost three bits.)
 template <typename T, int N>
-__global__ __launch_bounds__(256) void dbf_attend_few_kernel(const AttendArgs a) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(N == 4 ? 2 : 3))) void dbf_attend_few_kernel(const AttendArgs a) {
     constexpr int D = 64 * N;
     __shared__ float sums[4][FEW][N == 1 ? 64 : 128], stats[4][2][FEW];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
@@ -138,8 +240,7 @@ __global__ __launch_bounds__(256) void dbf_attend_few_kernel(const AttendArgs a)
     const int begin = part * a.chunk, end = r.ok ? min(begin + a.chunk, r.kv) : 0;
     if (part > 0 && begin >= end) return;
     // the column's query, by groups
-    dbf_h8 qe[N], qo[N];
-    float Q[N], kappa;
+    Columns<N> s = {};
     {
         const bool live = c < cols;
         const T* at = static_cast<const T*>(a.q) + (long long)(r.row0 + (live ? c / G : 0)) * a.q_stride + (long long)(head * G + (live ? c % G : 0)) * D + 16 * N * g;
@@ -157,7 +258,7 @@ __global__ __launch_bounds__(256) void dbf_attend_few_kernel(const AttendArgs a)
         }
         most = column_max(most);
         const int up = most > 0.f && most < __builtin_inff() ? 14 - __builtin_amdgcn_frexp_expf(most) : 0;
-        kappa = ldexpf(a.scale * 1.44269504089f, 24 - up);
+        s.kappa = ldexpf(a.scale * 1.44269504089f, 24 - up);
 #pragma unroll
         for (int p = 0; p < N; ++p) {
             float sum = 0.f;
@@ -165,117 +266,57 @@ __global__ __launch_bounds__(256) void dbf_attend_few_kernel(const AttendArgs a)
             for (int e = 0; e < 8; ++e) {
                 const int d = 8 * (e >> 2) + 4 * (e & 1) + (e & 2);
                 const _Float16 lo = (_Float16)ldexpf(v[p][d], up), hi = (_Float16)ldexpf(v[p][d + 1], up);
-                qe[p][e] = lo;
-                qo[p][e] = hi * (_Float16)0.0625f;
+                s.qe[p][e] = lo;
+                s.qo[p][e] = hi * (_Float16)0.0625f;
                 sum += (float)lo + (float)hi;
             }
-            Q[p] = column_sum(sum) * 0x1p-24f;
+            s.Q[p] = column_sum(sum) * 0x1p-24f;
         }
     }
-    const int seen = a.causal ? r.kv - r.rows + c / G + 1 : r.kv;   // tokens that the column sees
-    const int all_see = a.causal ? r.kv - r.rows + 1 : r.kv;        // ... that all columns see
-    float m = LOWEST, l = 0.f;
-    dbf_f4 o[4 * N] = {};
+    s.seen = a.causal ? r.kv - r.rows + c / G + 1 : r.kv;
+    s.kv = r.kv;
+    s.m = LOWEST;
+    const int all_see = a.causal ? r.kv - r.rows + 1 : r.kv;   // tokens that all columns see
     const int* table = a.table + (long long)req * a.table_stride;
     const int first = begin / 32 + wave, last = (end + 31) / 32 - 1, per_page = a.page_shift - 5;
-    bool known, known_next;
+    bool known = true, known_next = true;
     auto at = [&](int b, bool& is) {
         const int page = table[b >> per_page];
         is = (unsigned)page < (unsigned)a.n_pages;
         return a.cache + ((((long long)(is ? page : 0) * a.n_kv + head) << per_page) + (b & ((1 << per_page) - 1))) * dbf_record_bytes(D);
     };
-    Record<N> now, next;
-    if (first <= last) now.load(at(first, known), lane);
-    for (int b = first; b <= last; b += 4) {
-        next.load(at(min(b + 4, last), known_next), lane);
-        float x[2][4] = {};
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-#pragma unroll
-            for (int p = 0; p < N; ++p) {
-                dbf_h8 even, odd;
-                operands(now.k[t][2 * p], now.k[t][2 * p + 1], even, odd);
-                dbf_f4 acc = {0.f, 0.f, 0.f, 0.f};
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(even, qe[p], acc, 0, 0, 0);
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(odd, qo[p], acc, 0, 0, 0);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const dbf_h2 sb = word(now.kw[t][p][i]);
-                    x[t][i] = fmaf((float)sb[0], acc[i], x[t][i]);
-                    x[t][i] = fmaf((float)sb[1], Q[p], x[t][i]);
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[t][i] *= kappa;
-        }
-        if (32 * b + 32 > all_see || !known) {   // tokens that are not there for all: no scores, and no words (what lies there may be no number)
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int j = 32 * b + 16 * t + 4 * g + i;
-                    x[t][i] = j < seen ? (known ? x[t][i] : __builtin_nanf("")) : -__builtin_inff();
-#pragma unroll
-                    for (int p = 0; p < N; ++p) now.vw[t][p][i] = known && j < r.kv ? now.vw[t][p][i] : 0u;
-                }
-        }
-        float most = LOWEST;
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) most = fmaxf(most, x[t][i]);
-        if (__any(most > m + 8.f)) {
-            const float to = fmaxf(m, column_max(most)), keep = __builtin_amdgcn_exp2f(m - to);
-            m = to;
-            l *= keep;
-#pragma unroll
-            for (int j = 0; j < 4 * N; ++j) o[j] *= keep;
-        }
-        dbf_h8 weights;
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float w = __builtin_amdgcn_exp2f(x[t][i] - m + 7.f);
-                l += w;
-                weights[4 * t + 2 * (i & 1) + (i >> 1)] = (_Float16)w;
-            }
-#pragma unroll
-        for (int p = 0; p < N; ++p) {
-            dbf_h2 s02[2], s13[2], b02[2], b13[2];
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const dbf_u4 w = now.vw[t][p];
-                s02[t] = lows(w[0], w[2]);
-                s13[t] = lows(w[1], w[3]);
-                b02[t] = highs(w[0], w[2]);
-                b13[t] = highs(w[1], w[3]);
-            }
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                unsigned lo[4], hi[4];
-#pragma unroll
-                for (int t = 0; t < 2; ++t) values(now.v[p][2 * q + t], s02[t], b02[t], s13[t], b13[t], lo[2 * t], lo[2 * t + 1], hi[2 * t], hi[2 * t + 1]);
-                const dbf_h8 low = __builtin_bit_cast(dbf_h8, (dbf_u4){lo[0], lo[1], lo[2], lo[3]}), high = __builtin_bit_cast(dbf_h8, (dbf_u4){hi[0], hi[1], hi[2], hi[3]});
-                o[p + N * (2 * q)] = __builtin_amdgcn_mfma_f32_16x16x32_f16(low, weights, o[p + N * (2 * q)], 0, 0, 0);
-                o[p + N * (2 * q + 1)] = __builtin_amdgcn_mfma_f32_16x16x32_f16(high, weights, o[p + N * (2 * q + 1)], 0, 0, 0);
-            }
-        }
-        now = next;
+    // a step's values are under way while its scores are made, the next one's keys while the values are added
+    Keys<N> keys;
+    Values<N> in;
+    const uint8_t* rec = nullptr;
+    if (first <= last) keys.load(rec = at(first, known), lane);
+    auto step = [&](int b, bool all) {
+        float x[2][4];
+        in.load(rec, lane);
+        rec = at(min(b + 4, last), known_next);
+        s.scores(keys, known ? s.kappa : __builtin_nanf(""), x);
+        keys.load(rec, lane);
+        if (!all) s.mask(32 * b + 4 * g, known, x, in);
+        s.raise(x);
+        s.add(x, in);
         known = known_next;
-    }
+    };
+    // (two loops: the masks as a branch in one became selects, a sixth of every step's instructions)
+    int b = first;
+    for (; b <= last && 32 * b + 32 <= all_see; b += 4) step(b, true);
+    for (; b <= last; b += 4) step(b, false);
     // the four wavefronts' sums
-    l = column_sum(l);
+    s.l = column_sum(s.l);
     if (g == 0) {
-        stats[wave][0][c] = m;
-        stats[wave][1][c] = l;
+        stats[wave][0][c] = s.m;
+        stats[wave][1][c] = s.l;
     }
     constexpr int SPAN = N == 1 ? 64 : 128;
     for (int d0 = 0; d0 < D; d0 += SPAN) {
         if (d0) __syncthreads();
 #pragma unroll
         for (int j = 0; j < 4 * N; ++j)
-            if (16 * j >= d0 && 16 * j < d0 + SPAN) *reinterpret_cast<dbf_f4*>(&sums[wave][c][16 * j - d0 + 4 * g]) = o[j];
+            if (16 * j >= d0 && 16 * j < d0 + SPAN) *reinterpret_cast<dbf_f4*>(&sums[wave][c][16 * j - d0 + 4 * g]) = s.o[j];
         __syncthreads();
         for (int e = threadIdx.x; e < cols * SPAN; e += 256) {
             const int col = e / SPAN, d = e % SPAN;
@@ -302,42 +343,50 @@ __global__ __launch_bounds__(256) void dbf_attend_few_kernel(const AttendArgs a)
     }
 }
 
-// The parts of a row, joined in their order: a workgroup to a row and head.
+// The parts of a row, joined in their order: a workgroup to a row and head.  How much of each part counts is made first, then all are read with many loads under way.
 template <typename T>
 __global__ __launch_bounds__(256) void dbf_attend_join_kernel(const AttendArgs a) {
-    __shared__ float sums[256][4], total[4];
+    __shared__ float keep[MOST_PARTS], total[8];
+    __shared__ dbf_f4 sums[256];
     const int tid = threadIdx.x, req = blockIdx.z, head = blockIdx.y, col = blockIdx.x, D = a.dim, G = a.group, per = D / 4, lanes = 256 / per;
     const Request r = request(a, req);
     if (col >= min(r.rows, a.max_q) * G) return;
     const int parts = r.ok ? (r.kv + a.chunk - 1) / a.chunk : 0, d = tid % per, turn = tid / per;
     const long long step = a.max_q * G, first = ((long long)req * a.n_kv + head) * a.parts * step + col;
-    float most = LOWEST;
-    for (int p = tid; p < parts; p += 256) most = fmaxf(most, a.part_stat[2 * (first + p * step)]);
+    float m[MOST_PARTS / 256], l[MOST_PARTS / 256], most = LOWEST, sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < MOST_PARTS / 256; ++k) {
+        const int p = tid + 256 * k;
+        const float* at = a.part_stat + 2 * (first + min(p, parts - 1) * step);
+        m[k] = p < parts ? at[0] : LOWEST;
+        l[k] = p < parts ? at[1] : 0.f;
+        most = fmaxf(most, m[k]);
+    }
     most = dbf_wave_max(most);
     if ((tid & 63) == 0) total[tid >> 6] = most;
     __syncthreads();
     most = fmaxf(fmaxf(total[0], total[1]), fmaxf(total[2], total[3]));
-    dbf_f4 y = {0.f, 0.f, 0.f, 0.f};
-    float sum = 0.f;
-    for (int p = turn; p < parts; p += lanes) {
-        const long long at = first + p * step;
-        const float keep = __builtin_amdgcn_exp2f(a.part_stat[2 * at] - most);
-        const dbf_f4 x = *reinterpret_cast<const dbf_f4*>(a.part_out + at * D + 4 * d);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] = fmaf(keep, x[i], y[i]);
-        sum = fmaf(keep, a.part_stat[2 * at + 1], sum);
+    for (int k = 0; k < MOST_PARTS / 256; ++k) {
+        const float f = __builtin_amdgcn_exp2f(m[k] - most);
+        keep[tid + 256 * k] = f;
+        sum = fmaf(f, l[k], sum);
     }
+    sum = dbf_wave_sum_f(sum);
+    if ((tid & 63) == 0) total[4 + (tid >> 6)] = sum;
     __syncthreads();
-    *reinterpret_cast<dbf_f4*>(sums[tid]) = y;
-    __shared__ float of[256];
-    of[tid] = sum;
+    sum = (total[4] + total[5]) + (total[6] + total[7]);
+    dbf_f4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int p = turn; p < parts; p += lanes) {
+        const dbf_f4 x = *reinterpret_cast<const dbf_f4*>(a.part_out + (first + p * step) * D + 4 * d);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = fmaf(keep[p], x[i], y[i]);
+    }
+    sums[tid] = y;
     __syncthreads();
     if (turn) return;
-    for (int k = 1; k < lanes; ++k) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] += sums[k * per + d][i];
-        sum += of[k * per + d];
-    }
+    for (int k = 1; k < lanes; ++k) y += sums[k * per + d];
     T* out = static_cast<T*>(a.out) + (long long)(r.row0 + col / G) * a.out_stride + (long long)(head * G + col % G) * D + 4 * d;
 #pragma unroll
     for (int i = 0; i < 4; ++i) out[i] = dbf_from_float<T>(!r.ok ? __builtin_nanf("") : sum == 0.f ? 0.f : y[i] / sum);
@@ -421,6 +470,10 @@ int check_attend(const dbf_attend* a, const dbf_cache* c) {
     return DBF_OK;
 }
 
+#ifndef CUT_WGS
+#define CUT_WGS 4096
+#define CUT_LEAST 512
+#endif
 // How a call is cut: tokens of a part, parts of the longest request, bytes of their sums.
 struct Cut {
     bool few;
@@ -436,10 +489,9 @@ Cut cut_of(const dbf_attend* a, const dbf_cache* c) {
     if (k.few && a->max_kv > 0) {
         const long long rows = (long long)a->n_seq * c->n_kv_heads;
         // parts: as many workgroups as the chip holds four times over, of 256 tokens at least
-        long long parts = (4096 + rows - 1) / rows, chunk = (a->max_kv + parts - 1) / parts;
-        chunk = (chunk + 127) / 128 * 128;
-        if (chunk < 512) chunk = 512;
-        k.chunk = (int)(chunk > INT_MAX / 2 ? INT_MAX / 2 : chunk);
+        const long long parts = std::min<long long>((CUT_WGS + rows - 1) / rows, MOST_PARTS);
+        const long long chunk = std::max<long long>((a->max_kv + parts - 1) / parts, CUT_LEAST);
+        k.chunk = (int)std::min<long long>((chunk + 127) / 128 * 128, INT_MAX / 2);
         k.parts = (int)((a->max_kv + (long long)k.chunk - 1) / k.chunk);
         if (k.parts > 1) {
             const size_t n = (size_t)rows * k.parts * (size_t)(a->max_q * G);
