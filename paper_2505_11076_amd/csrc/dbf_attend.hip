@@ -15,13 +15,20 @@ struct AttendArgs {
     const uint8_t* cache;
     int n_tokens, n_seq, n_q, n_kv, max_q, max_kv, table_stride, causal, n_pages, page_shift, dim;
     int group;             // query heads of a key head
-    int chunk, parts;      // tokens of a part of the long axis; parts of the longest request
     float scale;
-    float *part_out, *part_stat;   // of parts: sums [request][head][part][row][head_dim], maximum and sum of the row [..][2]
+    float *part_out, *part_stat;   // of a share's first and last piece: sums [share][2][row][head_dim], maximum and sum of the row's weights [..][2]
+    int* cut;                      // [share][4]: request, head and last share of the item that begins in the share and goes on in others; -1: there is none
 };
 constexpr float LOWEST = -3.0e38f;   // of a running maximum: below all scores, and its difference from one is a number
-constexpr int MOST_PARTS = 512;      // of the long axis
+constexpr int MOST_SHARES = 1024;
+#ifndef BESIDE
+#define BESIDE 8
+#define LEAST_SHARED 1024
+#endif
 constexpr int FEW = 16;              // rows (tokens times heads) of a request and key head that are few
+
+// A word that no workgroup of the launch writes, at an address that is the same for all lanes, through the scalar cache.
+__device__ __forceinline__ int scalar(const int* p) { return *(const __attribute__((address_space(4))) int*)p; }
 
 // A request's rows and tokens; ok: they are what the call allows.
 struct Request {
@@ -74,7 +81,9 @@ __device__ __forceinline__ void operands(unsigned w0, unsigned w1, dbf_h8& even,
 // pairs of tokens 0, 2 and 1, 3 of the low value and of the high one.  s and b: the pairs' scales and zeros.  (1024 + c is fp16's 1024 with c in its last bits.)
 __device__ __forceinline__ void values(unsigned u, dbf_h2 s02, dbf_h2 b02, dbf_h2 s13, dbf_h2 b13, unsigned& lo02, unsigned& lo13, unsigned& hi02, unsigned& hi13) {
     const dbf_h2 less = {(_Float16)-1024.f, (_Float16)-1024.f}, part = {(_Float16)0.0625f, (_Float16)0.0625f}, less_part = {(_Float16)-64.f, (_Float16)-64.f};
-    auto code = [](unsigned v) { return __builtin_bit_cast(dbf_h2, v | 0x64006400u); };
+    unsigned thousand = 0x64006400u;
+    asm("" : "+v"(thousand));   // (in a register, so that and-or is one instruction: it takes one scalar operand)
+    auto code = [=](unsigned v) { return __builtin_bit_cast(dbf_h2, v | thousand); };
     auto value = [](dbf_h2 c, dbf_h2 s, dbf_h2 b) { return __builtin_bit_cast(unsigned, __builtin_elementwise_fma(c, s, b)); };
     lo02 = value(code(u & 0x000F000Fu) + less, s02, b02);
     lo13 = value(code(u >> 8 & 0x000F000Fu) + less, s13, b13);
@@ -228,17 +237,17 @@ struct Columns {
 //            (nearly all) joins no lanes and touches no sums.  Rounded to fp16 for the product, times 2^7: a weight 2^-21 of the largest still has all its bits.
 //   output:  V^T p^T, 16 values of a group x 16 columns x 32 tokens, of values made exact in fp16.  (Scales on the weights instead of the values were fewer
 //            instructions, but their rounding does not cancel between c and z: values near zero lost three bits.)
+template <int N>
+struct Shared {
+    float sums[4][FEW][N == 1 ? 64 : 128], stats[4][2][FEW];
+};
+// Records from .. to of a request and key head: into the output, or, of a piece, into its place among the parts.
 template <typename T, int N>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(N == 4 ? 2 : 3))) void dbf_attend_few_kernel(const AttendArgs a) {
+__device__ __forceinline__ void few_rows(const AttendArgs& a, const Request& r, int req, int head, int from, int to, long long piece, Shared<N>& shared) {
     constexpr int D = 64 * N;
-    __shared__ float sums[4][FEW][N == 1 ? 64 : 128], stats[4][2][FEW];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
-    const int part = blockIdx.x, head = blockIdx.y, req = blockIdx.z, G = a.group;
-    const Request r = request(a, req);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, c = lane & 15, G = a.group;
     const int cols = min(r.rows, a.max_q) * G;
     if (!cols) return;
-    const int begin = part * a.chunk, end = r.ok ? min(begin + a.chunk, r.kv) : 0;
-    if (part > 0 && begin >= end) return;
     // the column's query, by groups
     Columns<N> s = {};
     {
@@ -278,10 +287,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(N == 4 ? 2 
     s.m = LOWEST;
     const int all_see = a.causal ? r.kv - r.rows + 1 : r.kv;   // tokens that all columns see
     const int* table = a.table + (long long)req * a.table_stride;
-    const int first = begin / 32 + wave, last = (end + 31) / 32 - 1, per_page = a.page_shift - 5;
+    const int first = from + wave, last = to - 1, per_page = a.page_shift - 5;
     bool known = true, known_next = true;
     auto at = [&](int b, bool& is) {
-        const int page = table[b >> per_page];
+        const int page = scalar(table + (b >> per_page));
         is = (unsigned)page < (unsigned)a.n_pages;
         return a.cache + ((((long long)(is ? page : 0) * a.n_kv + head) << per_page) + (b & ((1 << per_page) - 1))) * dbf_record_bytes(D);
     };
@@ -307,57 +316,140 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(N == 4 ? 2 
     for (; b <= last; b += 4) step(b, false);
     // the four wavefronts' sums
     s.l = column_sum(s.l);
+    __syncthreads();   // (the piece before has been read)
     if (g == 0) {
-        stats[wave][0][c] = s.m;
-        stats[wave][1][c] = s.l;
+        shared.stats[wave][0][c] = s.m;
+        shared.stats[wave][1][c] = s.l;
     }
     constexpr int SPAN = N == 1 ? 64 : 128;
     for (int d0 = 0; d0 < D; d0 += SPAN) {
         if (d0) __syncthreads();
 #pragma unroll
         for (int j = 0; j < 4 * N; ++j)
-            if (16 * j >= d0 && 16 * j < d0 + SPAN) *reinterpret_cast<dbf_f4*>(&sums[wave][c][16 * j - d0 + 4 * g]) = s.o[j];
+            if (16 * j >= d0 && 16 * j < d0 + SPAN) *reinterpret_cast<dbf_f4*>(&shared.sums[wave][c][16 * j - d0 + 4 * g]) = s.o[j];
         __syncthreads();
         for (int e = threadIdx.x; e < cols * SPAN; e += 256) {
             const int col = e / SPAN, d = e % SPAN;
-            float most = stats[0][0][col];
-            for (int w = 1; w < 4; ++w) most = fmaxf(most, stats[w][0][col]);
+            float most = shared.stats[0][0][col];
+            for (int w = 1; w < 4; ++w) most = fmaxf(most, shared.stats[w][0][col]);
             float y = 0.f, sum = 0.f;
             for (int w = 0; w < 4; ++w) {
-                const float keep = __builtin_amdgcn_exp2f(stats[w][0][col] - most);
-                y = fmaf(keep, sums[w][col][d], y);
-                sum = fmaf(keep, stats[w][1][col], sum);
+                const float keep = __builtin_amdgcn_exp2f(shared.stats[w][0][col] - most);
+                y = fmaf(keep, shared.sums[w][col][d], y);
+                sum = fmaf(keep, shared.stats[w][1][col], sum);
             }
-            if (a.parts == 1) {
+            if (piece < 0) {
                 T* out = static_cast<T*>(a.out) + (long long)(r.row0 + col / G) * a.out_stride + (long long)(head * G + col % G) * D + d0 + d;
                 *out = dbf_from_float<T>(!r.ok ? __builtin_nanf("") : sum == 0.f ? 0.f : y / sum);
             } else {
-                const long long at = (((long long)req * a.n_kv + head) * a.parts + part) * (a.max_q * G) + col;
-                a.part_out[at * D + d0 + d] = y;
+                a.part_out[(piece * FEW + col) * D + d0 + d] = y;
                 if (d0 + d == 0) {
-                    a.part_stat[2 * at] = most;
-                    a.part_stat[2 * at + 1] = sum;
+                    a.part_stat[2 * (piece * FEW + col)] = most;
+                    a.part_stat[2 * (piece * FEW + col) + 1] = sum;
                 }
             }
         }
     }
 }
+__device__ __forceinline__ int records(const Request& r) { return r.ok && r.rows > 0 ? (r.kv + 31) / 32 : 0; }
 
-// The parts of a row, joined in their order: a workgroup to a row and head.  How much of each part counts is made first, then all are read with many loads under way.
+constexpr int few_waves(int N) { return N == 1 ? 4 : N == 2 ? 3 : 2; }   // wavefronts of a SIMD that have registers
+#define DBF_FEW_KERNEL(N) __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(few_waves(N))))
+
+// A workgroup to an item: a request and key head.
+template <typename T, int N>
+DBF_FEW_KERNEL(N) void dbf_attend_items_kernel(const AttendArgs a) {
+    __shared__ Shared<N> shared;
+    const Request r = request(a, blockIdx.y);
+    few_rows<T, N>(a, r, blockIdx.y, blockIdx.x, 0, records(r), -1, shared);
+}
+
+// An equal share of the whole call to each of as many workgroups as the chip holds at once: items lie one after the other, each its records and a constant for what it
+// costs beside them, and are cut where the shares end.  Lengths are only known here, so each workgroup makes the sums over the requests itself.  (Parts of a length chosen on the host,
+// a workgroup to each: 64 requests of 1 .. 8192 tokens 103 us at the best length, in shares 83; 131071 tokens of 8 heads 39 and 37.)
+template <typename T, int N>
+DBF_FEW_KERNEL(N) void dbf_attend_shares_kernel(const AttendArgs a) {
+    __shared__ Shared<N> shared;
+    __shared__ long long waves[4], found_start;
+    __shared__ int found;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, share = blockIdx.x;
+    auto cost_of = [&](int i) { return (long long)records(request(a, i)) + BESIDE; };
+    const int run = (a.n_seq + 255) / 256, from = min(tid * run, a.n_seq), to = min(from + run, a.n_seq);
+    long long own = 0;
+    for (int i = from; i < to; ++i) own += cost_of(i);
+    long long sum = own;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const long long o = __shfl_up(sum, d);
+        if (lane >= d) sum += o;
+    }
+    if (lane == 63) waves[wave] = sum;
+    __syncthreads();
+    long long before = sum - own, total = 0;
+    for (int w = 0; w < 4; ++w) {
+        if (w < wave) before += waves[w];
+        total += waves[w];
+    }
+    before *= a.n_kv;
+    total *= a.n_kv;
+    const long long size = (total + gridDim.x - 1) / gridDim.x, lo = share * size, hi = min(lo + size, total);
+    if (tid == 0) a.cut[4 * share] = -1;
+    if (lo >= total) return;
+    if (lo >= before && lo < before + own * a.n_kv) {
+        int i = from;
+        for (long long c = cost_of(i) * a.n_kv; lo >= before + c; c = cost_of(i) * a.n_kv) {
+            before += c;
+            ++i;
+        }
+        found = i;
+        found_start = before;
+    }
+    __syncthreads();
+    int i = __builtin_amdgcn_readfirstlane(found);
+    const long long begins = found_start;
+    Request r = request(a, i);
+    int n = records(r), cost = n + BESIDE, head = __builtin_amdgcn_readfirstlane((int)((lo - begins) / cost));
+    long long item = begins + (long long)head * cost;   // where the item begins
+    while (item < hi) {
+        const int first = (int)max(lo - item - BESIDE, 0LL), last = (int)min(hi - item - BESIDE, (long long)n);
+        if (n ? last > first : item >= lo) {
+            const bool whole = first == 0 && last == n;
+            if (!whole && first == 0 && tid == 0) {   // it begins here
+                a.cut[4 * share] = i;
+                a.cut[4 * share + 1] = head;
+                a.cut[4 * share + 2] = (int)((item + cost - 1) / size);
+            }
+            few_rows<T, N>(a, r, i, head, __builtin_amdgcn_readfirstlane(first), __builtin_amdgcn_readfirstlane(last), whole ? -1 : 2LL * share + (first == 0), shared);
+        }
+        item += cost;
+        if (++head == a.n_kv) {
+            head = 0;
+            if (++i == a.n_seq) break;
+            r = request(a, i);
+            n = records(r);
+            cost = n + BESIDE;
+        }
+    }
+}
+
+// The pieces of a row of an item that was cut, joined in their order: a workgroup to a row of the item that begins in a share.  How much of each piece counts is
+// made first, then all are read with many loads under way.
 template <typename T>
 __global__ __launch_bounds__(256) void dbf_attend_join_kernel(const AttendArgs a) {
-    __shared__ float keep[MOST_PARTS], total[8];
+    __shared__ float keep[MOST_SHARES], total[8];
     __shared__ dbf_f4 sums[256];
-    const int tid = threadIdx.x, req = blockIdx.z, head = blockIdx.y, col = blockIdx.x, D = a.dim, G = a.group, per = D / 4, lanes = 256 / per;
+    const int tid = threadIdx.x, share = blockIdx.y, col = blockIdx.x, D = a.dim, G = a.group, per = D / 4, lanes = 256 / per;
+    const int req = a.cut[4 * share], head = a.cut[4 * share + 1], parts = a.cut[4 * share + 2] - share + 1;
+    if (req < 0) return;
     const Request r = request(a, req);
     if (col >= min(r.rows, a.max_q) * G) return;
-    const int parts = r.ok ? (r.kv + a.chunk - 1) / a.chunk : 0, d = tid % per, turn = tid / per;
-    const long long step = a.max_q * G, first = ((long long)req * a.n_kv + head) * a.parts * step + col;
-    float m[MOST_PARTS / 256], l[MOST_PARTS / 256], most = LOWEST, sum = 0.f;
+    const int d = tid % per, turn = tid / per;
+    auto piece = [&](int p) { return (long long)(2 * (share + p) + (p == 0)) * FEW + col; };
+    float m[MOST_SHARES / 256], l[MOST_SHARES / 256], most = LOWEST, sum = 0.f;
 #pragma unroll
-    for (int k = 0; k < MOST_PARTS / 256; ++k) {
+    for (int k = 0; k < MOST_SHARES / 256; ++k) {
         const int p = tid + 256 * k;
-        const float* at = a.part_stat + 2 * (first + min(p, parts - 1) * step);
+        const float* at = a.part_stat + 2 * piece(min(p, parts - 1));
         m[k] = p < parts ? at[0] : LOWEST;
         l[k] = p < parts ? at[1] : 0.f;
         most = fmaxf(most, m[k]);
@@ -367,7 +459,7 @@ __global__ __launch_bounds__(256) void dbf_attend_join_kernel(const AttendArgs a
     __syncthreads();
     most = fmaxf(fmaxf(total[0], total[1]), fmaxf(total[2], total[3]));
 #pragma unroll
-    for (int k = 0; k < MOST_PARTS / 256; ++k) {
+    for (int k = 0; k < MOST_SHARES / 256; ++k) {
         const float f = __builtin_amdgcn_exp2f(m[k] - most);
         keep[tid + 256 * k] = f;
         sum = fmaf(f, l[k], sum);
@@ -379,7 +471,7 @@ __global__ __launch_bounds__(256) void dbf_attend_join_kernel(const AttendArgs a
     dbf_f4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
     for (int p = turn; p < parts; p += lanes) {
-        const dbf_f4 x = *reinterpret_cast<const dbf_f4*>(a.part_out + (first + p * step) * D + 4 * d);
+        const dbf_f4 x = *reinterpret_cast<const dbf_f4*>(a.part_out + piece(p) * D + 4 * d);
 #pragma unroll
         for (int i = 0; i < 4; ++i) y[i] = fmaf(keep[p], x[i], y[i]);
     }
@@ -389,7 +481,7 @@ __global__ __launch_bounds__(256) void dbf_attend_join_kernel(const AttendArgs a
     for (int k = 1; k < lanes; ++k) y += sums[k * per + d];
     T* out = static_cast<T*>(a.out) + (long long)(r.row0 + col / G) * a.out_stride + (long long)(head * G + col % G) * D + 4 * d;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) out[i] = dbf_from_float<T>(!r.ok ? __builtin_nanf("") : sum == 0.f ? 0.f : y[i] / sum);
+    for (int i = 0; i < 4; ++i) out[i] = dbf_from_float<T>(sum == 0.f ? 0.f : y[i] / sum);
 }
 
 // A workgroup to a row and head.
@@ -470,48 +562,39 @@ int check_attend(const dbf_attend* a, const dbf_cache* c) {
     return DBF_OK;
 }
 
-#ifndef CUT_WGS
-#define CUT_WGS 4096
-#define CUT_LEAST 512
-#endif
-// How a call is cut: tokens of a part, parts of the longest request, bytes of their sums.
+// How a call is run, and what its workspace holds.
 struct Cut {
     bool few;
-    int chunk, parts;
-    size_t out_bytes, stat_bytes;
+    int shares;   // 0: a workgroup to an item
+    size_t cut_bytes, stat_bytes, out_bytes;
 };
 Cut cut_of(const dbf_attend* a, const dbf_cache* c) {
     Cut k = {};
-    const int G = a->n_q_heads / c->n_kv_heads;
-    k.few = (long long)a->max_q * G <= FEW;
-    k.chunk = INT_MAX;
-    k.parts = 1;
-    if (k.few && a->max_kv > 0) {
-        const long long rows = (long long)a->n_seq * c->n_kv_heads;
-        // parts: as many workgroups as the chip holds four times over, of 256 tokens at least
-        const long long parts = std::min<long long>((CUT_WGS + rows - 1) / rows, MOST_PARTS);
-        const long long chunk = std::max<long long>((a->max_kv + parts - 1) / parts, CUT_LEAST);
-        k.chunk = (int)std::min<long long>((chunk + 127) / 128 * 128, INT_MAX / 2);
-        k.parts = (int)((a->max_kv + (long long)k.chunk - 1) / k.chunk);
-        if (k.parts > 1) {
-            const size_t n = (size_t)rows * k.parts * (size_t)(a->max_q * G);
-            k.out_bytes = n * c->head_dim * 4;
-            k.stat_bytes = (n * 8 + 255) / 256 * 256;
-        }
+    k.few = (long long)a->max_q * (a->n_q_heads / c->n_kv_heads) <= FEW;
+    if (k.few && a->max_kv > LEAST_SHARED) {
+        k.shares = 256 * few_waves(c->head_dim / 64);
+        k.cut_bytes = (size_t)k.shares * 16;
+        k.stat_bytes = (size_t)k.shares * 2 * FEW * 8;
+        k.out_bytes = (size_t)k.shares * 2 * FEW * c->head_dim * 4;
     }
     return k;
 }
 
+template <typename T, int N>
+void launch_few(const AttendArgs& a, int shares, hipStream_t stream) {
+    if (!shares) {
+        hipLaunchKernelGGL((dbf_attend_items_kernel<T, N>), dim3(a.n_kv, a.n_seq), dim3(256), 0, stream, a);
+        return;
+    }
+    hipLaunchKernelGGL((dbf_attend_shares_kernel<T, N>), dim3(shares), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL(dbf_attend_join_kernel<T>, dim3(a.max_q * a.group, shares), dim3(256), 0, stream, a);
+}
 template <typename T>
 int launch_attend(const AttendArgs& a, const Cut& cut, hipStream_t stream) {
-    if (!cut.few) {
-        hipLaunchKernelGGL(dbf_attend_simple_kernel<T>, dim3(a.max_q, a.n_q, a.n_seq), dim3(256), 0, stream, a);
-        return hipGetLastError() == hipSuccess ? DBF_OK : DBF_EHIP;
-    }
-    const auto kernel = a.dim == 64 ? dbf_attend_few_kernel<T, 1> : a.dim == 128 ? dbf_attend_few_kernel<T, 2> : dbf_attend_few_kernel<T, 4>;
-    hipLaunchKernelGGL(kernel, dim3(a.parts, a.n_kv, a.n_seq), dim3(256), 0, stream, a);
-    if (hipGetLastError() != hipSuccess) return DBF_EHIP;
-    if (a.parts > 1) hipLaunchKernelGGL(dbf_attend_join_kernel<T>, dim3(a.max_q * a.group, a.n_kv, a.n_seq), dim3(256), 0, stream, a);
+    if (!cut.few) hipLaunchKernelGGL(dbf_attend_simple_kernel<T>, dim3(a.max_q, a.n_q, a.n_seq), dim3(256), 0, stream, a);
+    else if (a.dim == 64) launch_few<T, 1>(a, cut.shares, stream);
+    else if (a.dim == 128) launch_few<T, 2>(a, cut.shares, stream);
+    else launch_few<T, 4>(a, cut.shares, stream);
     return hipGetLastError() == hipSuccess ? DBF_OK : DBF_EHIP;
 }
 
@@ -520,7 +603,7 @@ int launch_attend(const AttendArgs& a, const Cut& cut, hipStream_t stream) {
 extern "C" size_t dbf_cache_attend_workspace_bytes(const dbf_attend* attend, const dbf_cache* cache) {
     if (check_attend(attend, cache)) return 0;
     const Cut cut = cut_of(attend, cache);
-    return cut.out_bytes + cut.stat_bytes;
+    return cut.cut_bytes + cut.stat_bytes + cut.out_bytes;
 }
 
 extern "C" int dbf_cache_attend(const dbf_attend* attend, const dbf_cache* cache, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
@@ -539,12 +622,14 @@ extern "C" int dbf_cache_attend(const dbf_attend* attend, const dbf_cache* cache
     a.max_q = attend->max_q;  a.max_kv = attend->max_kv;  a.table_stride = attend->table_stride;  a.causal = attend->causal;
     a.n_pages = cache->n_pages;  a.page_shift = dbf_page_shift(cache->page_tokens);  a.dim = cache->head_dim;  a.scale = attend->scale;
     const Cut cut = cut_of(attend, cache);
-    if (cut.out_bytes) {
-        if (!workspace_dev || dbf_misaligned(workspace_dev, 256) || workspace_bytes < cut.out_bytes + cut.stat_bytes) return DBF_EWORKSPACE;
-        a.part_stat = static_cast<float*>(workspace_dev);
-        a.part_out = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + cut.stat_bytes);
+    if (cut.shares) {
+        if (!workspace_dev || dbf_misaligned(workspace_dev, 256) || workspace_bytes < cut.cut_bytes + cut.stat_bytes + cut.out_bytes) return DBF_EWORKSPACE;
+        char* at = static_cast<char*>(workspace_dev);
+        a.cut = reinterpret_cast<int*>(at);
+        a.part_stat = reinterpret_cast<float*>(at + cut.cut_bytes);
+        a.part_out = reinterpret_cast<float*>(at + cut.cut_bytes + cut.stat_bytes);
     }
-    a.group = a.n_q / a.n_kv;  a.chunk = cut.chunk;  a.parts = cut.parts;
+    a.group = a.n_q / a.n_kv;
     const auto stream = static_cast<hipStream_t>(hip_stream);
     return attend->dtype == DBF_F16 ? launch_attend<_Float16>(a, cut, stream) : launch_attend<dbf_bf16>(a, cut, stream);
 }
