@@ -237,9 +237,23 @@ struct Columns {
 //            (nearly all) joins no lanes and touches no sums.  Rounded to fp16 for the product, times 2^7: a weight 2^-21 of the largest still has all its bits.
 //   output:  V^T p^T, 16 values of a group x 16 columns x 32 tokens, of values made exact in fp16.  (Scales on the weights instead of the values were fewer
 //            instructions, but their rounding does not cancel between c and z: values near zero lost three bits.)
+// A record from memory to LDS as it is, under way until vmcnt says that it is not.
+template <int N>
+__device__ __forceinline__ void fetch(const uint8_t* rec, uint8_t* to, int lane) {
+    constexpr int BYTES = 36 * 64 * N;
+#pragma unroll
+    for (int k = 0; k < BYTES; k += 1024)
+        if (k + 1024 <= BYTES || lane < (BYTES - k) / 16)
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(rec + k + 16 * lane), (__attribute__((address_space(3))) void*)(to + k), 16, 0, 0);
+}
+
 template <int N>
 struct Shared {
-    float sums[4][FEW][N == 1 ? 64 : 128], stats[4][2][FEW];
+    union {
+        alignas(16) uint8_t stage[4][2][36 * 64 * N];        // two records of each wavefront
+        alignas(16) float sums[4][FEW][N == 1 ? 64 : 128];   // then its sums
+    };
+    float stats[4][2][FEW];
 };
 // Records from .. to of a request and key head: into the output, or, of a piece, into its place among the parts.
 template <typename T, int N>
@@ -294,21 +308,26 @@ __device__ __forceinline__ void few_rows(const AttendArgs& a, const Request& r, 
         is = (unsigned)page < (unsigned)a.n_pages;
         return a.cache + ((((long long)(is ? page : 0) * a.n_kv + head) << per_page) + (b & ((1 << per_page) - 1))) * dbf_record_bytes(D);
     };
-    // a step's values are under way while its scores are made, the next one's keys while the values are added
-    Keys<N> keys;
-    Values<N> in;
-    const uint8_t* rec = nullptr;
-    if (first <= last) keys.load(rec = at(first, known), lane);
+    // A record is in registers while the next one is under way to LDS.  (From memory to registers, half a step ahead, took 12 loads a record, most of them of words that
+    // 16 lanes share, for 5; and 38.9 us for 131071 tokens, 74.8 for the batch of 64.)
+    uint8_t (*stage)[36 * D] = shared.stage[wave];
+    __syncthreads();   // (the piece before has been read)
+    if (first <= last) fetch<N>(at(first, known_next), stage[0], lane);
+    int turn = 0;
     auto step = [&](int b, bool all) {
         float x[2][4];
-        in.load(rec, lane);
-        rec = at(min(b + 4, last), known_next);
+        Keys<N> keys;
+        Values<N> in;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        keys.load(stage[turn], lane);
+        in.load(stage[turn], lane);
+        known = known_next;
+        turn ^= 1;
+        if (b + 4 <= last) fetch<N>(at(b + 4, known_next), stage[turn], lane);   // (what was there has been used)
         s.scores(keys, known ? s.kappa : __builtin_nanf(""), x);
-        keys.load(rec, lane);
         if (!all) s.mask(32 * b + 4 * g, known, x, in);
         s.raise(x);
         s.add(x, in);
-        known = known_next;
     };
     // (two loops: the masks as a branch in one became selects, a sixth of every step's instructions)
     int b = first;
@@ -316,7 +335,7 @@ __device__ __forceinline__ void few_rows(const AttendArgs& a, const Request& r, 
     for (; b <= last; b += 4) step(b, false);
     // the four wavefronts' sums
     s.l = column_sum(s.l);
-    __syncthreads();   // (the piece before has been read)
+    __syncthreads();   // (no record is needed any more)
     if (g == 0) {
         shared.stats[wave][0][c] = s.m;
         shared.stats[wave][1][c] = s.l;
