@@ -237,14 +237,14 @@ struct Columns {
 //            (nearly all) joins no lanes and touches no sums.  Rounded to fp16 for the product, times 2^7: a weight 2^-21 of the largest still has all its bits.
 //   output:  V^T p^T, 16 values of a group x 16 columns x 32 tokens, of values made exact in fp16.  (Scales on the weights instead of the values were fewer
 //            instructions, but their rounding does not cancel between c and z: values near zero lost three bits.)
-// A record from memory to LDS as it is, under way until vmcnt says that it is not.
+// A record from memory to LDS as it is, under way until vmcnt says that it is not.  (2: read once, so it need not stay in the caches: 75 -> 68 us for the batch of 64.)
 template <int N>
 __device__ __forceinline__ void fetch(const uint8_t* rec, uint8_t* to, int lane) {
     constexpr int BYTES = 36 * 64 * N;
 #pragma unroll
     for (int k = 0; k < BYTES; k += 1024)
         if (k + 1024 <= BYTES || lane < (BYTES - k) / 16)
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(rec + k + 16 * lane), (__attribute__((address_space(3))) void*)(to + k), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(rec + k + 16 * lane), (__attribute__((address_space(3))) void*)(to + k), 16, 0, 2);
 }
 
 template <int N>
@@ -262,6 +262,20 @@ __device__ __forceinline__ void few_rows(const AttendArgs& a, const Request& r, 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, c = lane & 15, G = a.group;
     const int cols = min(r.rows, a.max_q) * G;
     if (!cols) return;
+    const int all_see = a.causal ? r.kv - r.rows + 1 : r.kv;   // tokens that all columns see
+    const int* table = a.table + (long long)req * a.table_stride;
+    const int first = from + wave, last = to - 1, per_page = a.page_shift - 5;
+    bool known = true, known_next = true;
+    auto at = [&](int b, bool& is) {
+        const int page = scalar(table + (b >> per_page));
+        is = (unsigned)page < (unsigned)a.n_pages;
+        return a.cache + ((((long long)(is ? page : 0) * a.n_kv + head) << per_page) + (b & ((1 << per_page) - 1))) * dbf_record_bytes(D);
+    };
+    // A record is in registers while the next one is under way to LDS.  (From memory to registers, half a step ahead, took 12 loads a record, most of them of words that
+    // 16 lanes share, for 5; and 38.9 us for 131071 tokens, 74.8 for the batch of 64.)
+    uint8_t (*stage)[36 * D] = shared.stage[wave];
+    __syncthreads();   // (the piece before has been read)
+    if (first <= last) fetch<N>(at(first, known_next), stage[0], lane);
     // the column's query, by groups
     Columns<N> s = {};
     {
@@ -299,20 +313,6 @@ __device__ __forceinline__ void few_rows(const AttendArgs& a, const Request& r, 
     s.seen = a.causal ? r.kv - r.rows + c / G + 1 : r.kv;
     s.kv = r.kv;
     s.m = LOWEST;
-    const int all_see = a.causal ? r.kv - r.rows + 1 : r.kv;   // tokens that all columns see
-    const int* table = a.table + (long long)req * a.table_stride;
-    const int first = from + wave, last = to - 1, per_page = a.page_shift - 5;
-    bool known = true, known_next = true;
-    auto at = [&](int b, bool& is) {
-        const int page = scalar(table + (b >> per_page));
-        is = (unsigned)page < (unsigned)a.n_pages;
-        return a.cache + ((((long long)(is ? page : 0) * a.n_kv + head) << per_page) + (b & ((1 << per_page) - 1))) * dbf_record_bytes(D);
-    };
-    // A record is in registers while the next one is under way to LDS.  (From memory to registers, half a step ahead, took 12 loads a record, most of them of words that
-    // 16 lanes share, for 5; and 38.9 us for 131071 tokens, 74.8 for the batch of 64.)
-    uint8_t (*stage)[36 * D] = shared.stage[wave];
-    __syncthreads();   // (the piece before has been read)
-    if (first <= last) fetch<N>(at(first, known_next), stage[0], lane);
     int turn = 0;
     auto step = [&](int b, bool all) {
         float x[2][4];
