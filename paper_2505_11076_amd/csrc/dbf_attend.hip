@@ -15,8 +15,10 @@ struct AttendArgs {
     const uint8_t* cache;
     int n_tokens, n_seq, n_q, n_kv, max_q, max_kv, table_stride, causal, n_pages, page_shift, dim;
     int group;             // query heads of a key head
+    int chunk, parts;      // many rows: tokens of a part of the long axis, and parts
     float scale;
     float *part_out, *part_stat;   // of a share's first and last piece: sums [share][2][row][head_dim], maximum and sum of the row's weights [..][2]
+                                   // (many rows: [request][head][part][row])
     int* cut;                      // [share][4]: request, head and last share of the item that begins in the share and goes on in others; -1: there is none
 };
 constexpr float LOWEST = -3.0e38f;   // of a running maximum: below all scores, and its difference from one is a number
@@ -25,6 +27,11 @@ constexpr int MOST_SHARES = 1024;
 #define BESIDE 8
 #define LEAST_SHARED 1024
 #endif
+constexpr int TILE = 64;             // tokens of a step of many rows
+#ifndef MANY_WAVES
+#define MANY_WAVES 4
+#endif
+constexpr int LEAST_CHUNK = 512;
 constexpr int FEW = 16;              // rows (tokens times heads) of a request and key head that are few
 
 // A word that no workgroup of the launch writes, at an address that is the same for all lanes, through the scalar cache.
@@ -503,71 +510,289 @@ __global__ __launch_bounds__(256) void dbf_attend_join_kernel(const AttendArgs a
     for (int i = 0; i < 4; ++i) out[i] = dbf_from_float<T>(sum == 0.f ? 0.f : y[i] / sum);
 }
 
-// A workgroup to a row and head.
-template <typename T>
-__global__ __launch_bounds__(256) void dbf_attend_simple_kernel(const AttendArgs a) {
-    __shared__ float q[256], p[256], part[4];
-    const int tid = threadIdx.x, head = blockIdx.y, D = a.dim, n = D / 64;
-    const Request r = request(a, blockIdx.z);
-    const int t = blockIdx.x;
-    if (t >= r.rows) return;
-    T* out = static_cast<T*>(a.out) + (long long)(r.row0 + t) * a.out_stride + (long long)head * D;
+// Many rows.  A workgroup takes 32 rows of a request and key head (tokens times the heads that share the keys) to each of its WAVES wavefronts, and walks the tokens in tiles
+// of 64: codes from memory to registers while the tile before is worked on, from there as exact fp16 values to LDS, once for all rows.
+//   scores:  K q^T, 32 tokens x 32 columns a product; a lane has 32 of a column's 64, the lane 32 on has the others.
+//   output:  V^T p^T, 32 values x 32 columns: the scores' places are the product's operand as they are, since the values' tokens are laid out in that order.
+// Both operands lie in LDS as the lanes take them, 16 bytes a lane one after the other.
+
+template <int N, int WAVES>
+struct Tiles {
+    dbf_u4 k[2][2][4 * N][64], v[2][2 * N][4][64];   // [which][record][16 values][lane], [which][32 values][16 tokens][lane]
+};
+
+// A thread's share of a tile's bytes.  Keys: of token tid % 64, PIECES runs of 16 values; values: of a record, group and half of it, 16 places by 8 tokens.
+template <int N, int WAVES>
+struct Share {
+    static constexpr int RUNS = 4 * N / WAVES > 0 ? 4 * N / WAVES : 1, UNITS = 2 * N / WAVES > 0 ? 2 * N / WAVES : 1;
+    static constexpr bool ALL_KEYS = 4 * N >= WAVES, ALL_VALUES = 2 * N >= WAVES;   // whether all wavefronts have some
+    dbf_u2 k[RUNS], v[UNITS][2];
+    unsigned kw[RUNS];
+    dbf_u4 vw[UNITS][2][2];
+
+    __device__ __forceinline__ void load(const uint8_t* rec0, const uint8_t* rec1, int lane, int wave) {
+        const int token = lane & 31;
+        const uint8_t* rec = lane < 32 ? rec0 : rec1;
+        if (ALL_KEYS || wave < 4 * N) {
+#pragma unroll
+            for (int e = 0; e < RUNS; ++e) {
+                const int run = wave * RUNS + e;
+                k[e] = *reinterpret_cast<const dbf_u2*>(rec + token * 32 * N + 8 * run);
+                kw[e] = *reinterpret_cast<const unsigned*>(rec + 2048 * N + 128 * (run % N) + 4 * token);
+            }
+        }
+        // lanes: place l, half of the four tokens' g, pair of runs q; wavefronts: record, then groups
+        const int l = lane & 15, hf = lane >> 4 & 1, q = lane >> 5;
+        const uint8_t* of = wave & 1 ? rec1 : rec0;
+        if (ALL_VALUES || wave < 2 * N) {
+#pragma unroll
+            for (int e = 0; e < UNITS; ++e) {
+                const int p = (wave >> 1) * UNITS + e;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int g = hf + 2 * h;
+                    v[e][h] = *reinterpret_cast<const dbf_u2*>(of + 1024 * N + 1024 * p + 16 * (16 * g + l) + 8 * q);
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) vw[e][h][t] = *reinterpret_cast<const dbf_u4*>(of + 2176 * N + 128 * p + 64 * t + 16 * g);
+                }
+            }
+        }
+    }
+    // Tokens that are not there (from `there` on, counted from the tile's first) and pages that are not: no values, and keys that are no numbers where the page is missing.
+    __device__ __forceinline__ void blank(int there, bool known0, bool known1, int lane, int wave) {
+        if (!(lane < 32 ? known0 : known1))
+#pragma unroll
+            for (int e = 0; e < RUNS; ++e) kw[e] = 0x7E007E00u;
+        const bool known = wave & 1 ? known1 : known0;
+        const int hf = lane >> 4 & 1;
+#pragma unroll
+        for (int e = 0; e < UNITS; ++e)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (!known || 32 * (wave & 1) + 16 * t + 4 * (hf + 2 * h) + i >= there) vw[e][h][t][i] = 0;
+    }
+    __device__ __forceinline__ void store(Tiles<N, WAVES>& tiles, int which, int lane, int wave) const {
+        if (ALL_KEYS || wave < 4 * N) {
+#pragma unroll
+            for (int e = 0; e < RUNS; ++e) {
+                const dbf_h2 s = lows(kw[e], kw[e]), b = highs(kw[e], kw[e]);
+#pragma unroll
+                for (int hf = 0; hf < 2; ++hf) {
+                    unsigned x[4];
+                    values(k[e][hf], s, b, s, b, x[0], x[1], x[2], x[3]);
+                    tiles.k[which][lane >> 5][wave * RUNS + e][(lane & 31) + 32 * hf] = (dbf_u4){x[0], x[1], x[2], x[3]};
+                }
+            }
+        }
+        const int l = lane & 15, hf = lane >> 4 & 1, q = lane >> 5;
+        if (ALL_VALUES || wave < 2 * N) {
+#pragma unroll
+            for (int e = 0; e < UNITS; ++e) {
+                const int p = (wave >> 1) * UNITS + e;
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    unsigned lo[4], hi[4];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const dbf_u4 w = vw[e][h][t];
+                        values(v[e][h][t], lows(w[0], w[2]), highs(w[0], w[2]), lows(w[1], w[3]), highs(w[1], w[3]), lo[2 * h], lo[2 * h + 1], hi[2 * h], hi[2 * h + 1]);
+                    }
+                    const int low = p + N * 2 * q, high = low + N, m = 2 * (wave & 1) + t;
+                    tiles.v[which][low >> 1][m][16 * (low & 1) + l + 32 * hf] = (dbf_u4){lo[0], lo[1], lo[2], lo[3]};
+                    tiles.v[which][high >> 1][m][16 * (high & 1) + l + 32 * hf] = (dbf_u4){hi[0], hi[1], hi[2], hi[3]};
+                }
+            }
+        }
+    }
+};
+
+__device__ __forceinline__ float both_max(float v) {   // of a lane and the one 32 on
+    const unsigned b = __builtin_bit_cast(unsigned, v);
+    const auto r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+    return fmaxf(__builtin_bit_cast(float, (unsigned)r[0]), __builtin_bit_cast(float, (unsigned)r[1]));
+}
+__device__ __forceinline__ float both_sum(float v) {
+    const unsigned b = __builtin_bit_cast(unsigned, v);
+    const auto r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+    return __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+}
+
+template <typename T, int N, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(N == 4 ? 1 : 2))) void dbf_attend_many_kernel(const AttendArgs a) {
+    constexpr int D = 64 * N;
+    __shared__ Tiles<N, WAVES> tiles;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hf = lane >> 5, G = a.group;
+    // (a request's later rows see more: they come first)
+    const int head = blockIdx.x % a.n_kv, part = blockIdx.x / a.n_kv, req = blockIdx.y, block = gridDim.z - 1 - blockIdx.z;
+    const Request r = request(a, req);
+    const int rows = min(r.rows, a.max_q) * G, row0 = block * 32 * WAVES;
+    if (row0 >= rows) return;
+    const int row = row0 + 32 * wave + (lane & 31), t = row / G;   // the column's row, of the request's token t
+    const bool live = row < rows;
+    T* out = static_cast<T*>(a.out) + (long long)(r.row0 + (live ? t : 0)) * a.out_stride + (long long)(head * G + (live ? row % G : 0)) * D;
     if (!r.ok) {
-        if (tid < D) out[tid] = dbf_from_float<T>(__builtin_nanf(""));
+        if (live && part == 0)
+            for (int d = 4 * hf; d < D; d += 8)
+                for (int i = 0; i < 4; ++i) out[d + i] = dbf_from_float<T>(__builtin_nanf(""));
         return;
     }
-    if (tid < D) q[tid] = dbf_to_float((static_cast<const T*>(a.q) + (long long)(r.row0 + t) * a.q_stride + (long long)head * D)[tid]) * a.scale;
-    const int kv_head = head / (a.n_q / a.n_kv), seen = a.causal ? min(r.kv, r.kv - r.rows + t + 1) : r.kv;
-    const int* table = a.table + (long long)blockIdx.z * a.table_stride;
-    float m = -__builtin_inff(), l = 0.f, o = 0.f;
-    auto record = [&](int j, bool& known) {
-        const int page = table[j >> a.page_shift];
-        known = page >= 0 && page < a.n_pages;
-        const long long slot = ((long long)(known ? page : 0) << a.page_shift) + (j & ((1 << a.page_shift) - 1));
-        return a.cache + dbf_record_at((int)slot, kv_head, a.n_kv, a.page_shift, D);
+    // tokens of the workgroup's part that some of its rows see; those that all rows and those that some rows of the wavefront see
+    const int last_t = min(row0 + 32 * WAVES, rows) - 1;
+    const int begin = part * a.chunk, end = min(a.causal ? r.kv - r.rows + last_t / G + 1 : r.kv, a.parts > 1 ? min(begin + a.chunk, r.kv) : r.kv);
+    const int seen = !live ? 0 : a.causal ? r.kv - r.rows + t + 1 : r.kv;
+    const int wave_all = a.causal ? r.kv - r.rows + (row0 + 32 * wave) / G + 1 : r.kv;
+    const int wave_some = row0 + 32 * wave >= rows ? 0 : a.causal ? r.kv - r.rows + (min(row0 + 32 * wave + 32, rows) - 1) / G + 1 : r.kv;
+    const int* table = a.table + (long long)req * a.table_stride;
+    const int per_page = a.page_shift - 5, last = (end + 31) / 32 - 1;
+    bool known0 = true, known1 = true;
+    auto at = [&](int b, bool& is) {
+        b = min(b, last);
+        const int page = scalar(table + (b >> per_page));
+        is = (unsigned)page < (unsigned)a.n_pages;
+        return a.cache + ((((long long)(is ? page : 0) * a.n_kv + head) << per_page) + (b & ((1 << per_page) - 1))) * dbf_record_bytes(D);
     };
-    for (int j0 = 0; j0 < seen; j0 += 256) {
-        __syncthreads();
-        const int j = j0 + tid;
-        float x = -__builtin_inff();
-        if (j < seen) {
-            bool known;
-            const uint8_t* rec = record(j, known);
-            x = known ? 0.f : __builtin_nanf("");
-            const dbf_h2* w = reinterpret_cast<const dbf_h2*>(rec + 32 * D) + (j & 31);
-            for (int d = 0; d < D; ++d) {
-                const dbf_h2 sb = w[32 * ((d >> 4) % n)];
-                const unsigned c = rec[(j & 31) * (D / 2) + (d >> 1)] >> 4 * (d & 1) & 15;
-                x = fmaf(q[d], fmaf((float)sb[0], (float)c, (float)sb[1]), x);
-            }
+    Share<N, WAVES> share;
+    auto load = [&](int first) {
+        const uint8_t* rec0 = at(first / 32, known0);
+        const uint8_t* rec1 = at(first / 32 + 1, known1);
+        share.load(rec0, rec1, lane, wave);
+    };
+    auto store = [&](int first, int which) {
+        if (first + TILE > r.kv || !known0 || !known1) {
+            asm volatile("");
+            share.blank(r.kv - first, known0, known1, lane, wave);
         }
-        float top = dbf_wave_max(x != x ? 0.f : x);
-        if ((tid & 63) == 0) part[tid >> 6] = top;
-        __syncthreads();
-        top = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
-        const float now = fmaxf(m, top), keep = m == now ? 1.f : expf(m - now);
-        const float e = x == -__builtin_inff() ? 0.f : expf(x - now);
-        p[tid] = e;
-        __syncthreads();
-        const float sum = dbf_wave_sum_f(e);
-        if ((tid & 63) == 0) part[tid >> 6] = sum;
-        __syncthreads();
-        l = l * keep + ((part[0] + part[1]) + (part[2] + part[3]));
-        o *= keep;
-        m = now;
-        if (tid < D) {
-            const int run = tid >> 4, g = run % n, k = run / n;
-            for (int i = 0; i < min(256, seen - j0); ++i) {
-                bool known;
-                const uint8_t* rec = record(j0 + i, known);
-                const int u = (j0 + i) & 31;
-                const dbf_h2 sb = reinterpret_cast<const dbf_h2*>(rec + 34 * D)[32 * g + u];
-                const unsigned c = rec[16 * D + 1024 * g + 16 * (16 * (u >> 2 & 3) + (tid & 15)) + 4 * (2 * (k >> 1) + (u >> 4)) + (u & 3)] >> 4 * (k & 1) & 15;
-                o = fmaf(p[i], known ? fmaf((float)sb[0], (float)c, (float)sb[1]) : 0.f, o);
+        share.store(tiles, which, lane, wave);
+    };
+    if (begin < end) load(begin);
+    // the column's query: of each 16 values the lane's 8, in the order of a word's codes
+    dbf_h8 q[4 * N];
+    float kappa;
+    {
+        const T* x = static_cast<const T*>(a.q) + (long long)(r.row0 + (live ? t : 0)) * a.q_stride + (long long)(head * G + (live ? row % G : 0)) * D + 8 * hf;
+        float most = 0.f;
+        for (int k = 0; k < 4 * N; ++k) {
+            float v[8];
+            load8(x + 16 * k, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) most = fmaxf(most, live ? fabsf(v[e]) : 0.f);
+        }
+        most = both_max(most);
+        const int up = most > 0.f && most < __builtin_inff() ? 15 - __builtin_amdgcn_frexp_expf(most) : 0;
+        kappa = fmaxf(ldexpf(fabsf(a.scale) * 1.44269504089f, -up), 0x1p-126f);   // (not 0: what is masked is -infinity times it)
+#pragma unroll
+        for (int k = 0; k < 4 * N; ++k) {
+            float v[8];
+            load8(x + 16 * k, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float y = live ? ldexpf(v[4 * (e & 1) + (e & 2) + (e >> 2)], up) : 0.f;
+                q[k][e] = (_Float16)(a.scale < 0.f ? -y : y);
             }
         }
     }
-    if (tid < D) out[tid] = dbf_from_float<T>(l == 0.f ? 0.f : o / l);
+    dbf_f16 o[2 * N] = {};
+    float m = LOWEST, l = 0.f;
+    if (begin < end) store(begin, 0);
+    int which = 0;
+    for (int first = begin; first < end; first += TILE, which ^= 1) {
+        __syncthreads();
+        const bool more = first + TILE < end;
+        if (more) load(first + TILE);
+        if (first < wave_some) {
+            dbf_f16 x[2] = {};
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int k = 0; k < 4 * N; ++k)
+                    x[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(dbf_h8, tiles.k[which][b][k][lane]), q[k], x[b], 0, 0, 0);
+            if (first + TILE > wave_all) {
+                asm volatile("");
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[b][i] = first + 32 * b + 8 * (i >> 2) + 4 * hf + (i & 3) < seen ? x[b][i] : -__builtin_inff();
+            }
+            float most = x[0][0];
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) most = fmaxf(most, x[b][i]);
+            most *= kappa;
+            if (__any(most > m + 8.f)) {
+                const float to = fmaxf(m, both_max(most)), keep = __builtin_amdgcn_exp2f(m - to);
+                m = to;
+                l *= keep;
+#pragma unroll
+                for (int j = 0; j < 2 * N; ++j) o[j] *= keep;
+            }
+            const float from = 7.f - m;
+            dbf_h8 weights[4];
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float w = __builtin_amdgcn_exp2f(fmaf(x[b][i], kappa, from));
+                    l += w;
+                    weights[2 * b + (i >> 3)][(i & 4) + 2 * (i & 1) + (i >> 1 & 1)] = (_Float16)w;
+                }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int j = 0; j < 2 * N; ++j)
+                    o[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(dbf_h8, tiles.v[which][j][k][lane]), weights[k], o[j], 0, 0, 0);
+        }
+        if (more) store(first + TILE, which ^ 1);
+    }
+    l = both_sum(l);
+    if (!live) return;
+    if (a.parts == 1) {
+        const float by = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+        for (int j = 0; j < 2 * N; ++j)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) out[32 * j + 8 * (i >> 2) + 4 * hf + (i & 3)] = dbf_from_float<T>(o[j][i] * by);
+        return;
+    }
+    const long long piece = (((long long)req * a.n_kv + head) * a.parts + part) * (a.max_q * G) + row;
+    if (hf == 0) {
+        a.part_stat[2 * piece] = m;
+        a.part_stat[2 * piece + 1] = l;
+    }
+#pragma unroll
+    for (int j = 0; j < 2 * N; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            *reinterpret_cast<dbf_f4*>(a.part_out + piece * D + 32 * j + 8 * k + 4 * hf) = (dbf_f4){o[j][4 * k], o[j][4 * k + 1], o[j][4 * k + 2], o[j][4 * k + 3]};
+}
+
+// The parts of the rows of such a call: head_dim / 4 lanes to a row.
+template <typename T>
+__global__ __launch_bounds__(256) void dbf_attend_parts_kernel(const AttendArgs a) {
+    const int D = a.dim, per = D / 4, G = a.group, head = blockIdx.y, req = blockIdx.z, row = blockIdx.x * (256 / per) + threadIdx.x / per, d = 4 * (threadIdx.x % per);
+    const Request r = request(a, req);
+    if (row >= min(r.rows, a.max_q) * G || !r.ok) return;
+    const long long step = (long long)a.max_q * G, first = ((long long)req * a.n_kv + head) * a.parts * step + row;
+    const int parts = min(a.parts, (r.kv + a.chunk - 1) / a.chunk);   // (those behind have no token of the request)
+    float m = LOWEST, l = 0.f;
+    dbf_f4 y = {0.f, 0.f, 0.f, 0.f};
+    for (int p = 0; p < parts; ++p) m = fmaxf(m, a.part_stat[2 * (first + p * step)]);
+#pragma unroll 4
+    for (int p = 0; p < parts; ++p) {
+        const long long at = first + p * step;
+        const float keep = __builtin_amdgcn_exp2f(a.part_stat[2 * at] - m);
+        l = fmaf(keep, a.part_stat[2 * at + 1], l);
+        const dbf_f4 x = *reinterpret_cast<const dbf_f4*>(a.part_out + at * D + d);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = fmaf(keep, x[i], y[i]);
+    }
+    T* out = static_cast<T*>(a.out) + (long long)(r.row0 + row / G) * a.out_stride + (long long)(head * G + row % G) * D + d;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[i] = dbf_from_float<T>(l == 0.f ? 0.f : y[i] / l);
 }
 
 int check_attend(const dbf_attend* a, const dbf_cache* c) {
@@ -584,7 +809,8 @@ int check_attend(const dbf_attend* a, const dbf_cache* c) {
 // How a call is run, and what its workspace holds.
 struct Cut {
     bool few;
-    int shares;   // 0: a workgroup to an item
+    int shares;         // few rows; 0: a workgroup to an item
+    int chunk, parts;   // many rows
     size_t cut_bytes, stat_bytes, out_bytes;
 };
 Cut cut_of(const dbf_attend* a, const dbf_cache* c) {
@@ -595,6 +821,22 @@ Cut cut_of(const dbf_attend* a, const dbf_cache* c) {
         k.cut_bytes = (size_t)k.shares * 16;
         k.stat_bytes = (size_t)k.shares * 2 * FEW * 8;
         k.out_bytes = (size_t)k.shares * 2 * FEW * c->head_dim * 4;
+    }
+    k.chunk = INT_MAX;
+    k.parts = 1;
+    if (!k.few && a->max_q > 0) {
+        // The long axis in parts where the rows alone are few workgroups, of LEAST_CHUNK tokens at least
+        const long long rows = (long long)a->max_q * (a->n_q_heads / c->n_kv_heads), groups = (rows + 32 * MANY_WAVES - 1) / (32 * MANY_WAVES) * c->n_kv_heads * a->n_seq;
+        const long long parts = std::min<long long>((512 + groups - 1) / groups, (a->max_kv + LEAST_CHUNK - 1) / LEAST_CHUNK);
+        if (parts > 1) {
+            k.chunk = (int)(((a->max_kv + parts - 1) / parts + TILE - 1) / TILE * TILE);
+            k.parts = (a->max_kv + k.chunk - 1) / k.chunk;
+        }
+        if (k.parts > 1) {
+            const size_t n = (size_t)rows * c->n_kv_heads * a->n_seq * k.parts;
+            k.stat_bytes = (n * 8 + 255) / 256 * 256;
+            k.out_bytes = n * c->head_dim * 4;
+        }
     }
     return k;
 }
@@ -609,9 +851,20 @@ void launch_few(const AttendArgs& a, int shares, hipStream_t stream) {
     hipLaunchKernelGGL(dbf_attend_join_kernel<T>, dim3(a.max_q * a.group, shares), dim3(256), 0, stream, a);
 }
 template <typename T>
+bool launch_many(const AttendArgs& a, hipStream_t stream) {
+    const long long rows = (long long)a.max_q * a.group, blocks = (rows + 32 * MANY_WAVES - 1) / (32 * MANY_WAVES), across = (long long)a.n_kv * a.parts;
+    if (blocks > 65535 || across > INT_MAX || rows > INT_MAX) return false;
+    const auto kernel = a.dim == 64 ? dbf_attend_many_kernel<T, 1, MANY_WAVES> : a.dim == 128 ? dbf_attend_many_kernel<T, 2, MANY_WAVES> : dbf_attend_many_kernel<T, 4, MANY_WAVES>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)across, a.n_seq, (unsigned)blocks), dim3(64 * MANY_WAVES), 0, stream, a);
+    const int of = 256 / (a.dim / 4);
+    if (a.parts > 1) hipLaunchKernelGGL(dbf_attend_parts_kernel<T>, dim3((unsigned)((rows + of - 1) / of), a.n_kv, a.n_seq), dim3(256), 0, stream, a);
+    return true;
+}
+template <typename T>
 int launch_attend(const AttendArgs& a, const Cut& cut, hipStream_t stream) {
-    if (!cut.few) hipLaunchKernelGGL(dbf_attend_simple_kernel<T>, dim3(a.max_q, a.n_q, a.n_seq), dim3(256), 0, stream, a);
-    else if (a.dim == 64) launch_few<T, 1>(a, cut.shares, stream);
+    if (!cut.few) {
+        if (!launch_many<T>(a, stream)) return DBF_EINVAL;
+    } else if (a.dim == 64) launch_few<T, 1>(a, cut.shares, stream);
     else if (a.dim == 128) launch_few<T, 2>(a, cut.shares, stream);
     else launch_few<T, 4>(a, cut.shares, stream);
     return hipGetLastError() == hipSuccess ? DBF_OK : DBF_EHIP;
@@ -641,14 +894,14 @@ extern "C" int dbf_cache_attend(const dbf_attend* attend, const dbf_cache* cache
     a.max_q = attend->max_q;  a.max_kv = attend->max_kv;  a.table_stride = attend->table_stride;  a.causal = attend->causal;
     a.n_pages = cache->n_pages;  a.page_shift = dbf_page_shift(cache->page_tokens);  a.dim = cache->head_dim;  a.scale = attend->scale;
     const Cut cut = cut_of(attend, cache);
-    if (cut.shares) {
+    if (cut.out_bytes) {
         if (!workspace_dev || dbf_misaligned(workspace_dev, 256) || workspace_bytes < cut.cut_bytes + cut.stat_bytes + cut.out_bytes) return DBF_EWORKSPACE;
         char* at = static_cast<char*>(workspace_dev);
         a.cut = reinterpret_cast<int*>(at);
         a.part_stat = reinterpret_cast<float*>(at + cut.cut_bytes);
         a.part_out = reinterpret_cast<float*>(at + cut.cut_bytes + cut.stat_bytes);
     }
-    a.group = a.n_q / a.n_kv;
+    a.group = a.n_q / a.n_kv;  a.chunk = cut.chunk;  a.parts = cut.parts;
     const auto stream = static_cast<hipStream_t>(hip_stream);
     return attend->dtype == DBF_F16 ? launch_attend<_Float16>(a, cut, stream) : launch_attend<dbf_bf16>(a, cut, stream);
 }

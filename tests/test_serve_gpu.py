@@ -412,6 +412,17 @@ def test_cache_attend_sizes_of_queries(dtype, size, q_len):
     check_attend(out, q, k, v, q_len, 64, dtype, float(np.float32(0.3 / size)), 1, "queries of %g" % size)
 
 
+@pytest.mark.parametrize("scale", [0.0, -0.2])
+@pytest.mark.parametrize("q_len", [[1, 1], [60, 30]])
+def test_cache_attend_other_scales(scale, q_len):
+    rng = np.random.default_rng(19)
+    kv = [500, 30]
+    data, pages, table, k, v = make_cache(rng, kv, 32, 2, 64)
+    q = torch.from_numpy(rng.normal(size=(sum(q_len), 4, 64))).cuda().half()
+    out = run_attend(data, pages, table, kv, q_len, q, 32, 2, 64, "f16", scale, 1)
+    check_attend(out, q, k, v, q_len, 64, "f16", float(np.float32(scale)), 1, "scale %g" % scale)
+
+
 def test_cache_attend_lone_peak_and_equal_scores():
     """One token with all the weight, at each place of a record; and keys that are all alike (the mean of the values)."""
     rng = np.random.default_rng(13)
