@@ -2,8 +2,9 @@
 //
 // One read of the logits, with a maximum m that may lag and the sums s = sum e^(x - m), t = sum e^(x - m) (x - m) of what has been read, in fp32:
 //     log sum e^x = m + log s,      entropy = log s - t / s.
-// The likeliest tokens: all values have keys (value, then the lower index) that differ.  A thread keeps its largest; the n-th largest of these is a bound that the n largest of all
-// are not below, and only the n threads whose largest keys are not below it can hold any: their values are read once more (from the cache), the few that pass are put in order.
+// The likeliest tokens: all values have keys (value, then the lower index) that differ.  A thread keeps its largest, four threads theirs; the n-th largest of these 64 is a
+// bound that the n largest of all are not below, and only threads whose largest key is not below it can hold any: their values are read once more (from the cache), the
+// few that pass are put in order.
 // A row is one workgroup's, or where rows are few the slices of several, whose sums and lists a second launch joins.
 // Bound by the read where rows are many: a value costs about nine issue slots (its exponential four), half of what the memory takes.
 #include <algorithm>
@@ -57,16 +58,18 @@ __device__ __forceinline__ Sums join(Sums a, Sums b) {
     r.t = fmaf(a.s, da, a.t) * ea + fmaf(b.s, db, b.t) * eb;
     return r;
 }
+__device__ __forceinline__ float log_of(float s) { return s > 0.f ? __builtin_amdgcn_logf(s) * 0.693147181f : __builtin_nanf(""); }
 __device__ __forceinline__ Sums wave_join(Sums v) {
-#pragma unroll
-    for (int d = 32; d; d /= 2) {
-        const Sums o = {__shfl_xor(v.m, d), __shfl_xor(v.s, d), __shfl_xor(v.t, d)};
-        v = join(v, o);
-    }
-    return v;
+    Sums r;
+    r.m = dbf_wave_max(v.m);
+    const float d = below(v.m - r.m), e = __builtin_amdgcn_exp2f(d * 1.44269504089f);
+    r.s = dbf_wave_sum_f(v.s * e);
+    r.t = dbf_wave_sum_f(fmaf(v.s, d, v.t) * e);
+    return r;
 }
 
-// Values i .. i + 7 of a row of n, whose end a run may overlap: what is not there is -infinity.  The loads have no use of their own, so several may be under way.
+// Values i .. i + 7 of n values that end a row, or a slice of one, of RUN at least: a run that overlaps the end is read as the last eight (also of the slice before), and
+// what is not there is -infinity.  The loads have no use of their own, so several may be under way.
 template <typename T>
 struct Run {
     dbf_u4 w[sizeof(T) / 2];
@@ -87,9 +90,34 @@ struct Run {
             for (int e = 0; e < RUN; ++e) v[e] = e < skip ? -__builtin_inff() : v[e];
         }
     }
-    // the index of value e
-    static __device__ __forceinline__ int index(int i, int n, int e) { return min(i, n - RUN) + e; }
 };
+// The keys of run i of x[0 .. n) to out; base: the index of x[0].
+template <typename T, typename Out>
+__device__ __forceinline__ void keys_of_run(const T* x, int i, int n, int base, Out out) {
+    Run<T> run;
+    run.load(x, i, n);
+    float v[RUN];
+    run.get(i, n, v);
+    const int at = min(i, n - RUN);
+#pragma unroll
+    for (int e = 0; e < RUN; ++e)
+        if (at + e >= i) out(key_of(v[e], base + at + e));
+}
+// The n-th largest of 64 keys in LDS (0: none); 1 if there are no n.  Every wavefront for itself.  (For 256 keys 64-bit comparisons were 4 us, and a search bit by bit as much: a step of it
+// is a chain from vector compare to scalar count and back.)
+__device__ __forceinline__ u64 bound_of(const u64* keys, int n) {
+    typedef u64 two __attribute__((ext_vector_type(2)));
+    const u64 own = keys[threadIdx.x & 63];
+    int larger = 0;
+#pragma unroll 8
+    for (int k = 0; k < 32; ++k) {
+        const two v = reinterpret_cast<const two*>(keys)[k];
+        larger += (v[0] > own) + (v[1] > own);
+    }
+    const u64 at = __ballot(own && larger == n - 1);
+    if (!at) return 1;
+    return __shfl(own, __ffsll((unsigned long long)at) - 1);
+}
 
 // The n largest of keys[0 .. count) (LDS, all different), in order, by how many are larger; out(place, key).
 template <typename Out>
@@ -97,15 +125,17 @@ __device__ __forceinline__ void in_order(const u64* keys, int count, int n, Out 
     for (int i = threadIdx.x; i < count; i += THREADS) {
         const u64 own = keys[i];
         int larger = 0;
+#pragma unroll 4
         for (int k = 0; k < count; ++k) larger += keys[k] > own;
         if (larger < n) out(larger, own);
     }
 }
 
 struct Work {
-    u64 keys[THREADS], passed[ROOM];
-    int chosen[MOST_TOP], count;
-    u64 bound;
+    alignas(16) u64 groups[64];   // largest of four threads each
+    u64 keys[THREADS];
+    u64 passed[ROOM];
+    int chosen[THREADS], holders, count;
     Sums sums[THREADS / 64];
 };
 
@@ -113,39 +143,36 @@ struct Work {
 template <typename T, typename Out>
 __device__ __forceinline__ void likeliest(const T* x, int n, int base, u64 best, int n_top, Work& work, Out out) {
     const int tid = threadIdx.x, wanted = min(n_top, n);
-    work.keys[tid] = best;
-    if (tid == 0) {
-        work.count = 0;
-        work.bound = 1;   // (fewer threads than tokens wanted: all pass)
-    }
+    u64 four = max(best, __shfl_xor(best, 1));
+    four = max(four, __shfl_xor(four, 2));
+    if ((tid & 3) == 0) work.groups[tid >> 2] = four;
+    if (tid == 0) work.count = work.holders = 0;
     __syncthreads();
-    int larger = 0;
-    for (int k = 0; k < THREADS; ++k) larger += work.keys[k] > best;
-    if (best && larger < wanted) work.chosen[larger] = tid;
-    if (best && larger == wanted - 1) work.bound = best;
-    const int holders = __syncthreads_count(best && larger < wanted);
-    const u64 bound = work.bound;
+    const u64 bound = bound_of(work.groups, wanted);
+    if (best >= bound) work.chosen[atomicAdd(&work.holders, 1)] = tid;   // (in any order: it is only a list)
+    __syncthreads();
+    const int holders = work.holders;
     const int runs = (n + RUN - 1) / RUN, each = (runs + THREADS - 1) / THREADS;
     for (int k = tid; k < holders * each; k += THREADS) {
         const int run = work.chosen[k % holders] + k / holders * THREADS;
         if (run >= runs) continue;
-        for (int e = 0; e < RUN; ++e) {
-            const int i = run * RUN + e;
-            const u64 key = i < n ? key_of(dbf_to_float(x[i]), base + i) : 0;
-            if (key >= bound) {
-                const int at = atomicAdd(&work.count, 1);   // (in any order: they are put in order by their keys)
-                if (at < ROOM) work.passed[at] = key;
-            }
-        }
+        auto pass = [&](u64 key) {
+            if (key < bound) return;
+            const int at = atomicAdd(&work.count, 1);   // (in any order: they are put in order by their keys)
+            if (at < ROOM) work.passed[at] = key;
+        };
+        keys_of_run(x, run * RUN, n, base, pass);
     }
     __syncthreads();
     const int count = work.count;
-    if (count <= ROOM) {
+    if (__builtin_expect(count <= ROOM, 1)) {
         in_order(work.passed, count, wanted, out);
     } else {   // rows made so that few threads hold thousands of the largest: one after the other
         u64 last = ~0ull;
+#pragma unroll 1
         for (int k = 0; k < wanted; ++k) {
             u64 top = 0;
+#pragma unroll 1
             for (int i = tid; i < n; i += THREADS) {
                 const u64 key = key_of(dbf_to_float(x[i]), base + i);
                 if ((k == 0 || key < last) && key > top) top = key;
@@ -163,8 +190,19 @@ __device__ __forceinline__ void likeliest(const T* x, int n, int base, u64 best,
     }
 }
 
-__device__ __forceinline__ void finish(const LogprobArgs& a, int row, Sums s, float target_value, int target, float log_s) {
-    if (a.logprob) a.logprob[row] = target < 0 ? 0.f : target >= a.vocab ? __builtin_nanf("") : (target_value - s.m) - log_s;
+// A row's target and its logit, asked for before anything else.
+struct Target {
+    int id;
+    float value;
+    template <typename T>
+    __device__ __forceinline__ Target(const LogprobArgs& a, int row, const T* x, bool asked) : id(-1), value(0.f) {
+        if (!asked || !a.logprob) return;
+        id = a.targets[row];
+        if (id >= 0 && id < a.vocab) value = dbf_to_float(x[id]);
+    }
+};
+__device__ __forceinline__ void finish(const LogprobArgs& a, int row, Sums s, const Target& target, float log_s) {
+    if (a.logprob) a.logprob[row] = target.id < 0 ? 0.f : target.id >= a.vocab ? __builtin_nanf("") : (target.value - s.m) - log_s;
     if (a.entropy) a.entropy[row] = log_s - s.t / s.s;
 }
 
@@ -173,50 +211,41 @@ __global__ __launch_bounds__(THREADS) void dbf_logprobs_kernel(const LogprobArgs
     __shared__ Work work;
     const int tid = threadIdx.x, row = blockIdx.x / a.slices, slice = blockIdx.x % a.slices, base = slice * a.slice, n = min(a.slice, a.vocab - base);
     const T* x = static_cast<const T*>(a.x) + row * a.stride + base;
+    const Target target(a, row, static_cast<const T*>(a.x) + row * a.stride, tid == 0 && a.slices == 1);
     Sums s = {LEAST, 0.f, 0.f};
     float most = -__builtin_inff();
     int most_run = INT_MAX;   // the first run that holds it
     constexpr int AHEAD = 4, STEP = THREADS * RUN * AHEAD;
-    if (n >= RUN) {
-        Run<T> run[AHEAD];
-        for (int i0 = tid * RUN; i0 < n; i0 += STEP) {
+    Run<T> run[AHEAD];
+    for (int i0 = tid * RUN; i0 < n; i0 += STEP) {
 #pragma unroll
-            for (int k = 0; k < AHEAD; ++k) run[k].load(x, i0 + k * THREADS * RUN, n);
-            float v[AHEAD][RUN], top = -__builtin_inff();
+        for (int k = 0; k < AHEAD; ++k) run[k].load(x, i0 + k * THREADS * RUN, n);
+        float v[AHEAD][RUN], top = -__builtin_inff();
 #pragma unroll
-            for (int k = 0; k < AHEAD; ++k) {
-                const int i = i0 + k * THREADS * RUN;
-                run[k].get(i, n, v[k]);
-                float largest = v[k][0];
+        for (int k = 0; k < AHEAD; ++k) {
+            const int i = i0 + k * THREADS * RUN;
+            run[k].get(i, n, v[k]);
+            float largest = v[k][0];
 #pragma unroll
-                for (int e = 1; e < RUN; ++e) largest = fmaxf(largest, v[k][e]);
-                if (TOP && i < n && (largest > most || most_run == INT_MAX)) {
-                    most = largest;
-                    most_run = i;
-                }
-                top = fmaxf(top, largest);
+            for (int e = 1; e < RUN; ++e) largest = fmaxf(largest, v[k][e]);
+            if (TOP && i < n && (largest > most || most_run == INT_MAX)) {
+                most = largest;
+                most_run = i;
             }
-            if (top > s.m + 8.f) {   // (rarely, once the first run is read)
-                const Sums o = s;
-                s = join(o, (Sums){fminf(top, 3.4e38f), 0.f, 0.f});
+            top = fmaxf(top, largest);
+        }
+        if (top > s.m + 8.f) {   // (rarely, once the first run is read)
+            const Sums o = s;
+            s = join(o, (Sums){fminf(top, 3.4e38f), 0.f, 0.f});
+        }
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+            for (int e = 0; e < RUN; ++e) {
+                const float d = v[k][e] - s.m, w = __builtin_amdgcn_exp2f(d * 1.44269504089f);
+                s.s += w;
+                s.t = fmaf(w, below(d), s.t);
             }
-#pragma unroll
-            for (int k = 0; k < AHEAD; ++k)
-#pragma unroll
-                for (int e = 0; e < RUN; ++e) {
-                    const float d = v[k][e] - s.m, w = __builtin_amdgcn_exp2f(d * 1.44269504089f);
-                    s.s += w;
-                    s.t = fmaf(w, below(d), s.t);
-                }
-        }
-    } else {
-        for (int i = tid; i < n; i += THREADS) {
-            const float v = dbf_to_float(x[i]);
-            s = (Sums){fminf(fmaxf(v, LEAST), 3.4e38f), 1.f, 0.f};
-            if (v - v != 0.f) s.s = s.t = v == -__builtin_inff() ? 0.f : __builtin_nanf("");
-            most = v;
-            most_run = i / RUN * RUN;
-        }
     }
     const bool number = s.s < __builtin_inff() && s.t == s.t;   // (a logit of +infinity makes the sum that)
     s = wave_join(s);
@@ -224,11 +253,10 @@ __global__ __launch_bounds__(THREADS) void dbf_logprobs_kernel(const LogprobArgs
     const bool numbers = !__syncthreads_or(!number);   // of the workgroup's part
     s = join(join(work.sums[0], work.sums[1]), join(work.sums[2], work.sums[3]));
     if (!numbers) s.s = s.t = __builtin_nanf("");
-    const float log_s = s.s > 0.f ? logf(s.s) : __builtin_nanf("");
+    const float log_s = log_of(s.s);
     if (tid == 0) {
         if (a.slices == 1) {
-            const int target = a.logprob ? a.targets[row] : -1;
-            finish(a, row, s, target >= 0 && target < a.vocab ? dbf_to_float(x[target]) : 0.f, target, log_s);
+            finish(a, row, s, target, log_s);
         } else {
             a.part_sums[(long long)row * a.slices + slice] = s;
         }
@@ -236,27 +264,49 @@ __global__ __launch_bounds__(THREADS) void dbf_logprobs_kernel(const LogprobArgs
     if (!TOP) return;
     // the thread's largest key: the first of its values that is as large as any (or is no number)
     u64 best = 0;
-    if (most_run != INT_MAX) {
-        const int runs = (n + RUN - 1) / RUN;
-        if (numbers) {
-            for (int e = 0; e < RUN && most_run + e < n; ++e) best = max(best, key_of(dbf_to_float(x[most_run + e]), base + most_run + e));
-        } else {
-            for (int r = tid; r < runs; r += THREADS)
-                for (int e = 0; e < RUN && r * RUN + e < n; ++e) best = max(best, key_of(dbf_to_float(x[r * RUN + e]), base + r * RUN + e));
-        }
-    }
-    if (n < RUN && tid) best = 0;   // (one run: the first thread's)
-    if (n < RUN && tid == 0)
-        for (int e = 0; e < n; ++e) best = max(best, key_of(dbf_to_float(x[e]), base + e));
-    if (a.slices == 1) {
-        likeliest(x, n, base, best, a.n_top, work, [&](int k, u64 key) {
-            a.top_ids[(long long)row * a.n_top + k] = (int)~(unsigned)key;
-            a.top_logprobs[(long long)row * a.n_top + k] = (value_of(key) - s.m) - log_s;
-        });
+    auto keep = [&](u64 key) { best = max(best, key); };
+    if (__builtin_expect(numbers, 1)) {
+        if (most_run != INT_MAX) keys_of_run(x, most_run, n, base, keep);
     } else {
-        u64* list = a.part_top + ((long long)row * a.slices + slice) * a.n_top;
-        for (int k = n + tid; k < a.n_top; k += THREADS) list[k] = 0;
-        likeliest(x, n, base, best, a.n_top, work, [&](int k, u64 key) { list[k] = key; });
+#pragma unroll 1
+        for (int i = tid * RUN; i < n; i += THREADS * RUN) keys_of_run(x, i, n, base, keep);
+    }
+    const long long list = ((long long)row * a.slices + slice) * a.n_top;   // (of the row itself if it has one slice)
+    if (a.slices > 1)
+        for (int k = n + tid; k < a.n_top; k += THREADS) a.part_top[list + k] = 0;
+    likeliest(x, n, base, best, a.n_top, work, [&](int k, u64 key) {
+        if (a.slices > 1) {
+            a.part_top[list + k] = key;
+        } else {
+            a.top_ids[list + k] = (int)~(unsigned)key;
+            a.top_logprobs[list + k] = (value_of(key) - s.m) - log_s;
+        }
+    });
+}
+
+// Rows of fewer than RUN tokens: a thread to each.
+template <typename T>
+__global__ __launch_bounds__(THREADS) void dbf_logprobs_short_kernel(const LogprobArgs a) {
+    const int row = blockIdx.x * THREADS + threadIdx.x;
+    if (row >= a.n_rows) return;
+    const T* x = static_cast<const T*>(a.x) + row * a.stride;
+    Sums s = {LEAST, 0.f, 0.f};
+    for (int i = 0; i < a.vocab; ++i) {
+        const float v = dbf_to_float(x[i]);
+        s = join(s, (Sums){fminf(fmaxf(v, LEAST), 3.4e38f), v - v == 0.f ? 1.f : v == -__builtin_inff() ? 0.f : __builtin_nanf(""), 0.f});
+    }
+    const float log_s = log_of(s.s);
+    finish(a, row, s, Target(a, row, x, true), log_s);
+    u64 last = ~0ull;
+    for (int k = 0; k < a.n_top; ++k) {
+        u64 top = 0;
+        for (int i = 0; i < a.vocab; ++i) {
+            const u64 key = key_of(dbf_to_float(x[i]), i);
+            if ((k == 0 || key < last) && key > top) top = key;
+        }
+        last = top;
+        a.top_ids[(long long)row * a.n_top + k] = (int)~(unsigned)top;
+        a.top_logprobs[(long long)row * a.n_top + k] = (value_of(top) - s.m) - log_s;
     }
 }
 
@@ -268,35 +318,32 @@ __global__ __launch_bounds__(THREADS) void dbf_logprobs_join_kernel(const Logpro
     const Sums nothing = {LEAST, 0.f, 0.f};
     Sums s = tid < a.slices ? a.part_sums[(long long)row * a.slices + tid] : nothing;   // (slices <= THREADS)
     const u64* lists = a.part_top + (long long)row * a.slices * a.n_top;
-    const u64 first = a.n_top && tid < a.slices ? lists[(long long)tid * a.n_top] : 0;
+    const Target target(a, row, static_cast<const T*>(a.x) + row * a.stride, tid == 0);
+    u64 first = 0, listed[ROOM / THREADS];
+    if (a.n_top) {
+        if (tid < a.slices) first = lists[(long long)tid * a.n_top];
+#pragma unroll
+        for (int k = 0; k < ROOM / THREADS; ++k) listed[k] = tid + k * THREADS < a.slices * a.n_top ? lists[tid + k * THREADS] : 0;
+    }
     const bool number = s.s == s.s;
     s = wave_join(s);
     if ((tid & 63) == 0) work.sums[tid >> 6] = s;
     const bool numbers = !__syncthreads_or(!number);
     s = join(join(work.sums[0], work.sums[1]), join(work.sums[2], work.sums[3]));
     if (!numbers) s.s = s.t = __builtin_nanf("");
-    const float log_s = s.s > 0.f ? logf(s.s) : __builtin_nanf("");
+    const float log_s = log_of(s.s);
     if (tid == 0) {
-        const int target = a.logprob ? a.targets[row] : -1;
-        finish(a, row, s, target >= 0 && target < a.vocab ? dbf_to_float((static_cast<const T*>(a.x) + row * a.stride)[target]) : 0.f, target, log_s);
+        finish(a, row, s, target, log_s);
     }
     if (!a.n_top) return;
     // the same bound again: of slices' largest; at most n_top slices have keys that pass
-    work.keys[tid] = first;
-    if (tid == 0) {
-        work.count = 0;
-        work.bound = 1;
-    }
+    if (tid < 64) work.groups[tid] = first;
+    if (tid == 0) work.count = 0;
     __syncthreads();
-    int larger = 0;
-    for (int k = 0; k < a.slices; ++k) larger += work.keys[k] > first;
-    if (first && larger == a.n_top - 1) work.bound = first;
-    __syncthreads();
-    const u64 bound = work.bound;
-    for (int k = tid; k < a.slices * a.n_top; k += THREADS) {
-        const u64 key = lists[k];
-        if (key >= bound) work.passed[atomicAdd(&work.count, 1)] = key;   // (at most n_top lists: MOST_LISTED)
-    }
+    const u64 bound = bound_of(work.groups, a.n_top);
+#pragma unroll
+    for (int k = 0; k < ROOM / THREADS; ++k)
+        if (listed[k] >= bound) work.passed[atomicAdd(&work.count, 1)] = listed[k];   // (all lists together have room)
     __syncthreads();
     in_order(work.passed, work.count, a.n_top, [&](int k, u64 key) {
         a.top_ids[(long long)row * a.n_top + k] = (int)~(unsigned)key;
@@ -323,6 +370,10 @@ Room room_of(int n_rows, int vocab, int n_top) {
 
 template <typename T>
 int launch(const LogprobArgs& a, hipStream_t stream) {
+    if (a.vocab < RUN) {
+        hipLaunchKernelGGL(dbf_logprobs_short_kernel<T>, dim3((a.n_rows + THREADS - 1) / THREADS), dim3(THREADS), 0, stream, a);
+        return hipGetLastError() == hipSuccess ? DBF_OK : DBF_EHIP;
+    }
     const long long groups = (long long)a.slices * a.n_rows;
     if (groups > INT_MAX) return DBF_EINVAL;
     const dim3 grid((unsigned)groups), threads(THREADS);
