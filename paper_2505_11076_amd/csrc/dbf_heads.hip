@@ -1,8 +1,8 @@
 // Norms and rotation of query and key heads, and the write of keys and values to the cache in 4 bits (include/dbf.h: dbf_qk_norm_rope,
 // dbf_cache_append, dbf_cache_read).
 //
-// A wavefront takes one head of one token.  Norm: x w / sqrt(mean x^2 + eps); rotation: pairs (a cos - b sin, b cos + a sin); all of a head is in fp32 in LDS
-// when it is rounded, once: to 16 bits, or to a code per value with a scale and a zero per 64.
+// Norm: x w / sqrt(mean x^2 + eps); rotation: pairs (a cos - b sin, b cos + a sin).  In fp32, rounded once: to 16 bits, or to a code per value with a scale and
+// a zero per 64.
 #include <initializer_list>
 
 #include "dbf_cache.h"
@@ -32,6 +32,7 @@ __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
+// Any even head size: a wavefront takes one head of one token, by LDS.
 // A head's norm and rotation, from memory to `row` in LDS, by one wavefront.
 template <typename T>
 __device__ __forceinline__ void turn(const HeadsArgs& a, const T* x, const T* weight, int token, int lane, float* row) {
@@ -164,6 +165,195 @@ __global__ __launch_bounds__(64 * WAVES) void dbf_heads_kernel(const HeadsArgs a
     else store_cache<4>(a, row, v_row, slot, head, lane);
 }
 
+// Heads of 64 N values with pairs of whole quads: a head is 8 N lanes' with two quads (four values) each, so that a pair of quads that turn into each other is one lane's, and
+// 8 / N heads a wavefront's.  Query heads come first, then the key heads (with their values, where those go to the cache); a wavefront has one kind.
+// (A wavefront to a head, values of a lane 64 apart and through LDS: 238 us for 8191 tokens of 40 heads of 128, 165 us for 2047 of 32 + 32 into the cache.)
+template <typename T>
+struct Quad {
+    dbf_u2 w;
+    __device__ __forceinline__ void load(const T* x, int quad) { w = *reinterpret_cast<const dbf_u2_any*>(x + 4 * quad); }
+    __device__ __forceinline__ float operator[](int e) const { return dbf_to_float(__builtin_bit_cast(T, (uint16_t)(w[e >> 1] >> 16 * (e & 1)))); }
+    static __device__ __forceinline__ void store(T* x, int quad, const float* v) {
+        dbf_u2 out = {0u, 0u};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) out[e >> 1] |= (unsigned)__builtin_bit_cast(uint16_t, dbf_from_float<T>(v[e])) << 16 * (e & 1);
+        *reinterpret_cast<dbf_u2_any*>(x + 4 * quad) = out;
+    }
+};
+template <int N>   // of the 8 N lanes of a head, in all of them
+__device__ __forceinline__ float head_sum(float v) {
+    if constexpr (N == 1) return dbf_row8_sum_f(v);
+    v = dbf_row16_sum_f(v);
+    if constexpr (N == 2) return v;
+    const unsigned b = __builtin_bit_cast(unsigned, v);
+    const auto r = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+    return __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+}
+template <int N>
+__device__ __forceinline__ float head_max(float v) {
+    if constexpr (N == 1) return dbf_row8_max(v);
+    v = dbf_row16_max(v);
+    if constexpr (N == 2) return v;
+    const unsigned b = __builtin_bit_cast(unsigned, v);
+    const auto r = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+    return fmaxf(__builtin_bit_cast(float, (unsigned)r[0]), __builtin_bit_cast(float, (unsigned)r[1]));
+}
+// Four values' codes, 16 bits.
+__device__ __forceinline__ unsigned codes_of(const float* x, float by, float z) {
+    unsigned out = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) out |= (unsigned)fminf(fmaxf(rintf(x[e] / by) + z, 0.f), 15.f) << 4 * e;
+    return out;
+}
+__device__ __forceinline__ bool hold(float* x) {   // within what the cache holds; whether all are finite
+    bool fine = true;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const bool finite = fabsf(x[e]) < __builtin_inff();
+        fine = fine && finite;
+        x[e] = finite ? fminf(fmaxf(x[e], -DBF_CACHE_MOST), DBF_CACHE_MOST) : 0.f;
+    }
+    return fine;
+}
+
+template <typename T, int N, bool CACHE>
+__global__ __launch_bounds__(64 * WAVES) void dbf_heads_quads_kernel(const HeadsArgs a) {
+    constexpr int D = 64 * N, LANES = 8 * N, HEADS = 8 / N;
+    const int lane = threadIdx.x & 63, sub = lane % LANES;
+    const int q_steps = a.q ? (a.n_q + HEADS - 1) / HEADS : 0, k_steps = a.k ? (a.n_kv + HEADS - 1) / HEADS : 0;
+    const long long item = (long long)blockIdx.x * WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), per = q_steps + k_steps;
+    const int token = (int)(item / per), step = (int)(item % per);
+    if (token >= a.n_tokens) return;
+    const bool query = step < q_steps;
+    const int n = query ? a.n_q : a.n_kv, head = (query ? step : step - q_steps) * HEADS + lane / LANES;
+    const bool live = head < n;
+    const int at = live ? head : n - 1;
+    // the lane's quads
+    const int hq = a.interleaved ? 0 : a.rot >> 3;   // quads of half the rotated values
+    const int qa = sub < hq ? sub : 2 * sub, qb = sub < hq ? sub + hq : 2 * sub + 1;
+    const bool turns = a.rope && (a.interleaved ? 8 * sub < a.rot : sub < hq);
+    const T* x = query ? static_cast<const T*>(a.q) + token * a.q_stride : static_cast<const T*>(a.k) + token * a.k_stride;
+    const T* weight = static_cast<const T*>(query ? a.q_weight : a.k_weight);
+    Quad<T> xa, xb, wa, wb;
+    xa.load(x + (long long)at * D, qa);
+    xb.load(x + (long long)at * D, qb);
+    if (weight) {
+        wa.load(weight, qa);
+        wb.load(weight, qb);
+    }
+    // values of the cache: a quad and the one that shares its bytes
+    const int vq = sub / (4 * N), vp = (sub >> 2) % N, vu = sub & 3, va = 4 * (vp + 2 * N * vq) + vu;
+    int slot = -1;
+    Quad<T> ya, yb;
+    if (CACHE && !query) {
+        const T* v = static_cast<const T*>(a.v) + token * a.v_stride + (long long)at * D;
+        ya.load(v, va);
+        yb.load(v, va + 4 * N);
+        slot = a.slots[token];
+    }
+    dbf_f4 c = {1.f, 1.f, 1.f, 1.f}, sn = {0.f, 0.f, 0.f, 0.f};
+    if (a.rope) {
+        const int p = a.positions[token];
+        const bool known = p >= 0 && p < a.rope_len;
+        if (turns) {
+            typedef float f4_any __attribute__((ext_vector_type(4), aligned(4)));
+            const float* table = a.rope + (long long)(known ? p : 0) * a.rot + 4 * sub;
+            c = *reinterpret_cast<const f4_any*>(table);
+            sn = *reinterpret_cast<const f4_any*>(table + (a.rot >> 1));
+            if (!known) c[0] = c[1] = c[2] = c[3] = __builtin_nanf("");
+        }
+    }
+    float v[8];   // quad a, quad b
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        v[e] = xa[e];
+        v[4 + e] = xb[e];
+        sum = fmaf(v[e], v[e], fmaf(v[4 + e], v[4 + e], sum));
+    }
+    if (weight) {
+        const float scale = 1.f / sqrtf(head_sum<N>(sum) / (float)D + a.eps);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[e] *= scale * wa[e];
+            v[4 + e] *= scale * wb[e];
+        }
+    }
+    if (!turns) {   // (also no product with 0: its partner may be infinite)
+    } else if (a.interleaved) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float s = v[2 * e], t = v[2 * e + 1];
+            v[2 * e] = s * c[e] - t * sn[e];
+            v[2 * e + 1] = t * c[e] + s * sn[e];
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float s = v[e], t = v[4 + e];
+            v[e] = s * c[e] - t * sn[e];
+            v[4 + e] = t * c[e] + s * sn[e];
+        }
+    }
+    if (query || !CACHE) {
+        T* out = query ? static_cast<T*>(a.q_out) + token * a.q_out_stride : static_cast<T*>(a.k_out) + token * a.k_out_stride;
+        if (live) {
+            Quad<T>::store(out + (long long)head * D, qa, v);
+            Quad<T>::store(out + (long long)head * D, qb, v + 4);
+        }
+        return;
+    }
+    if (!CACHE || slot < 0 || slot >= a.n_slots) return;
+    float y[8];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        y[e] = ya[e];
+        y[4 + e] = yb[e];
+    }
+    const bool k_fine = hold(v), own_fine = hold(y) && k_fine;
+    const bool fine = !((__ballot(!own_fine) >> (lane & ~(LANES - 1))) & ((N == 4 ? 0xFFFFFFFFull : (1ull << LANES) - 1)));
+    // the keys' groups: a quad's group is that of its run of four quads
+    const int ga = (qa >> 2) % N, gb = (qb >> 2) % N;
+    float ks[N], kz[N];
+    float lo_a = fminf(fminf(v[0], v[1]), fminf(v[2], v[3])), hi_a = fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]));
+    float lo_b = fminf(fminf(v[4], v[5]), fminf(v[6], v[7])), hi_b = fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7]));
+    float sa = 0.f, za = 0.f, sb = 0.f, zb = 0.f, s_own = 0.f, z_own = 0.f;
+#pragma unroll
+    for (int p = 0; p < N; ++p) {
+        const float low = head_max<N>(fmaxf(fmaxf(ga == p ? -lo_a : 0.f, gb == p ? -lo_b : 0.f), 0.f)), high = head_max<N>(fmaxf(fmaxf(ga == p ? hi_a : 0.f, gb == p ? hi_b : 0.f), 0.f));
+        ks[p] = dbf_group_scale(high + low);
+        kz[p] = rintf(low / (ks[p] > 0.f ? ks[p] : 1.f));
+        if (ga == p) sa = ks[p], za = kz[p];
+        if (gb == p) sb = ks[p], zb = kz[p];
+        if (sub == p) s_own = ks[p], z_own = kz[p];
+    }
+    // the values' group: lanes of the same vp
+    float vlo = 0.f, vhi = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        vlo = fmaxf(vlo, -y[e]);
+        vhi = fmaxf(vhi, y[e]);
+    }
+#pragma unroll
+    for (int d : {1, 2, 4 * N}) {
+        vlo = fmaxf(vlo, __shfl_xor(vlo, d));
+        vhi = fmaxf(vhi, __shfl_xor(vhi, d));
+    }
+    const float vs = dbf_group_scale(vhi + vlo), v_by = vs > 0.f ? vs : 1.f, vz = rintf(vlo / v_by);
+    if (!live) return;
+    uint8_t* rec = a.cache + dbf_record_at(slot, head, a.n_kv, a.page_shift, D);
+    const int t = slot & 31, tile = t >> 4, g = (t >> 2) & 3, i = t & 3;
+    *reinterpret_cast<uint16_t*>(rec + t * 32 * N + 2 * qa) = (uint16_t)codes_of(v, sa > 0.f ? sa : 1.f, za);
+    *reinterpret_cast<uint16_t*>(rec + t * 32 * N + 2 * qb) = (uint16_t)codes_of(v + 4, sb > 0.f ? sb : 1.f, zb);
+    const unsigned low = codes_of(y, v_by, vz), high = codes_of(y + 4, v_by, vz);
+    uint8_t* bytes = rec + 1024 * N + 1024 * vp + 16 * (16 * g + 4 * vu) + 4 * (2 * vq + tile) + i;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) bytes[16 * e] = (uint8_t)((low >> 4 * e & 15) | (high >> 4 * e & 15) << 4);
+    dbf_h2* words = reinterpret_cast<dbf_h2*>(rec + 2048 * N);
+    if (sub < N) words[32 * sub + t] = (dbf_h2){(_Float16)s_own, (_Float16)(fine ? -s_own * z_own : __builtin_nanf(""))};
+    if (vq == 0 && vu == 0) words[32 * N + 32 * vp + t] = fine ? (dbf_h2){(_Float16)vs, (_Float16)(-vs * vz)} : (dbf_h2){(_Float16)0.f, (_Float16)0.f};
+}
+
 template <typename T>
 __global__ __launch_bounds__(64 * WAVES) void dbf_cache_read_kernel(const uint8_t* cache, const int* slots, int n_tokens, int n_slots, int n_kv, int dim,
                                                                     int page_shift, T* k_out, T* v_out) {
@@ -218,13 +408,28 @@ HeadsArgs heads_args(const dbf_heads* h) {
     return a;
 }
 
-int launch_heads(const HeadsArgs& a, int dtype, void* hip_stream) {
+template <typename T, int N>
+void launch_quads(const HeadsArgs& a, unsigned groups, hipStream_t stream) {
+    const auto kernel = a.cache ? dbf_heads_quads_kernel<T, N, true> : dbf_heads_quads_kernel<T, N, false>;
+    hipLaunchKernelGGL(kernel, dim3(groups), dim3(64 * WAVES), 0, stream, a);
+}
+template <typename T>
+int launch_heads(const HeadsArgs& a, hipStream_t stream) {
     if (!a.n_tokens) return DBF_OK;
-    const long long items = (long long)a.n_tokens * ((a.q ? a.n_q : 0) + (a.k ? a.n_kv : 0)), groups = (items + WAVES - 1) / WAVES;
+    // heads of 64, 128 and 256 values that turn by whole quads; any other by the general kernel
+    const bool quads = (a.dim == 64 || a.dim == 128 || a.dim == 256) && a.rot % 8 == 0;
+    const int heads = quads ? 512 / a.dim : 1;   // of a wavefront
+    const long long items = (long long)a.n_tokens * ((a.q ? (a.n_q + heads - 1) / heads : 0) + (a.k ? (a.n_kv + heads - 1) / heads : 0)), groups = (items + WAVES - 1) / WAVES;
     if (groups > INT_MAX) return DBF_EINVAL;
-    const auto kernel = dtype == DBF_F16 ? dbf_heads_kernel<_Float16> : dbf_heads_kernel<dbf_bf16>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(64 * WAVES), 0, static_cast<hipStream_t>(hip_stream), a);
+    if (!quads) hipLaunchKernelGGL(dbf_heads_kernel<T>, dim3((unsigned)groups), dim3(64 * WAVES), 0, stream, a);
+    else if (a.dim == 64) launch_quads<T, 1>(a, (unsigned)groups, stream);
+    else if (a.dim == 128) launch_quads<T, 2>(a, (unsigned)groups, stream);
+    else launch_quads<T, 4>(a, (unsigned)groups, stream);
     return hipGetLastError() == hipSuccess ? DBF_OK : DBF_EHIP;
+}
+
+int launch_heads(const HeadsArgs& a, int dtype, hipStream_t stream) {
+    return dtype == DBF_F16 ? launch_heads<_Float16>(a, stream) : launch_heads<dbf_bf16>(a, stream);
 }
 
 }  // namespace
@@ -237,7 +442,7 @@ extern "C" size_t dbf_cache_bytes(int n_pages, int page_tokens, int n_kv_heads, 
 extern "C" int dbf_qk_norm_rope(const dbf_heads* heads, void* hip_stream) {
     if (const int bad = check_heads(heads)) return bad;
     if (heads->k && (!heads->k_out || heads->k_out_stride < (long long)heads->n_kv_heads * heads->head_dim)) return DBF_EINVAL;
-    return launch_heads(heads_args(heads), heads->dtype, hip_stream);
+    return launch_heads(heads_args(heads), heads->dtype, static_cast<hipStream_t>(hip_stream));
 }
 
 extern "C" int dbf_cache_append(const dbf_heads* heads, const dbf_cache* cache, const int32_t* slots, void* hip_stream) {
@@ -251,7 +456,7 @@ extern "C" int dbf_cache_append(const dbf_heads* heads, const dbf_cache* cache, 
     a.cache = static_cast<uint8_t*>(cache->data);
     a.n_slots = cache->n_pages * cache->page_tokens;
     a.page_shift = dbf_page_shift(cache->page_tokens);
-    return launch_heads(a, heads->dtype, hip_stream);
+    return launch_heads(a, heads->dtype, static_cast<hipStream_t>(hip_stream));
 }
 
 extern "C" int dbf_cache_read(const dbf_cache* cache, const int32_t* slots, int n_tokens, void* k_out, void* v_out, int dtype, void* hip_stream) {
