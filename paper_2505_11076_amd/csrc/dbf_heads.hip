@@ -198,11 +198,16 @@ __device__ __forceinline__ float head_max(float v) {
     const auto r = __builtin_amdgcn_permlane16_swap(b, b, false, false);
     return fmaxf(__builtin_bit_cast(float, (unsigned)r[0]), __builtin_bit_cast(float, (unsigned)r[1]));
 }
-// Four values' codes, 16 bits.
+// Four values' codes, 16 bits.  The quotient x / by, correctly rounded, from 1 / by, correctly rounded: its remainder corrects the product (three instructions for ten of a division).
+// It has to be: a value of few bits may lie halfway between two codes.
 __device__ __forceinline__ unsigned codes_of(const float* x, float by, float z) {
+    const float inverse = 1.f / by;
     unsigned out = 0;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) out |= (unsigned)fminf(fmaxf(rintf(x[e] / by) + z, 0.f), 15.f) << 4 * e;
+    for (int e = 0; e < 4; ++e) {
+        const float near = x[e] * inverse, q = fmaf(fmaf(-near, by, x[e]), inverse, near);
+        out |= (unsigned)fminf(fmaxf(rintf(q) + z, 0.f), 15.f) << 4 * e;
+    }
     return out;
 }
 __device__ __forceinline__ bool hold(float* x) {   // within what the cache holds; whether all are finite
@@ -221,7 +226,9 @@ __global__ __launch_bounds__(64 * WAVES) void dbf_heads_quads_kernel(const Heads
     constexpr int D = 64 * N, LANES = 8 * N, HEADS = 8 / N;
     const int lane = threadIdx.x & 63, sub = lane % LANES;
     const int q_steps = a.q ? (a.n_q + HEADS - 1) / HEADS : 0, k_steps = a.k ? (a.n_kv + HEADS - 1) / HEADS : 0;
-    const long long item = (long long)blockIdx.x * WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), per = q_steps + k_steps;
+    // (neighbouring tokens, whose values share the cache's bytes and lines, to one compute die: workgroups are dealt out to the eight one by one)
+    const unsigned each = gridDim.x / 8, group = CACHE && blockIdx.x < 8 * each ? blockIdx.x % 8 * each + blockIdx.x / 8 : blockIdx.x;
+    const unsigned item = group * WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), per = q_steps + k_steps;
     const int token = (int)(item / per), step = (int)(item % per);
     if (token >= a.n_tokens) return;
     const bool query = step < q_steps;
@@ -420,7 +427,7 @@ int launch_heads(const HeadsArgs& a, hipStream_t stream) {
     const bool quads = (a.dim == 64 || a.dim == 128 || a.dim == 256) && a.rot % 8 == 0;
     const int heads = quads ? 512 / a.dim : 1;   // of a wavefront
     const long long items = (long long)a.n_tokens * ((a.q ? (a.n_q + heads - 1) / heads : 0) + (a.k ? (a.n_kv + heads - 1) / heads : 0)), groups = (items + WAVES - 1) / WAVES;
-    if (groups > INT_MAX) return DBF_EINVAL;
+    if (groups > INT_MAX / WAVES) return DBF_EINVAL;
     if (!quads) hipLaunchKernelGGL(dbf_heads_kernel<T>, dim3((unsigned)groups), dim3(64 * WAVES), 0, stream, a);
     else if (a.dim == 64) launch_quads<T, 1>(a, (unsigned)groups, stream);
     else if (a.dim == 128) launch_quads<T, 2>(a, (unsigned)groups, stream);
