@@ -198,25 +198,23 @@ __device__ __forceinline__ float head_max(float v) {
     const auto r = __builtin_amdgcn_permlane16_swap(b, b, false, false);
     return fmaxf(__builtin_bit_cast(float, (unsigned)r[0]), __builtin_bit_cast(float, (unsigned)r[1]));
 }
-// Four values' codes, 16 bits.  The quotient x / by, correctly rounded, from 1 / by, correctly rounded: its remainder corrects the product (three instructions for ten of a division).
-// It has to be: a value of few bits may lie halfway between two codes.
-__device__ __forceinline__ unsigned codes_of(const float* x, float by, float z) {
-    const float inverse = 1.f / by;
-    unsigned out = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const float near = x[e] * inverse, q = fmaf(fmaf(-near, by, x[e]), inverse, near);
-        out |= (unsigned)fminf(fmaxf(rintf(q) + z, 0.f), 15.f) << 4 * e;
-    }
-    return out;
+// A value's code, as a number.  The quotient x / by, correctly rounded, from 1 / by, correctly rounded: its remainder corrects the product (three instructions for ten of a
+// division).  It has to be: a value of few bits may lie halfway between two codes.
+__device__ __forceinline__ float code_of(float x, float by, float inverse, float z) {
+    const float near = x * inverse, q = fmaf(fmaf(-near, by, x), inverse, near);
+    return __builtin_amdgcn_fmed3f(rintf(q) + z, 0.f, 15.f);
 }
-__device__ __forceinline__ bool hold(float* x) {   // within what the cache holds; whether all are finite
+// Values within what the cache holds; whether all are finite.  (The sum of their sizes says that nothing is to be done, nearly always.)
+__device__ __forceinline__ bool hold(float* x) {
+    const float size = ((fabsf(x[0]) + fabsf(x[1])) + (fabsf(x[2]) + fabsf(x[3]))) + ((fabsf(x[4]) + fabsf(x[5])) + (fabsf(x[6]) + fabsf(x[7])));
     bool fine = true;
+    if (__any(!(size <= DBF_CACHE_MOST))) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const bool finite = fabsf(x[e]) < __builtin_inff();
-        fine = fine && finite;
-        x[e] = finite ? fminf(fmaxf(x[e], -DBF_CACHE_MOST), DBF_CACHE_MOST) : 0.f;
+        for (int e = 0; e < 8; ++e) {
+            const bool finite = fabsf(x[e]) < __builtin_inff();
+            fine = fine && finite;
+            x[e] = finite ? fminf(fmaxf(x[e], -DBF_CACHE_MOST), DBF_CACHE_MOST) : 0.f;
+        }
     }
     return fine;
 }
@@ -350,41 +348,64 @@ __global__ __launch_bounds__(64 * WAVES) void dbf_heads_quads_kernel(const Heads
     if (!live) return;
     uint8_t* rec = a.cache + dbf_record_at(slot, head, a.n_kv, a.page_shift, D);
     const int t = slot & 31, tile = t >> 4, g = (t >> 2) & 3, i = t & 3;
-    *reinterpret_cast<uint16_t*>(rec + t * 32 * N + 2 * qa) = (uint16_t)codes_of(v, sa > 0.f ? sa : 1.f, za);
-    *reinterpret_cast<uint16_t*>(rec + t * 32 * N + 2 * qb) = (uint16_t)codes_of(v + 4, sb > 0.f ? sb : 1.f, zb);
-    const unsigned low = codes_of(y, v_by, vz), high = codes_of(y + 4, v_by, vz);
+    auto pack = [](const float* x, float scale, float zero) {   // four codes, 16 bits: whole numbers below 2^16 in fp32
+        const float by = scale > 0.f ? scale : 1.f, inverse = 1.f / by;
+        return (uint16_t)(unsigned)fmaf(fmaf(fmaf(code_of(x[3], by, inverse, zero), 16.f, code_of(x[2], by, inverse, zero)), 16.f, code_of(x[1], by, inverse, zero)), 16.f,
+                                        code_of(x[0], by, inverse, zero));
+    };
+    *reinterpret_cast<uint16_t*>(rec + t * 32 * N + 2 * qa) = pack(v, sa, za);
+    *reinterpret_cast<uint16_t*>(rec + t * 32 * N + 2 * qb) = pack(v + 4, sb, zb);
+    const float v_inverse = 1.f / v_by;
     uint8_t* bytes = rec + 1024 * N + 1024 * vp + 16 * (16 * g + 4 * vu) + 4 * (2 * vq + tile) + i;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) bytes[16 * e] = (uint8_t)((low >> 4 * e & 15) | (high >> 4 * e & 15) << 4);
+    for (int e = 0; e < 4; ++e)
+        bytes[16 * e] = (uint8_t)(unsigned)fmaf(code_of(y[4 + e], v_by, v_inverse, vz), 16.f, code_of(y[e], v_by, v_inverse, vz));
     dbf_h2* words = reinterpret_cast<dbf_h2*>(rec + 2048 * N);
     if (sub < N) words[32 * sub + t] = (dbf_h2){(_Float16)s_own, (_Float16)(fine ? -s_own * z_own : __builtin_nanf(""))};
     if (vq == 0 && vu == 0) words[32 * N + 32 * vp + t] = fine ? (dbf_h2){(_Float16)vs, (_Float16)(-vs * vz)} : (dbf_h2){(_Float16)0.f, (_Float16)0.f};
 }
 
 template <typename T>
-__global__ __launch_bounds__(64 * WAVES) void dbf_cache_read_kernel(const uint8_t* cache, const int* slots, int n_tokens, int n_slots, int n_kv, int dim,
-                                                                    int page_shift, T* k_out, T* v_out) {
-    const int lane = threadIdx.x & 63;
-    const long long item = (long long)blockIdx.x * WAVES + (threadIdx.x >> 6);
-    const int token = (int)(item / n_kv), head = (int)(item % n_kv), n = dim / 64;
-    if (token >= n_tokens) return;
-    const int slot = slots[token];
-    const bool held = slot >= 0 && slot < n_slots;
-    const uint8_t* rec = cache + dbf_record_at(held ? slot : 0, head, n_kv, page_shift, dim);
-    const int t = slot & 31, tile = t >> 4, g = (t >> 2) & 3, i = t & 3;
-    for (int d = lane; d < dim; d += 64) {
-        const int run = d >> 4, p = run % n, r = run / n;
-        float kx = 0.f, vx = 0.f;
-        if (held) {
-            const dbf_h2 kw = reinterpret_cast<const dbf_h2*>(rec + 32 * dim)[32 * p + t], vw = reinterpret_cast<const dbf_h2*>(rec + 34 * dim)[32 * p + t];
-            const unsigned kb = rec[t * (dim / 2) + (d >> 1)], vb = rec[16 * dim + 1024 * p + 16 * (16 * g + (d & 15)) + 4 * (2 * (r >> 1) + tile) + i];
-            kx = fmaf((float)kw[0], (float)(kb >> 4 * (d & 1) & 15), (float)kw[1]);
-            vx = fmaf((float)vw[0], (float)(vb >> 4 * (r & 1) & 15), (float)vw[1]);
-        }
-        const long long at = ((long long)token * n_kv + head) * dim + d;
-        k_out[at] = dbf_from_float<T>(kx);
-        v_out[at] = dbf_from_float<T>(vx);
+__device__ __forceinline__ void store4(T* out, const float* v) {
+    if constexpr (sizeof(T) == 4) {
+        typedef float f4_any __attribute__((ext_vector_type(4), aligned(4)));
+        *reinterpret_cast<f4_any*>(out) = (f4_any){v[0], v[1], v[2], v[3]};
+    } else {
+        Quad<T>::store(out, 0, v);
     }
+}
+// Lanes as in the kernel above: a lane has two neighbouring quads of the keys, and of the values a quad and the one that shares its bytes.
+template <typename T, int N>
+__global__ __launch_bounds__(64 * WAVES) void dbf_cache_read_kernel(const uint8_t* cache, const int* slots, int n_tokens, int n_slots, int n_kv, int page_shift, T* k_out, T* v_out) {
+    constexpr int D = 64 * N, LANES = 8 * N, HEADS = 8 / N;
+    const int lane = threadIdx.x & 63, sub = lane % LANES, steps = (n_kv + HEADS - 1) / HEADS;
+    const unsigned item = blockIdx.x * WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int token = (int)(item / steps), head = (int)(item % steps) * HEADS + lane / LANES;
+    if (token >= n_tokens || head >= n_kv) return;
+    const int slot = slots[token];
+    float k[8] = {}, v[8] = {};
+    const int vq = sub / (4 * N), vp = (sub >> 2) % N, vu = sub & 3, va = 4 * (vp + 2 * N * vq) + vu;
+    if (slot >= 0 && slot < n_slots) {
+        const uint8_t* rec = cache + dbf_record_at(slot, head, n_kv, page_shift, D);
+        const int t = slot & 31, tile = t >> 4, g = (t >> 2) & 3, i = t & 3;
+        const dbf_h2* words = reinterpret_cast<const dbf_h2*>(rec + 2048 * N);
+        const dbf_h2 kw = words[32 * ((sub >> 1) % N) + t], vw = words[32 * N + 32 * vp + t];
+        const unsigned codes = *reinterpret_cast<const unsigned*>(rec + t * 32 * N + 4 * sub);
+        const uint8_t* bytes = rec + 1024 * N + 1024 * vp + 16 * (16 * g + 4 * vu) + 4 * (2 * vq + tile) + i;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) k[e] = fmaf((float)kw[0], (float)(codes >> 4 * e & 15), (float)kw[1]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const unsigned b = bytes[16 * e];
+            v[e] = fmaf((float)vw[0], (float)(b & 15), (float)vw[1]);
+            v[4 + e] = fmaf((float)vw[0], (float)(b >> 4), (float)vw[1]);
+        }
+    }
+    const long long at = ((long long)token * n_kv + head) * D;
+    store4(k_out + at + 8 * sub, k);
+    store4(k_out + at + 8 * sub + 4, k + 4);
+    store4(v_out + at + 4 * va, v);
+    store4(v_out + at + 4 * (va + 4 * N), v + 4);
 }
 
 // What is wrong with a call's heads: the same for both entry points.
@@ -439,6 +460,17 @@ int launch_heads(const HeadsArgs& a, int dtype, hipStream_t stream) {
     return dtype == DBF_F16 ? launch_heads<_Float16>(a, stream) : launch_heads<dbf_bf16>(a, stream);
 }
 
+template <typename T>
+int launch_read(const dbf_cache* c, const int32_t* slots, int n_tokens, void* k_out, void* v_out, hipStream_t stream) {
+    const int heads = 512 / c->head_dim;   // of a wavefront
+    const long long groups = ((long long)n_tokens * ((c->n_kv_heads + heads - 1) / heads) + WAVES - 1) / WAVES;
+    if (groups > INT_MAX / WAVES) return DBF_EINVAL;
+    const auto kernel = c->head_dim == 64 ? dbf_cache_read_kernel<T, 1> : c->head_dim == 128 ? dbf_cache_read_kernel<T, 2> : dbf_cache_read_kernel<T, 4>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(64 * WAVES), 0, stream, static_cast<const uint8_t*>(c->data), slots, n_tokens, c->n_pages * c->page_tokens, c->n_kv_heads,
+                       dbf_page_shift(c->page_tokens), static_cast<T*>(k_out), static_cast<T*>(v_out));
+    return hipGetLastError() == hipSuccess ? DBF_OK : DBF_EHIP;
+}
+
 }  // namespace
 
 extern "C" size_t dbf_cache_bytes(int n_pages, int page_tokens, int n_kv_heads, int head_dim) {
@@ -472,20 +504,8 @@ extern "C" int dbf_cache_read(const dbf_cache* cache, const int32_t* slots, int 
     const unsigned size = dtype == DBF_F32 ? 4 : 2;
     if (dbf_misaligned(slots, 4) || dbf_misaligned(k_out, size) || dbf_misaligned(v_out, size)) return DBF_EINVAL;
     if (!n_tokens) return DBF_OK;
-    const long long groups = ((long long)n_tokens * cache->n_kv_heads + WAVES - 1) / WAVES;
-    if (groups > INT_MAX) return DBF_EINVAL;
-    const dim3 grid((unsigned)groups), threads(64 * WAVES);
     const auto stream = static_cast<hipStream_t>(hip_stream);
-    const uint8_t* data = static_cast<const uint8_t*>(cache->data);
-    const int n_slots = cache->n_pages * cache->page_tokens, shift = dbf_page_shift(cache->page_tokens);
-    if (dtype == DBF_F16)
-        hipLaunchKernelGGL(dbf_cache_read_kernel<_Float16>, grid, threads, 0, stream, data, slots, n_tokens, n_slots, cache->n_kv_heads, cache->head_dim, shift,
-                           static_cast<_Float16*>(k_out), static_cast<_Float16*>(v_out));
-    else if (dtype == DBF_BF16)
-        hipLaunchKernelGGL(dbf_cache_read_kernel<dbf_bf16>, grid, threads, 0, stream, data, slots, n_tokens, n_slots, cache->n_kv_heads, cache->head_dim, shift,
-                           static_cast<dbf_bf16*>(k_out), static_cast<dbf_bf16*>(v_out));
-    else
-        hipLaunchKernelGGL(dbf_cache_read_kernel<float>, grid, threads, 0, stream, data, slots, n_tokens, n_slots, cache->n_kv_heads, cache->head_dim, shift,
-                           static_cast<float*>(k_out), static_cast<float*>(v_out));
-    return hipGetLastError() == hipSuccess ? DBF_OK : DBF_EHIP;
+    return dtype == DBF_F16    ? launch_read<_Float16>(cache, slots, n_tokens, k_out, v_out, stream)
+           : dtype == DBF_BF16 ? launch_read<dbf_bf16>(cache, slots, n_tokens, k_out, v_out, stream)
+                               : launch_read<float>(cache, slots, n_tokens, k_out, v_out, stream);
 }
