@@ -16,7 +16,6 @@ struct AttendArgs {
     int n_tokens, n_seq, n_q, n_kv, max_q, max_kv, table_stride, causal, n_pages, page_shift, dim;
     int group;             // query heads of a key head
     int chunk, parts;      // many rows: tokens of a part of the long axis, and parts
-    int halves;            // ... by workgroups of 256
     float scale;
     float *part_out, *part_stat;   // of a share's first and last piece: sums [share][2][row][head_dim], maximum and sum of the row's weights [..][2]
                                    // (many rows: [request][head][part][row])
@@ -31,13 +30,6 @@ constexpr int MOST_SHARES = 1024;
 constexpr int TILE = 64;             // tokens of a step of many rows
 #ifndef MANY_WAVES
 #define MANY_WAVES 4
-#endif
-#ifndef KEYS_AHEAD
-#define KEYS_AHEAD 6
-#define VALUES_AHEAD 6
-#endif
-#ifndef LEAST_HALVES
-#define LEAST_HALVES 192
 #endif
 constexpr int LEAST_CHUNK = 512;
 constexpr int FEW = 16;              // rows (tokens times heads) of a request and key head that are few
@@ -618,18 +610,6 @@ struct Share {
     }
 };
 
-// The reads of products' operands from LDS so many products ahead of them.
-template <int PRODUCTS, int AHEAD>
-__device__ __forceinline__ void ahead() {
-    __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
-#pragma unroll
-    for (int k = 0; k < PRODUCTS - AHEAD; ++k) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-    }
-    __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
-}
-
 __device__ __forceinline__ float both_max(float v) {   // of a lane and the one 32 on
     const unsigned b = __builtin_bit_cast(unsigned, v);
     const auto r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
@@ -641,59 +621,63 @@ __device__ __forceinline__ float both_sum(float v) {
     return __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
 }
 
-// A wavefront's 32 rows: which they are, their queries, statistics and sums.
 template <typename T, int N, int WAVES>
-struct Rows {
-    static constexpr int D = 64 * N;
-    int head, req, part, row, token_row, n_rows, kv;
-    int first, end;        // tokens of the workgroup's part that some of its rows see
-    int seen, all, some;   // tokens that the lane's row, all rows and some row of the wavefront see
-    bool live;
-    const T* query;
-    T* out;
-    dbf_h8 q[4 * N];
-    dbf_f16 o[2 * N];
-    float kappa, m, l;
-
-    // false: there are none, or they have been dealt with
-    __device__ __forceinline__ bool begin(const AttendArgs& a, int lane, int wave) {
-        // (a request's later rows see more: they come first)
-        const int block = gridDim.z - 1 - blockIdx.z, G = a.group, hf = lane >> 5;
-        head = blockIdx.x % a.n_kv, part = blockIdx.x / a.n_kv, req = blockIdx.y;
-        const Request r = request(a, req);
-        n_rows = min(r.rows, a.max_q) * G;
-        kv = r.kv;
-        const int row0 = block * 32 * WAVES;
-        if (row0 >= n_rows) return false;
-        row = row0 + 32 * wave + (lane & 31);
-        live = row < n_rows;
-        const int t = live ? row / G : 0, h = head * G + (live ? row % G : 0);
-        query = static_cast<const T*>(a.q) + (long long)(r.row0 + t) * a.q_stride + (long long)h * D + 8 * hf;
-        out = static_cast<T*>(a.out) + (long long)(r.row0 + t) * a.out_stride + (long long)h * D;
-        if (!r.ok) {
-            if (live && part == 0)
-                for (int d = 4 * hf; d < D; d += 8)
-                    for (int i = 0; i < 4; ++i) out[d + i] = dbf_from_float<T>(__builtin_nanf(""));
-            return false;
-        }
-        auto sees = [&](int of) { return a.causal ? r.kv - r.rows + of / G + 1 : r.kv; };
-        first = part * a.chunk;
-        end = min(sees(min(row0 + 32 * WAVES, n_rows) - 1), a.parts > 1 ? min(first + a.chunk, r.kv) : r.kv);
-        seen = live ? sees(row) : 0;
-        all = sees(row0 + 32 * wave);
-        some = row0 + 32 * wave >= n_rows ? 0 : sees(min(row0 + 32 * wave + 32, n_rows) - 1);
-        m = LOWEST;
-        l = 0.f;
-#pragma unroll
-        for (int j = 0; j < 2 * N; ++j) o[j] = (dbf_f16){};
-        return true;
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(N == 4 ? 1 : 2))) void dbf_attend_many_kernel(const AttendArgs a) {
+    constexpr int D = 64 * N;
+    __shared__ Tiles<N, WAVES> tiles;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hf = lane >> 5, G = a.group;
+    // (a request's later rows see more: they come first)
+    const int head = blockIdx.x % a.n_kv, part = blockIdx.x / a.n_kv, req = blockIdx.y, block = gridDim.z - 1 - blockIdx.z;
+    const Request r = request(a, req);
+    const int rows = min(r.rows, a.max_q) * G, row0 = block * 32 * WAVES;
+    if (row0 >= rows) return;
+    const int row = row0 + 32 * wave + (lane & 31), t = row / G;   // the column's row, of the request's token t
+    const bool live = row < rows;
+    T* out = static_cast<T*>(a.out) + (long long)(r.row0 + (live ? t : 0)) * a.out_stride + (long long)(head * G + (live ? row % G : 0)) * D;
+    if (!r.ok) {
+        if (live && part == 0)
+            for (int d = 4 * hf; d < D; d += 8)
+                for (int i = 0; i < 4; ++i) out[d + i] = dbf_from_float<T>(__builtin_nanf(""));
+        return;
     }
-    // of each 16 values the lane's 8, in the order of a word's codes
-    __device__ __forceinline__ void queries(const AttendArgs& a, int lane) {
+    // tokens of the workgroup's part that some of its rows see; those that all rows and those that some rows of the wavefront see
+    const int last_t = min(row0 + 32 * WAVES, rows) - 1;
+    const int begin = part * a.chunk, end = min(a.causal ? r.kv - r.rows + last_t / G + 1 : r.kv, a.parts > 1 ? min(begin + a.chunk, r.kv) : r.kv);
+    const int seen = !live ? 0 : a.causal ? r.kv - r.rows + t + 1 : r.kv;
+    const int wave_all = a.causal ? r.kv - r.rows + (row0 + 32 * wave) / G + 1 : r.kv;
+    const int wave_some = row0 + 32 * wave >= rows ? 0 : a.causal ? r.kv - r.rows + (min(row0 + 32 * wave + 32, rows) - 1) / G + 1 : r.kv;
+    const int* table = a.table + (long long)req * a.table_stride;
+    const int per_page = a.page_shift - 5, last = (end + 31) / 32 - 1;
+    bool known0 = true, known1 = true;
+    auto at = [&](int b, bool& is) {
+        b = min(b, last);
+        const int page = scalar(table + (b >> per_page));
+        is = (unsigned)page < (unsigned)a.n_pages;
+        return a.cache + ((((long long)(is ? page : 0) * a.n_kv + head) << per_page) + (b & ((1 << per_page) - 1))) * dbf_record_bytes(D);
+    };
+    Share<N, WAVES> share;
+    auto load = [&](int first) {
+        const uint8_t* rec0 = at(first / 32, known0);
+        const uint8_t* rec1 = at(first / 32 + 1, known1);
+        share.load(rec0, rec1, lane, wave);
+    };
+    auto store = [&](int first, int which) {
+        if (first + TILE > r.kv || !known0 || !known1) {
+            asm volatile("");
+            share.blank(r.kv - first, known0, known1, lane, wave);
+        }
+        share.store(tiles, which, lane, wave);
+    };
+    if (begin < end) load(begin);
+    // the column's query: of each 16 values the lane's 8, in the order of a word's codes
+    dbf_h8 q[4 * N];
+    float kappa;
+    {
+        const T* x = static_cast<const T*>(a.q) + (long long)(r.row0 + (live ? t : 0)) * a.q_stride + (long long)(head * G + (live ? row % G : 0)) * D + 8 * hf;
         float most = 0.f;
         for (int k = 0; k < 4 * N; ++k) {
             float v[8];
-            load8(query + 16 * k, v);
+            load8(x + 16 * k, v);
 #pragma unroll
             for (int e = 0; e < 8; ++e) most = fmaxf(most, live ? fabsf(v[e]) : 0.f);
         }
@@ -703,7 +687,7 @@ struct Rows {
 #pragma unroll
         for (int k = 0; k < 4 * N; ++k) {
             float v[8];
-            load8(query + 16 * k, v);
+            load8(x + 16 * k, v);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float y = live ? ldexpf(v[4 * (e & 1) + (e & 2) + (e >> 2)], up) : 0.f;
@@ -711,285 +695,79 @@ struct Rows {
             }
         }
     }
-    // The weights of the tile that begins at token `from`, from its products x.
-    __device__ __forceinline__ void weigh(int from, int hf, dbf_f16 (&x)[2], dbf_h8 (&weights)[4]) {
-        if (from + TILE > all) {
-            asm volatile("");
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) x[b][i] = from + 32 * b + 8 * (i >> 2) + 4 * hf + (i & 3) < seen ? x[b][i] : -__builtin_inff();
-        }
-        float most = x[0][0];
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) most = fmaxf(most, x[b][i]);
-        most *= kappa;
-        if (__any(most > m + 8.f)) {
-            const float to = fmaxf(m, both_max(most)), keep = __builtin_amdgcn_exp2f(m - to);
-            m = to;
-            l *= keep;
-#pragma unroll
-            for (int j = 0; j < 2 * N; ++j) o[j] *= keep;
-        }
-        const float less = 7.f - m;
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float w = __builtin_amdgcn_exp2f(fmaf(x[b][i], kappa, less));
-                l += w;
-                weights[2 * b + (i >> 3)][(i & 4) + 2 * (i & 1) + (i >> 1 & 1)] = (_Float16)w;
-            }
-    }
-    __device__ __forceinline__ void write(const AttendArgs& a, int hf) {
-        l = both_sum(l);
-        if (!live) return;
-        if (a.parts == 1) {
-            const float by = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-            for (int j = 0; j < 2 * N; ++j)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) out[32 * j + 8 * (i >> 2) + 4 * hf + (i & 3)] = dbf_from_float<T>(o[j][i] * by);
-            return;
-        }
-        const long long piece = (((long long)req * a.n_kv + head) * a.parts + part) * (a.max_q * a.group) + row;
-        if (hf == 0) {
-            a.part_stat[2 * piece] = m;
-            a.part_stat[2 * piece + 1] = l;
-        }
-#pragma unroll
-        for (int j = 0; j < 2 * N; ++j)
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                *reinterpret_cast<dbf_f4*>(a.part_out + piece * D + 32 * j + 8 * k + 4 * hf) = (dbf_f4){o[j][4 * k], o[j][4 * k + 1], o[j][4 * k + 2], o[j][4 * k + 3]};
-    }
-};
-
-template <typename T, int N, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(N == 4 ? 1 : 2))) void dbf_attend_many_kernel(const AttendArgs a) {
-    constexpr int D = 64 * N;
-    __shared__ Tiles<N, WAVES> tiles;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hf = lane >> 5;
-    Rows<T, N, WAVES> rows;
-    if (!rows.begin(a, lane, wave)) return;
-    const int* table = a.table + (long long)rows.req * a.table_stride;
-    const int begin = rows.first, end = rows.end, per_page = a.page_shift - 5, last = (end + 31) / 32 - 1;
-    bool known0 = true, known1 = true;
-    auto at = [&](int b, bool& is) {
-        b = min(b, last);
-        const int page = scalar(table + (b >> per_page));
-        is = (unsigned)page < (unsigned)a.n_pages;
-        return a.cache + ((((long long)(is ? page : 0) * a.n_kv + rows.head) << per_page) + (b & ((1 << per_page) - 1))) * dbf_record_bytes(D);
-    };
-    Share<N, WAVES> share;
-    auto load = [&](int first) {
-        const uint8_t* rec0 = at(first / 32, known0);
-        const uint8_t* rec1 = at(first / 32 + 1, known1);
-        share.load(rec0, rec1, lane, wave);
-    };
-    auto store = [&](int first, int which) {
-        if (first + TILE > rows.kv || !known0 || !known1) {
-            asm volatile("");
-            share.blank(rows.kv - first, known0, known1, lane, wave);
-        }
-        share.store(tiles, which, lane, wave);
-    };
-    if (begin < end) load(begin);
-    rows.queries(a, lane);
+    dbf_f16 o[2 * N] = {};
+    float m = LOWEST, l = 0.f;
     if (begin < end) store(begin, 0);
     int which = 0;
     for (int first = begin; first < end; first += TILE, which ^= 1) {
         __syncthreads();
         const bool more = first + TILE < end;
         if (more) load(first + TILE);
-        if (first < rows.some) {
+        if (first < wave_some) {
             dbf_f16 x[2] = {};
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int k = 0; k < 4 * N; ++k)
-                    x[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(dbf_h8, tiles.k[which][b][k][lane]), rows.q[k], x[b], 0, 0, 0);
-            ahead<8 * N, KEYS_AHEAD>();
-            dbf_h8 weights[4];
-            rows.weigh(first, hf, x, weights);
+                    x[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(dbf_h8, tiles.k[which][b][k][lane]), q[k], x[b], 0, 0, 0);
+            if (first + TILE > wave_all) {
+                asm volatile("");
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
+                for (int b = 0; b < 2; ++b)
 #pragma unroll
-                for (int j = 0; j < 2 * N; ++j)
-                    rows.o[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(dbf_h8, tiles.v[which][j][k][lane]), weights[k], rows.o[j], 0, 0, 0);
-            ahead<8 * N, VALUES_AHEAD>();
-        }
-        if (more) store(first + TILE, which ^ 1);
-    }
-    rows.write(a, hf);
-}
-
-// The same for 256 rows and heads of up to 128 values, by eight wavefronts in two halves, one of each half to a SIMD, half a step apart: while one multiplies -- the values of the tile
-// before, then the keys of this one -- the other makes its weights and its share of the tiles to come, so that matrix and vector instructions meet.  (Four wavefronts that do one after the
-// other and are not held apart take turns at each pipe instead: 224 us for the prompts of 2048 rows on 3001 tokens, of which 61 were the making of tiles, for 128 rows only.)
-template <int N>
-struct Portion {
-    static constexpr bool ALL = 4 * N >= 8;   // whether all eight wavefronts have one
-    static constexpr int EACH = ALL ? 4 * N / 8 : 1;
-    dbf_u2 k[EACH];
-    unsigned kw[EACH], v[EACH][2];
-    dbf_u4 vw[EACH][2];
-    bool known;   // the page of the lane's keys
-
-    // keys: a run of 16 values of the tile's 64 tokens, one to a lane
-    __device__ __forceinline__ void load_keys(const uint8_t* rec0, const uint8_t* rec1, bool known0, bool known1, int lane, int wave) {
-        const uint8_t* rec = lane < 32 ? rec0 : rec1;
-        const int token = lane & 31;
-        known = lane < 32 ? known0 : known1;
-        if (ALL || wave < 4 * N)
-#pragma unroll
-            for (int e = 0; e < EACH; ++e) {
-                const int run = wave + 8 * e;
-                k[e] = *reinterpret_cast<const dbf_u2*>(rec + token * 32 * N + 8 * run);
-                kw[e] = *reinterpret_cast<const unsigned*>(rec + 2048 * N + 128 * (run % N) + 4 * token);
+                    for (int i = 0; i < 16; ++i) x[b][i] = first + 32 * b + 8 * (i >> 2) + 4 * hf + (i & 3) < seen ? x[b][i] : -__builtin_inff();
             }
-    }
-    __device__ __forceinline__ void store_keys(dbf_u4 (&to)[2][4 * N][64], int lane, int wave) const {
-        if (ALL || wave < 4 * N)
-#pragma unroll
-            for (int e = 0; e < EACH; ++e) {
-                const unsigned w = known ? kw[e] : 0x7E007E00u;   // (no numbers of a page that is missing)
-                const dbf_h2 s = lows(w, w), b = highs(w, w);
-#pragma unroll
-                for (int hf = 0; hf < 2; ++hf) {
-                    unsigned x[4];
-                    values(k[e][hf], s, b, s, b, x[0], x[1], x[2], x[3]);
-                    to[lane >> 5][wave + 8 * e][(lane & 31) + 32 * hf] = (dbf_u4){x[0], x[1], x[2], x[3]};
-                }
-            }
-    }
-    // values: of a group and 16 tokens (record wave & 1, half of it wave >> 1 & 1), lanes: place l, half of the fours of tokens hf, pair of runs q
-    __device__ __forceinline__ void load_values(const uint8_t* rec, int lane, int wave) {
-        const int l = lane & 15, hf = lane >> 4 & 1, q = lane >> 5, t = wave >> 1 & 1;
-        if (ALL || wave < 4 * N)
-#pragma unroll
-            for (int e = 0; e < EACH; ++e)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int p = (wave >> 2) + 2 * e, g = hf + 2 * h;
-                    v[e][h] = *reinterpret_cast<const unsigned*>(rec + 1024 * N + 1024 * p + 16 * (16 * g + l) + 4 * (2 * q + t));
-                    vw[e][h] = *reinterpret_cast<const dbf_u4*>(rec + 2176 * N + 128 * p + 64 * t + 16 * g);
-                }
-    }
-    // ... of which those from token `there` of the tile on are not there
-    __device__ __forceinline__ void blank_values(int there, int lane, int wave) {
-        const int hf = lane >> 4 & 1, t = wave >> 1 & 1;
-#pragma unroll
-        for (int e = 0; e < EACH; ++e)
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (32 * (wave & 1) + 16 * t + 4 * (hf + 2 * h) + i >= there) vw[e][h][i] = 0;
-    }
-    __device__ __forceinline__ void store_values(dbf_u4 (&to)[2 * N][4][64], int lane, int wave) const {
-        const int l = lane & 15, hf = lane >> 4 & 1, q = lane >> 5, m = 2 * (wave & 1) + (wave >> 1 & 1);
-        if (ALL || wave < 4 * N)
-#pragma unroll
-            for (int e = 0; e < EACH; ++e) {
-                unsigned lo[4], hi[4];
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const dbf_u4 w = vw[e][h];
-                    values(v[e][h], lows(w[0], w[2]), highs(w[0], w[2]), lows(w[1], w[3]), highs(w[1], w[3]), lo[2 * h], lo[2 * h + 1], hi[2 * h], hi[2 * h + 1]);
-                }
-                const int low = (wave >> 2) + 2 * e + N * 2 * q, high = low + N;
-                to[low >> 1][m][16 * (low & 1) + l + 32 * hf] = (dbf_u4){lo[0], lo[1], lo[2], lo[3]};
-                to[high >> 1][m][16 * (high & 1) + l + 32 * hf] = (dbf_u4){hi[0], hi[1], hi[2], hi[3]};
-            }
-    }
-};
-
-template <typename T, int N>
-__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void dbf_attend_halves_kernel(const AttendArgs a) {
-    constexpr int D = 64 * N;
-    __shared__ Tiles<N, 8> tiles;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hf = lane >> 5, half = wave >> 2;
-    Rows<T, N, 8> rows;
-    if (!rows.begin(a, lane, wave)) return;
-    const int begin = rows.first, end = rows.end, n = (end - begin + TILE - 1) / TILE;
-    const int* table = a.table + (long long)rows.req * a.table_stride;
-    const int per_page = a.page_shift - 5, last = (end + 31) / 32 - 1;
-    auto at = [&](int b, bool& is) {
-        b = min(b, last);
-        const int page = scalar(table + (b >> per_page));
-        is = (unsigned)page < (unsigned)a.n_pages;
-        return a.cache + ((((long long)(is ? page : 0) * a.n_kv + rows.head) << per_page) + (b & ((1 << per_page) - 1))) * dbf_record_bytes(D);
-    };
-    Portion<N> portion;
-    bool known_values = true;
-    auto load_keys = [&](int i) {
-        bool known0, known1;
-        const uint8_t* rec0 = at(begin / 32 + 2 * i, known0);
-        const uint8_t* rec1 = at(begin / 32 + 2 * i + 1, known1);
-        portion.load_keys(rec0, rec1, known0, known1, lane, wave);
-    };
-    auto load_values = [&](int i) { portion.load_values(at(begin / 32 + 2 * i + (wave & 1), known_values), lane, wave); };
-    // this wavefront's share of tile i's values and of the next one's keys, and the loads of those after them
-    auto make = [&](int i) {
-        const int there = known_values ? rows.kv - begin - TILE * i : 0;
-        if (there < TILE) {
-            asm volatile("");
-            portion.blank_values(there, lane, wave);
-        }
-        portion.store_values(tiles.v[i & 1], lane, wave);
-        portion.store_keys(tiles.k[(i + 1) & 1], lane, wave);
-        load_values(i + 1);
-        load_keys(i + 2);
-    };
-    if (n > 0) {
-        load_keys(0);
-        load_values(0);
-    }
-    rows.queries(a, lane);
-    dbf_f16 x[2];
-    dbf_h8 weights[4];
-    const int own = min(n, (rows.some - begin + TILE - 1) / TILE);   // tiles of which the wavefront sees some tokens
-    auto multiply = [&](int i) {
-        if (i > 0 && i <= own) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-#pragma unroll
-                for (int j = 0; j < 2 * N; ++j)
-                    rows.o[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(dbf_h8, tiles.v[(i - 1) & 1][j][k][lane]), weights[k], rows.o[j], 0, 0, 0);
-            ahead<8 * N, VALUES_AHEAD>();
-        }
-        if (i < own) {
-            x[0] = x[1] = (dbf_f16){};
+            float most = x[0][0];
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
-                for (int k = 0; k < 4 * N; ++k)
-                    x[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(dbf_h8, tiles.k[i & 1][b][k][lane]), rows.q[k], x[b], 0, 0, 0);
-            ahead<8 * N, KEYS_AHEAD>();
+                for (int i = 0; i < 16; ++i) most = fmaxf(most, x[b][i]);
+            most *= kappa;
+            if (__any(most > m + 8.f)) {
+                const float to = fmaxf(m, both_max(most)), keep = __builtin_amdgcn_exp2f(m - to);
+                m = to;
+                l *= keep;
+#pragma unroll
+                for (int j = 0; j < 2 * N; ++j) o[j] *= keep;
+            }
+            const float from = 7.f - m;
+            dbf_h8 weights[4];
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float w = __builtin_amdgcn_exp2f(fmaf(x[b][i], kappa, from));
+                    l += w;
+                    weights[2 * b + (i >> 3)][(i & 4) + 2 * (i & 1) + (i >> 1 & 1)] = (_Float16)w;
+                }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int j = 0; j < 2 * N; ++j)
+                    o[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(dbf_h8, tiles.v[which][j][k][lane]), weights[k], o[j], 0, 0, 0);
         }
-    };
-    if (n > 0) {
-        portion.store_keys(tiles.k[0], lane, wave);
-        load_keys(1);
-        __syncthreads();
-        if (half) {
-            make(0);
-            __syncthreads();
-        }
-        for (int i = 0; i < n; ++i) {
-            multiply(i);
-            __syncthreads();
-            if (i < own) rows.weigh(begin + TILE * i, hf, x, weights);
-            if (i + half < n) make(i + half);
-            __syncthreads();
-        }
-        multiply(n);
-        if (!half) __syncthreads();
+        if (more) store(first + TILE, which ^ 1);
     }
-    rows.write(a, hf);
+    l = both_sum(l);
+    if (!live) return;
+    if (a.parts == 1) {
+        const float by = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+        for (int j = 0; j < 2 * N; ++j)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) out[32 * j + 8 * (i >> 2) + 4 * hf + (i & 3)] = dbf_from_float<T>(o[j][i] * by);
+        return;
+    }
+    const long long piece = (((long long)req * a.n_kv + head) * a.parts + part) * (a.max_q * G) + row;
+    if (hf == 0) {
+        a.part_stat[2 * piece] = m;
+        a.part_stat[2 * piece + 1] = l;
+    }
+#pragma unroll
+    for (int j = 0; j < 2 * N; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            *reinterpret_cast<dbf_f4*>(a.part_out + piece * D + 32 * j + 8 * k + 4 * hf) = (dbf_f4){o[j][4 * k], o[j][4 * k + 1], o[j][4 * k + 2], o[j][4 * k + 3]};
 }
 
 // The parts of the rows of such a call: head_dim / 4 lanes to a row.
@@ -1033,7 +811,6 @@ struct Cut {
     bool few;
     int shares;         // few rows; 0: a workgroup to an item
     int chunk, parts;   // many rows
-    bool halves;        // ... by workgroups of 256
     size_t cut_bytes, stat_bytes, out_bytes;
 };
 Cut cut_of(const dbf_attend* a, const dbf_cache* c) {
@@ -1049,10 +826,8 @@ Cut cut_of(const dbf_attend* a, const dbf_cache* c) {
     k.parts = 1;
     if (!k.few && a->max_q > 0) {
         // The long axis in parts where the rows alone are few workgroups, of LEAST_CHUNK tokens at least
-        const long long rows = (long long)a->max_q * (a->n_q_heads / c->n_kv_heads), others = (long long)c->n_kv_heads * a->n_seq;
-        k.halves = c->head_dim <= 128 && rows >= LEAST_HALVES;
-        const long long groups = (k.halves ? (rows + 255) / 256 : (rows + 32 * MANY_WAVES - 1) / (32 * MANY_WAVES)) * others, fill = k.halves ? 256 : 512;
-        const long long parts = std::min<long long>((fill + groups - 1) / groups, (a->max_kv + LEAST_CHUNK - 1) / LEAST_CHUNK);
+        const long long rows = (long long)a->max_q * (a->n_q_heads / c->n_kv_heads), groups = (rows + 32 * MANY_WAVES - 1) / (32 * MANY_WAVES) * c->n_kv_heads * a->n_seq;
+        const long long parts = std::min<long long>((512 + groups - 1) / groups, (a->max_kv + LEAST_CHUNK - 1) / LEAST_CHUNK);
         if (parts > 1) {
             k.chunk = (int)(((a->max_kv + parts - 1) / parts + TILE - 1) / TILE * TILE);
             k.parts = (a->max_kv + k.chunk - 1) / k.chunk;
@@ -1079,13 +854,8 @@ template <typename T>
 bool launch_many(const AttendArgs& a, hipStream_t stream) {
     const long long rows = (long long)a.max_q * a.group, blocks = (rows + 32 * MANY_WAVES - 1) / (32 * MANY_WAVES), across = (long long)a.n_kv * a.parts;
     if (blocks > 65535 || across > INT_MAX || rows > INT_MAX) return false;
-    if (a.halves) {
-        const auto kernel = a.dim == 64 ? dbf_attend_halves_kernel<T, 1> : dbf_attend_halves_kernel<T, 2>;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)across, a.n_seq, (unsigned)((rows + 255) / 256)), dim3(512), 0, stream, a);
-    } else {
-        const auto kernel = a.dim == 64 ? dbf_attend_many_kernel<T, 1, MANY_WAVES> : a.dim == 128 ? dbf_attend_many_kernel<T, 2, MANY_WAVES> : dbf_attend_many_kernel<T, 4, MANY_WAVES>;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)across, a.n_seq, (unsigned)blocks), dim3(64 * MANY_WAVES), 0, stream, a);
-    }
+    const auto kernel = a.dim == 64 ? dbf_attend_many_kernel<T, 1, MANY_WAVES> : a.dim == 128 ? dbf_attend_many_kernel<T, 2, MANY_WAVES> : dbf_attend_many_kernel<T, 4, MANY_WAVES>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)across, a.n_seq, (unsigned)blocks), dim3(64 * MANY_WAVES), 0, stream, a);
     const int of = 256 / (a.dim / 4);
     if (a.parts > 1) hipLaunchKernelGGL(dbf_attend_parts_kernel<T>, dim3((unsigned)((rows + of - 1) / of), a.n_kv, a.n_seq), dim3(256), 0, stream, a);
     return true;
@@ -1131,7 +901,7 @@ extern "C" int dbf_cache_attend(const dbf_attend* attend, const dbf_cache* cache
         a.part_stat = reinterpret_cast<float*>(at + cut.cut_bytes);
         a.part_out = reinterpret_cast<float*>(at + cut.cut_bytes + cut.stat_bytes);
     }
-    a.group = a.n_q / a.n_kv;  a.chunk = cut.chunk;  a.parts = cut.parts;  a.halves = cut.halves;
+    a.group = a.n_q / a.n_kv;  a.chunk = cut.chunk;  a.parts = cut.parts;
     const auto stream = static_cast<hipStream_t>(hip_stream);
     return attend->dtype == DBF_F16 ? launch_attend<_Float16>(a, cut, stream) : launch_attend<dbf_bf16>(a, cut, stream);
 }
