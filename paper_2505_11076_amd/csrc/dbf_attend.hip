@@ -23,14 +23,9 @@ struct AttendArgs {
 };
 constexpr float LOWEST = -3.0e38f;   // of a running maximum: below all scores, and its difference from one is a number
 constexpr int MOST_SHARES = 1024;
-#ifndef BESIDE
-#define BESIDE 8
-#define LEAST_SHARED 1024
-#endif
+constexpr int BESIDE = 8;            // records' time that an item takes beside its records (4: batch of 64 in 88 us for 81; 12 and 16 the same)
 constexpr int TILE = 64;             // tokens of a step of many rows
-#ifndef MANY_WAVES
-#define MANY_WAVES 4
-#endif
+constexpr int MANY_WAVES = 4;       // wavefronts of a workgroup of many rows, 32 rows each
 constexpr int LEAST_CHUNK = 512;
 constexpr int FEW = 16;              // rows (tokens times heads) of a request and key head that are few
 
@@ -610,6 +605,18 @@ struct Share {
     }
 };
 
+// The reads of products' operands from LDS so many products ahead of them.
+template <int PRODUCTS, int AHEAD>
+__device__ __forceinline__ void ahead() {
+    __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+#pragma unroll
+    for (int k = 0; k < PRODUCTS - AHEAD; ++k) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
+}
+
 __device__ __forceinline__ float both_max(float v) {   // of a lane and the one 32 on
     const unsigned b = __builtin_bit_cast(unsigned, v);
     const auto r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
@@ -710,6 +717,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(N ==
 #pragma unroll
                 for (int k = 0; k < 4 * N; ++k)
                     x[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(dbf_h8, tiles.k[which][b][k][lane]), q[k], x[b], 0, 0, 0);
+            ahead<8 * N, 6>();
             if (first + TILE > wave_all) {
                 asm volatile("");
 #pragma unroll
@@ -745,6 +753,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(N ==
 #pragma unroll
                 for (int j = 0; j < 2 * N; ++j)
                     o[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(dbf_h8, tiles.v[which][j][k][lane]), weights[k], o[j], 0, 0, 0);
+            ahead<8 * N, 6>();
         }
         if (more) store(first + TILE, which ^ 1);
     }
@@ -816,7 +825,10 @@ struct Cut {
 Cut cut_of(const dbf_attend* a, const dbf_cache* c) {
     Cut k = {};
     k.few = (long long)a->max_q * (a->n_q_heads / c->n_kv_heads) <= FEW;
-    if (k.few && a->max_kv > LEAST_SHARED) {
+    // Items are shared out where the longest may be more than a workgroup should have: 2048 tokens, and more the more items there are to fill the chip beside it.  us, an item to a
+    // workgroup and shared out: 8 items of 1000 tokens 10.9 and 13.6, of 4000 29 and 17; 256 of 4000 32 and 38; 512 of 1 .. 4000 43 and 40, of 4000 52 and 62, of 1 .. 8192 78 and 69;
+    // 2400 of 1 .. 2500 90 and 113.  (The sums over all requests and the join of cut items are 8 us.)
+    if (k.few && a->max_kv > 2048 + 8LL * a->n_seq * c->n_kv_heads) {
         k.shares = 256 * few_waves(c->head_dim / 64);
         k.cut_bytes = (size_t)k.shares * 16;
         k.stat_bytes = (size_t)k.shares * 2 * FEW * 8;

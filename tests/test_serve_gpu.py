@@ -378,6 +378,18 @@ def test_cache_attend(kv, q_len, hq, hk, D, page, dtype, causal):
     check_attend(out, q, k, v, q_len, D, dtype, 1 / math.sqrt(D), causal, "attend")
 
 
+SHARED = [  # requests of which some are long and the items few: they are shared out among workgroups, cut anywhere
+    ([5000, 0, 33, 1, 9000, 64], [1] * 6, 4, 2, 64, 32, "f16", 1), ([4200, 3, 2600], [2, 1, 4], 4, 2, 256, 128, "bf16", 1), ([20011], [1], 16, 1, 128, 64, "f16", 1),
+    ([0, 0, 6000], [1, 1, 1], 7, 1, 128, 256, "bf16", 1), ([3000, 2999, 2, 7000], [3, 5, 5, 0], 4, 2, 128, 32, "f16", 0), ([70, 9, 2500, 0, 31] * 9, [1] * 45, 2, 1, 64, 32, "f16", 1),
+    ([12000, 2], [4, 8], 2, 1, 128, 64, "f16", 1), ([2400] * 3, [1] * 3, 8, 8, 256, 64, "f16", 1)]
+
+
+@pytest.mark.parametrize("kv,q_len,hq,hk,D,page,dtype,causal", SHARED)
+def test_cache_attend_shared_out(kv, q_len, hq, hk, D, page, dtype, causal):
+    assert max(kv) > 2048 + 8 * len(kv) * hk and max(q_len) * (hq // hk) <= 16
+    test_cache_attend(kv, q_len, hq, hk, D, page, dtype, causal)
+
+
 @pytest.mark.parametrize("kv,q_len,more", [([40, 300], [1, 1], 5000), ([40, 300], [30, 7], 3000), ([200], [200], 100)])
 def test_cache_attend_with_larger_bounds_than_lengths(kv, q_len, more):
     """max_q and max_kv choose the launch (parts, rows of a workgroup): what is beyond the lengths adds nothing."""
