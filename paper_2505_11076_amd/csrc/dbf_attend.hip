@@ -434,7 +434,7 @@ DBF_FEW_KERNEL(N) void dbf_attend_shares_kernel(const AttendArgs a) {
     while (item < hi) {
         const int first = (int)max(lo - item - BESIDE, 0LL), last = (int)min(hi - item - BESIDE, (long long)n);
         if (n ? last > first : item >= lo) {
-            const bool whole = first == 0 && last == n;
+            const bool whole = !n || (first == 0 && last == n);   // (an item without records is answered in the share that it begins in, also where its cost goes on in the next)
             if (!whole && first == 0 && tid == 0) {   // it begins here
                 a.cut[4 * share] = i;
                 a.cut[4 * share + 1] = head;
