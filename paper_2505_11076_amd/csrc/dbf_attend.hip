@@ -507,7 +507,8 @@ __global__ __launch_bounds__(256) void dbf_attend_join_kernel(const AttendArgs a
 
 // Many rows.  A workgroup takes 32 rows of a request and key head (tokens times the heads that share the keys) to each of its WAVES wavefronts, and walks the tokens in tiles
 // of 64: codes from memory to registers while the tile before is worked on, from there as exact fp16 values to LDS, once for all rows.
-//   scores:  K q^T, 32 tokens x 32 columns a product; a lane has 32 of a column's 64, the lane 32 on has the others.
+//   scores:  K q^T, 32 tokens x 32 columns a product; a lane has 32 of a column's 64, the lane 32 on has the others.  The tokens' order is such that the 8 of a lane that
+//            follow each other are those of a lane's 16 bytes of values in the cache.
 //   output:  V^T p^T, 32 values x 32 columns: the scores' places are the product's operand as they are, since the values' tokens are laid out in that order.
 // Both operands lie in LDS as the lanes take them, 16 bytes a lane one after the other.
 
@@ -516,62 +517,51 @@ struct Tiles {
     dbf_u4 k[2][2][4 * N][64], v[2][2 * N][4][64];   // [which][record][16 values][lane], [which][32 values][16 tokens][lane]
 };
 
-// A thread's share of a tile's bytes.  Keys: of token tid % 64, PIECES runs of 16 values; values: of a record, group and half of it, 16 places by 8 tokens.
+// A thread's share of a tile's bytes, all of one record: keys of a token, runs of 16 values; values of groups, 16 places by 8 tokens of the four.
 template <int N, int WAVES>
 struct Share {
     static constexpr int RUNS = 4 * N / WAVES > 0 ? 4 * N / WAVES : 1, UNITS = 2 * N / WAVES > 0 ? 2 * N / WAVES : 1;
     static constexpr bool ALL_KEYS = 4 * N >= WAVES, ALL_VALUES = 2 * N >= WAVES;   // whether all wavefronts have some
-    dbf_u2 k[RUNS], v[UNITS][2];
+    dbf_u2 k[RUNS];
     unsigned kw[RUNS];
-    dbf_u4 vw[UNITS][2][2];
+    dbf_u4 v[UNITS], vw[UNITS][2];
 
-    __device__ __forceinline__ void load(const uint8_t* rec0, const uint8_t* rec1, int lane, int wave) {
-        const int token = lane & 31;
-        const uint8_t* rec = lane < 32 ? rec0 : rec1;
+    __device__ __forceinline__ void load(const uint8_t* rec, int lane, int wave) {
+        const int token = lane & 31, g = lane >> 4;
         if (ALL_KEYS || wave < 4 * N) {
 #pragma unroll
             for (int e = 0; e < RUNS; ++e) {
-                const int run = wave * RUNS + e;
-                k[e] = *reinterpret_cast<const dbf_u2*>(rec + token * 32 * N + 8 * run);
-                kw[e] = *reinterpret_cast<const unsigned*>(rec + 2048 * N + 128 * (run % N) + 4 * token);
+                const int run = 2 * ((wave >> 1) * RUNS + e) + (lane >> 5);
+                k[e] = *reinterpret_cast<const dbf_u2*>(rec + (unsigned)(token * 32 * N + 8 * run));
+                kw[e] = *reinterpret_cast<const unsigned*>(rec + (unsigned)(2048 * N + 128 * (run % N) + 4 * token));
             }
         }
-        // lanes: place l, half of the four tokens' g, pair of runs q; wavefronts: record, then groups
-        const int l = lane & 15, hf = lane >> 4 & 1, q = lane >> 5;
-        const uint8_t* of = wave & 1 ? rec1 : rec0;
         if (ALL_VALUES || wave < 2 * N) {
 #pragma unroll
             for (int e = 0; e < UNITS; ++e) {
                 const int p = (wave >> 1) * UNITS + e;
+                v[e] = *reinterpret_cast<const dbf_u4*>(rec + (unsigned)(1024 * N + 1024 * p + 16 * lane));
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int g = hf + 2 * h;
-                    v[e][h] = *reinterpret_cast<const dbf_u2*>(of + 1024 * N + 1024 * p + 16 * (16 * g + l) + 8 * q);
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) vw[e][h][t] = *reinterpret_cast<const dbf_u4*>(of + 2176 * N + 128 * p + 64 * t + 16 * g);
-                }
+                for (int t = 0; t < 2; ++t) vw[e][t] = *reinterpret_cast<const dbf_u4*>(rec + (unsigned)(2176 * N + 128 * p + 64 * t + 16 * g));
             }
         }
     }
-    // Tokens that are not there (from `there` on, counted from the tile's first) and pages that are not: no values, and keys that are no numbers where the page is missing.
-    __device__ __forceinline__ void blank(int there, bool known0, bool known1, int lane, int wave) {
-        if (!(lane < 32 ? known0 : known1))
+    // Tokens that are not there (from `there` on, counted from the record's first) and pages that are not: no values, and keys that are no numbers where the page is missing.
+    __device__ __forceinline__ void blank(int there, bool known, int lane) {
+        if (!known)
 #pragma unroll
             for (int e = 0; e < RUNS; ++e) kw[e] = 0x7E007E00u;
-        const bool known = wave & 1 ? known1 : known0;
-        const int hf = lane >> 4 & 1;
 #pragma unroll
         for (int e = 0; e < UNITS; ++e)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (!known || 32 * (wave & 1) + 16 * t + 4 * (hf + 2 * h) + i >= there) vw[e][h][t][i] = 0;
+                for (int i = 0; i < 4; ++i)
+                    if (!known || 16 * t + 4 * (lane >> 4) + i >= there) vw[e][t][i] = 0;
     }
     __device__ __forceinline__ void store(Tiles<N, WAVES>& tiles, int which, int lane, int wave) const {
         if (ALL_KEYS || wave < 4 * N) {
+            const int place = (lane & 3) | (lane >> 2 & 1) << 2 | (lane >> 4 & 1) << 3 | (lane >> 3 & 1) << 4;   // the token's among the product's 32
 #pragma unroll
             for (int e = 0; e < RUNS; ++e) {
                 const dbf_h2 s = lows(kw[e], kw[e]), b = highs(kw[e], kw[e]);
@@ -579,26 +569,29 @@ struct Share {
                 for (int hf = 0; hf < 2; ++hf) {
                     unsigned x[4];
                     values(k[e][hf], s, b, s, b, x[0], x[1], x[2], x[3]);
-                    tiles.k[which][lane >> 5][wave * RUNS + e][(lane & 31) + 32 * hf] = (dbf_u4){x[0], x[1], x[2], x[3]};
+                    tiles.k[which][wave & 1][2 * ((wave >> 1) * RUNS + e) + (lane >> 5)][place + 32 * hf] = (dbf_u4){x[0], x[1], x[2], x[3]};
                 }
             }
         }
-        const int l = lane & 15, hf = lane >> 4 & 1, q = lane >> 5;
+        const int l = lane & 15, g = lane >> 4, m = 2 * (wave & 1) + (g >> 1);
         if (ALL_VALUES || wave < 2 * N) {
 #pragma unroll
             for (int e = 0; e < UNITS; ++e) {
                 const int p = (wave >> 1) * UNITS + e;
+                dbf_h2 s02[2], b02[2], s13[2], b13[2];
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
+                    const dbf_u4 w = vw[e][t];
+                    s02[t] = lows(w[0], w[2]), b02[t] = highs(w[0], w[2]), s13[t] = lows(w[1], w[3]), b13[t] = highs(w[1], w[3]);
+                }
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
                     unsigned lo[4], hi[4];
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const dbf_u4 w = vw[e][h][t];
-                        values(v[e][h][t], lows(w[0], w[2]), highs(w[0], w[2]), lows(w[1], w[3]), highs(w[1], w[3]), lo[2 * h], lo[2 * h + 1], hi[2 * h], hi[2 * h + 1]);
-                    }
-                    const int low = p + N * 2 * q, high = low + N, m = 2 * (wave & 1) + t;
-                    tiles.v[which][low >> 1][m][16 * (low & 1) + l + 32 * hf] = (dbf_u4){lo[0], lo[1], lo[2], lo[3]};
-                    tiles.v[which][high >> 1][m][16 * (high & 1) + l + 32 * hf] = (dbf_u4){hi[0], hi[1], hi[2], hi[3]};
+                    for (int t = 0; t < 2; ++t) values(v[e][2 * q + t], s02[t], b02[t], s13[t], b13[t], lo[2 * t], lo[2 * t + 1], hi[2 * t], hi[2 * t + 1]);
+                    const int low = p + N * 2 * q, high = low + N;
+                    tiles.v[which][low >> 1][m][16 * (low & 1) + l + 32 * (g & 1)] = (dbf_u4){lo[0], lo[1], lo[2], lo[3]};
+                    tiles.v[which][high >> 1][m][16 * (high & 1) + l + 32 * (g & 1)] = (dbf_u4){hi[0], hi[1], hi[2], hi[3]};
                 }
             }
         }
@@ -655,7 +648,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(N ==
     const int wave_some = row0 + 32 * wave >= rows ? 0 : a.causal ? r.kv - r.rows + (min(row0 + 32 * wave + 32, rows) - 1) / G + 1 : r.kv;
     const int* table = a.table + (long long)req * a.table_stride;
     const int per_page = a.page_shift - 5, last = (end + 31) / 32 - 1;
-    bool known0 = true, known1 = true;
+    bool known = true;
     auto at = [&](int b, bool& is) {
         b = min(b, last);
         const int page = scalar(table + (b >> per_page));
@@ -663,15 +656,11 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(N ==
         return a.cache + ((((long long)(is ? page : 0) * a.n_kv + head) << per_page) + (b & ((1 << per_page) - 1))) * dbf_record_bytes(D);
     };
     Share<N, WAVES> share;
-    auto load = [&](int first) {
-        const uint8_t* rec0 = at(first / 32, known0);
-        const uint8_t* rec1 = at(first / 32 + 1, known1);
-        share.load(rec0, rec1, lane, wave);
-    };
+    auto load = [&](int first) { share.load(at(first / 32 + (wave & 1), known), lane, wave); };
     auto store = [&](int first, int which) {
-        if (first + TILE > r.kv || !known0 || !known1) {
+        if (first + TILE > r.kv || !known) {
             asm volatile("");
-            share.blank(r.kv - first, known0, known1, lane, wave);
+            share.blank(r.kv - first - 32 * (wave & 1), known, lane);
         }
         share.store(tiles, which, lane, wave);
     };
@@ -723,36 +712,44 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(N ==
 #pragma unroll
                 for (int b = 0; b < 2; ++b)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) x[b][i] = first + 32 * b + 8 * (i >> 2) + 4 * hf + (i & 3) < seen ? x[b][i] : -__builtin_inff();
+                    for (int i = 0; i < 16; ++i) x[b][i] = first + 32 * b + 16 * (i >> 2 & 1) + 8 * (i >> 3) + 4 * hf + (i & 3) < seen ? x[b][i] : -__builtin_inff();
             }
-            float most = x[0][0];
+            // Weights by the maximum so far, times 2^7; their sum says whether one of them is too large for fp16 or far above the others' place: then the maximum is raised and they
+            // are made again, else nobody looks for it.  (Sums of the rounded weights, which the product below has: subnormal ones count here as they do there.)
+            unsigned weights[4][4];
+            auto weigh = [&] {
+                const float from = 7.f - m;
+                float sum[4] = {};   // (one after the other they wait for each other: 206 -> 203 us)
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
+                for (int b = 0; b < 2; ++b)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) most = fmaxf(most, x[b][i]);
-            most *= kappa;
-            if (__any(most > m + 8.f)) {
-                const float to = fmaxf(m, both_max(most)), keep = __builtin_amdgcn_exp2f(m - to);
+                    for (int i = 0; i < 16; i += (i & 1) ? 3 : 1) {
+                        const dbf_h2 w = {(_Float16)__builtin_amdgcn_exp2f(fmaf(x[b][i], kappa, from)), (_Float16)__builtin_amdgcn_exp2f(fmaf(x[b][i + 2], kappa, from))};
+                        sum[2 * b + (i & 1)] = __builtin_amdgcn_fdot2(w, (dbf_h2){(_Float16)1.f, (_Float16)1.f}, sum[2 * b + (i & 1)], false);
+                        weights[2 * b + (i >> 3)][2 * (i >> 2 & 1) + (i & 1)] = __builtin_bit_cast(unsigned, w);
+                    }
+                return (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            };
+            float sum = weigh();
+            if (__any(!(sum <= 0x1p15f))) {   // (also where it is no number)
+                float most = x[0][0];
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) most = fmaxf(most, x[b][i]);
+                const float to = fmaxf(m, both_max(most * kappa)), keep = __builtin_amdgcn_exp2f(m - to);
                 m = to;
                 l *= keep;
 #pragma unroll
                 for (int j = 0; j < 2 * N; ++j) o[j] *= keep;
+                sum = weigh();
             }
-            const float from = 7.f - m;
-            dbf_h8 weights[4];
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float w = __builtin_amdgcn_exp2f(fmaf(x[b][i], kappa, from));
-                    l += w;
-                    weights[2 * b + (i >> 3)][(i & 4) + 2 * (i & 1) + (i >> 1 & 1)] = (_Float16)w;
-                }
+            l += sum;
 #pragma unroll
             for (int k = 0; k < 4; ++k)
 #pragma unroll
                 for (int j = 0; j < 2 * N; ++j)
-                    o[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(dbf_h8, tiles.v[which][j][k][lane]), weights[k], o[j], 0, 0, 0);
+                    o[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(dbf_h8, tiles.v[which][j][k][lane]), __builtin_bit_cast(dbf_h8, (dbf_u4){weights[k][0], weights[k][1], weights[k][2], weights[k][3]}), o[j], 0, 0, 0);
             ahead<8 * N, 6>();
         }
         if (more) store(first + TILE, which ^ 1);
