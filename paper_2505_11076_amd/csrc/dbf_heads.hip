@@ -189,20 +189,43 @@ __device__ __forceinline__ float head_sum(float v) {
     const auto r = __builtin_amdgcn_permlane16_swap(b, b, false, false);
     return __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
 }
+// The largest of values that are not negative, by their bits (as numbers a maximum makes each of its operands a quiet one first): of the lanes of a head ...
+__device__ __forceinline__ unsigned larger(unsigned v, unsigned w) { return v > w ? v : w; }
 template <int N>
-__device__ __forceinline__ float head_max(float v) {
-    if constexpr (N == 1) return dbf_row8_max(v);
-    v = dbf_row16_max(v);
-    if constexpr (N == 2) return v;
-    const unsigned b = __builtin_bit_cast(unsigned, v);
-    const auto r = __builtin_amdgcn_permlane16_swap(b, b, false, false);
-    return fmaxf(__builtin_bit_cast(float, (unsigned)r[0]), __builtin_bit_cast(float, (unsigned)r[1]));
+__device__ __forceinline__ float head_max(float x) {
+    unsigned v = __builtin_bit_cast(unsigned, x);
+    v = larger(v, dbf_dpp_move<0xB1>(v));    // 1 away
+    v = larger(v, dbf_dpp_move<0x4E>(v));    // 2
+    v = larger(v, dbf_dpp_move<0x141>(v));   // 4: the other half of eight lanes, which has one value by now
+    if constexpr (N > 1) v = larger(v, dbf_dpp_move<0x128>(v));   // 8
+    if constexpr (N > 2) {
+        const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        v = larger(r[0], r[1]);
+    }
+    return __builtin_bit_cast(float, v);
 }
-// A value's code, as a number.  The quotient x / by, correctly rounded, from 1 / by, correctly rounded: its remainder corrects the product (three instructions for ten of a
-// division).  It has to be: a value of few bits may lie halfway between two codes.
+// ... and of those that agree in bits 2 .. of their place but the top one.
+template <int N>
+__device__ __forceinline__ float group_max(float x) {
+    unsigned v = __builtin_bit_cast(unsigned, x);
+    v = larger(v, dbf_dpp_move<0xB1>(v));
+    v = larger(v, dbf_dpp_move<0x4E>(v));
+    if constexpr (N == 1) v = larger(v, dbf_dpp_move<0x141>(v));
+    if constexpr (N == 2) v = larger(v, dbf_dpp_move<0x128>(v));
+    if constexpr (N == 4) {
+        const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        v = larger(r[0], r[1]);
+    }
+    return __builtin_bit_cast(float, v);
+}
+// A value's code, as a number.  Its quotient has to be correctly rounded: a value of few bits may lie halfway between two codes.
 __device__ __forceinline__ float code_of(float x, float by, float inverse, float z) {
-    const float near = x * inverse, q = fmaf(fmaf(-near, by, x), inverse, near);
-    return __builtin_amdgcn_fmed3f(rintf(q) + z, 0.f, 15.f);
+    return __builtin_amdgcn_fmed3f(rintf(dbf_quotient(x, by, inverse)) + z, 0.f, 15.f);
+}
+// 1 / by of a scale, correctly rounded: one of at most 7 bits, so its product with the approximate inverse is exact in the remainder, and no inverse lies near the middle of two fp32.
+__device__ __forceinline__ float inverse_of(float by) {
+    const float near = __builtin_amdgcn_rcpf(by);
+    return fmaf(fmaf(-by, near, 1.f), near, near);
 }
 // Values within what the cache holds; whether all are finite.  (The sum of their sizes says that nothing is to be done, nearly always.)
 __device__ __forceinline__ bool hold(float* x) {
@@ -319,18 +342,18 @@ __global__ __launch_bounds__(64 * WAVES) void dbf_heads_quads_kernel(const Heads
     const bool fine = !((__ballot(!own_fine) >> (lane & ~(LANES - 1))) & ((N == 4 ? 0xFFFFFFFFull : (1ull << LANES) - 1)));
     // the keys' groups: a quad's group is that of its run of four quads
     const int ga = (qa >> 2) % N, gb = (qb >> 2) % N;
-    float ks[N], kz[N];
+    float ks[N];
     float lo_a = fminf(fminf(v[0], v[1]), fminf(v[2], v[3])), hi_a = fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]));
     float lo_b = fminf(fminf(v[4], v[5]), fminf(v[6], v[7])), hi_b = fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7]));
-    float sa = 0.f, za = 0.f, sb = 0.f, zb = 0.f, s_own = 0.f, z_own = 0.f;
+    float sa = 0.f, za = 0.f, ia = 0.f, sb = 0.f, zb = 0.f, ib = 0.f, s_own = 0.f, z_own = 0.f;   // scales (1 for 0), zeros, inverses
 #pragma unroll
     for (int p = 0; p < N; ++p) {
         const float low = head_max<N>(fmaxf(fmaxf(ga == p ? -lo_a : 0.f, gb == p ? -lo_b : 0.f), 0.f)), high = head_max<N>(fmaxf(fmaxf(ga == p ? hi_a : 0.f, gb == p ? hi_b : 0.f), 0.f));
         ks[p] = dbf_group_scale(high + low);
-        kz[p] = rintf(low / (ks[p] > 0.f ? ks[p] : 1.f));
-        if (ga == p) sa = ks[p], za = kz[p];
-        if (gb == p) sb = ks[p], zb = kz[p];
-        if (sub == p) s_own = ks[p], z_own = kz[p];
+        const float by = ks[p] > 0.f ? ks[p] : 1.f, inverse = inverse_of(by), zero = rintf(dbf_quotient(low, by, inverse));
+        if (ga == p) sa = by, za = zero, ia = inverse;
+        if (gb == p) sb = by, zb = zero, ib = inverse;
+        if (sub == p) s_own = ks[p], z_own = zero;
     }
     // the values' group: lanes of the same vp
     float vlo = 0.f, vhi = 0.f;
@@ -339,23 +362,18 @@ __global__ __launch_bounds__(64 * WAVES) void dbf_heads_quads_kernel(const Heads
         vlo = fmaxf(vlo, -y[e]);
         vhi = fmaxf(vhi, y[e]);
     }
-#pragma unroll
-    for (int d : {1, 2, 4 * N}) {
-        vlo = fmaxf(vlo, __shfl_xor(vlo, d));
-        vhi = fmaxf(vhi, __shfl_xor(vhi, d));
-    }
-    const float vs = dbf_group_scale(vhi + vlo), v_by = vs > 0.f ? vs : 1.f, vz = rintf(vlo / v_by);
+    vlo = group_max<N>(vlo);
+    vhi = group_max<N>(vhi);
+    const float vs = dbf_group_scale(vhi + vlo), v_by = vs > 0.f ? vs : 1.f, v_inverse = inverse_of(v_by), vz = rintf(dbf_quotient(vlo, v_by, v_inverse));
     if (!live) return;
     uint8_t* rec = a.cache + dbf_record_at(slot, head, a.n_kv, a.page_shift, D);
     const int t = slot & 31, tile = t >> 4, g = (t >> 2) & 3, i = t & 3;
-    auto pack = [](const float* x, float scale, float zero) {   // four codes, 16 bits: whole numbers below 2^16 in fp32
-        const float by = scale > 0.f ? scale : 1.f, inverse = 1.f / by;
+    auto pack = [](const float* x, float by, float inverse, float zero) {   // four codes, 16 bits: whole numbers below 2^16 in fp32
         return (uint16_t)(unsigned)fmaf(fmaf(fmaf(code_of(x[3], by, inverse, zero), 16.f, code_of(x[2], by, inverse, zero)), 16.f, code_of(x[1], by, inverse, zero)), 16.f,
                                         code_of(x[0], by, inverse, zero));
     };
-    *reinterpret_cast<uint16_t*>(rec + t * 32 * N + 2 * qa) = pack(v, sa, za);
-    *reinterpret_cast<uint16_t*>(rec + t * 32 * N + 2 * qb) = pack(v + 4, sb, zb);
-    const float v_inverse = 1.f / v_by;
+    *reinterpret_cast<uint16_t*>(rec + t * 32 * N + 2 * qa) = pack(v, sa, ia, za);
+    *reinterpret_cast<uint16_t*>(rec + t * 32 * N + 2 * qb) = pack(v + 4, sb, ib, zb);
     uint8_t* bytes = rec + 1024 * N + 1024 * vp + 16 * (16 * g + 4 * vu) + 4 * (2 * vq + tile) + i;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
