@@ -242,20 +242,23 @@ __device__ __forceinline__ bool hold(float* x) {
     return fine;
 }
 
+// Tokens of a wavefront's key heads on their way to the cache: in a row of slots, four tokens' codes of a value share a word, which one lane writes.
+constexpr int tokens_together(int N, bool cache) { return !cache ? 1 : N == 4 ? 2 : 4; }
 template <typename T, int N, bool CACHE>
 __global__ __launch_bounds__(64 * WAVES) void dbf_heads_quads_kernel(const HeadsArgs a) {
-    constexpr int D = 64 * N, LANES = 8 * N, HEADS = 8 / N;
+    constexpr int D = 64 * N, LANES = 8 * N, HEADS = 8 / N, TOKENS = tokens_together(N, CACHE);
     const int lane = threadIdx.x & 63, sub = lane % LANES;
-    const int q_steps = a.q ? (a.n_q + HEADS - 1) / HEADS : 0, k_steps = a.k ? (a.n_kv + HEADS - 1) / HEADS : 0;
+    const int q_steps = a.q ? (a.n_q + HEADS - 1) / HEADS : 0, k_steps = a.k ? (a.n_kv * TOKENS + HEADS - 1) / HEADS : 0;
     // (neighbouring tokens, whose values share the cache's bytes and lines, to one compute die: workgroups are dealt out to the eight one by one)
     const unsigned each = gridDim.x / 8, group = CACHE && blockIdx.x < 8 * each ? blockIdx.x % 8 * each + blockIdx.x / 8 : blockIdx.x;
-    const unsigned item = group * WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), per = q_steps + k_steps;
-    const int token = (int)(item / per), step = (int)(item % per);
-    if (token >= a.n_tokens) return;
-    const bool query = step < q_steps;
-    const int n = query ? a.n_q : a.n_kv, head = (query ? step : step - q_steps) * HEADS + lane / LANES;
-    const bool live = head < n;
-    const int at = live ? head : n - 1;
+    const unsigned item = group * WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), per = TOKENS * q_steps + k_steps;
+    const int first = (int)(item / per) * TOKENS, step = (int)(item % per);   // first of its tokens
+    const bool query = step < TOKENS * q_steps;
+    const int turn = query ? step / q_steps : lane / LANES % TOKENS, there = first + turn;
+    if (query ? there >= a.n_tokens : first >= a.n_tokens) return;
+    const int n = query ? a.n_q : a.n_kv, head = query ? step % q_steps * HEADS + lane / LANES : (step - TOKENS * q_steps) * (HEADS / TOKENS) + lane / LANES / TOKENS;
+    const bool live = head < n && there < a.n_tokens;
+    const int at = min(head, n - 1), token = min(there, a.n_tokens - 1);
     // the lane's quads
     const int hq = a.interleaved ? 0 : a.rot >> 3;   // quads of half the rotated values
     const int qa = sub < hq ? sub : 2 * sub, qb = sub < hq ? sub + hq : 2 * sub + 1;
@@ -331,7 +334,11 @@ __global__ __launch_bounds__(64 * WAVES) void dbf_heads_quads_kernel(const Heads
         }
         return;
     }
-    if (!CACHE || slot < 0 || slot >= a.n_slots) return;
+    if constexpr (!CACHE) return;
+    const bool held = live && slot >= 0 && slot < a.n_slots;
+    if (!__any(held)) return;
+    const int slot0 = __shfl(slot, lane & ~(LANES * (TOKENS - 1)));   // the first token's
+    const bool row = __all(there < a.n_tokens && slot >= 0 && slot < a.n_slots && slot == slot0 + turn);
     float y[8];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -365,19 +372,54 @@ __global__ __launch_bounds__(64 * WAVES) void dbf_heads_quads_kernel(const Heads
     vlo = group_max<N>(vlo);
     vhi = group_max<N>(vhi);
     const float vs = dbf_group_scale(vhi + vlo), v_by = vs > 0.f ? vs : 1.f, v_inverse = inverse_of(v_by), vz = rintf(dbf_quotient(vlo, v_by, v_inverse));
-    if (!live) return;
+    unsigned bytes = 0;   // of four places, the group's first 4 vu
+#pragma unroll
+    for (int e = 0; e < 4; ++e) bytes |= (unsigned)fmaf(code_of(y[4 + e], v_by, v_inverse, vz), 16.f, code_of(y[e], v_by, v_inverse, vz)) << 8 * e;
+    if (TOKENS > 1 && row) {   // lane of a token: one place (two of two tokens), its tokens' bytes
+        unsigned others = 0;
+#pragma unroll
+        for (int j = 0; j < TOKENS; ++j) {
+            const unsigned w = __shfl(bytes, (lane & ~(LANES * (TOKENS - 1))) + j * LANES);
+            if constexpr (TOKENS == 4) others |= (w >> 8 * turn & 255) << 8 * j;
+            else others |= (w >> 16 * turn & 255) << 8 * j | (w >> (16 * turn + 8) & 255) << (8 * j + 16);
+        }
+        bytes = others;
+    }
+    if (!held) return;
     uint8_t* rec = a.cache + dbf_record_at(slot, head, a.n_kv, a.page_shift, D);
-    const int t = slot & 31, tile = t >> 4, g = (t >> 2) & 3, i = t & 3;
+    const int t = slot & 31;
+    auto place = [&](int slot, int l) {   // of a token's byte of the group's place l
+        return a.cache + dbf_record_at(slot, head, a.n_kv, a.page_shift, D) + 1024 * N + 1024 * vp + 16 * (16 * (slot >> 2 & 3) + l) + 4 * (2 * vq + (slot >> 4 & 1)) + (slot & 3);
+    };
     auto pack = [](const float* x, float by, float inverse, float zero) {   // four codes, 16 bits: whole numbers below 2^16 in fp32
         return (uint16_t)(unsigned)fmaf(fmaf(fmaf(code_of(x[3], by, inverse, zero), 16.f, code_of(x[2], by, inverse, zero)), 16.f, code_of(x[1], by, inverse, zero)), 16.f,
                                         code_of(x[0], by, inverse, zero));
     };
     *reinterpret_cast<uint16_t*>(rec + t * 32 * N + 2 * qa) = pack(v, sa, ia, za);
     *reinterpret_cast<uint16_t*>(rec + t * 32 * N + 2 * qb) = pack(v + 4, sb, ib, zb);
-    uint8_t* bytes = rec + 1024 * N + 1024 * vp + 16 * (16 * g + 4 * vu) + 4 * (2 * vq + tile) + i;
+    const int i0 = __builtin_amdgcn_readfirstlane(slot0 & 3);
+    if (TOKENS == 1 || !row || (TOKENS == 2 && (i0 & 1))) {
+        if (TOKENS == 2 && row) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-        bytes[16 * e] = (uint8_t)(unsigned)fmaf(code_of(y[4 + e], v_by, v_inverse, vz), 16.f, code_of(y[e], v_by, v_inverse, vz));
+            for (int e = 0; e < 2; ++e) {
+                *place(slot0, 4 * vu + 2 * turn + e) = (uint8_t)(bytes >> 16 * e);
+                *place(slot0 + 1, 4 * vu + 2 * turn + e) = (uint8_t)(bytes >> (16 * e + 8));
+            }
+        } else {
+            uint8_t* own = place(slot, 4 * vu);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) own[16 * e] = (uint8_t)(bytes >> 8 * e);
+        }
+    } else if (TOKENS == 2) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) *reinterpret_cast<uint16_t*>(place(slot0, 4 * vu + 2 * turn + e)) = (uint16_t)(bytes >> 16 * e);
+    } else {   // from i0 on in one word of four tokens, the rest in the next one
+        uint8_t *one = place(slot0, 4 * vu + turn), *next = place(slot0 + 4 - i0, 4 * vu + turn);
+        if (i0 == 0) *reinterpret_cast<unsigned*>(one) = bytes;
+        else if (i0 == 1) *one = (uint8_t)bytes, *reinterpret_cast<uint16_t*>(one + 1) = (uint16_t)(bytes >> 8), *next = (uint8_t)(bytes >> 24);
+        else if (i0 == 2) *reinterpret_cast<uint16_t*>(one) = (uint16_t)bytes, *reinterpret_cast<uint16_t*>(next) = (uint16_t)(bytes >> 16);
+        else *one = (uint8_t)bytes, *reinterpret_cast<uint16_t*>(next) = (uint16_t)(bytes >> 8), next[2] = (uint8_t)(bytes >> 24);
+    }
     dbf_h2* words = reinterpret_cast<dbf_h2*>(rec + 2048 * N);
     if (sub < N) words[32 * sub + t] = (dbf_h2){(_Float16)s_own, (_Float16)(fine ? -s_own * z_own : __builtin_nanf(""))};
     if (vq == 0 && vu == 0) words[32 * N + 32 * vp + t] = fine ? (dbf_h2){(_Float16)vs, (_Float16)(-vs * vz)} : (dbf_h2){(_Float16)0.f, (_Float16)0.f};
@@ -464,8 +506,9 @@ int launch_heads(const HeadsArgs& a, hipStream_t stream) {
     if (!a.n_tokens) return DBF_OK;
     // heads of 64, 128 and 256 values that turn by whole quads; any other by the general kernel
     const bool quads = (a.dim == 64 || a.dim == 128 || a.dim == 256) && a.rot % 8 == 0;
-    const int heads = quads ? 512 / a.dim : 1;   // of a wavefront
-    const long long items = (long long)a.n_tokens * ((a.q ? (a.n_q + heads - 1) / heads : 0) + (a.k ? (a.n_kv + heads - 1) / heads : 0)), groups = (items + WAVES - 1) / WAVES;
+    const int heads = quads ? 512 / a.dim : 1, together = quads ? tokens_together(a.dim / 64, a.cache) : 1;   // of a wavefront
+    const long long turns = ((long long)a.n_tokens + together - 1) / together;
+    const long long items = turns * ((a.q ? together * ((a.n_q + heads - 1) / heads) : 0) + (a.k ? (a.n_kv * together + heads - 1) / heads : 0)), groups = (items + WAVES - 1) / WAVES;
     if (groups > INT_MAX / WAVES) return DBF_EINVAL;
     if (!quads) hipLaunchKernelGGL(dbf_heads_kernel<T>, dim3((unsigned)groups), dim3(64 * WAVES), 0, stream, a);
     else if (a.dim == 64) launch_quads<T, 1>(a, (unsigned)groups, stream);

@@ -248,6 +248,42 @@ def test_cache_append_without_norm_is_exact(T, hq, hk, D, page, dtype, pad, offs
                     assert np.array_equal(f64(o[t, h]), x, equal_nan=True)
 
 
+@pytest.mark.parametrize("hq,hk,D,page,dtype", [(3, 3, 128, 32, "f16"), (0, 5, 64, 64, "bf16"), (2, 3, 256, 32, "f16"), (9, 1, 64, 32, "f16"), (0, 8, 128, 64, "bf16")])
+@pytest.mark.parametrize("shift", [0, 1, 2, 3])
+def test_cache_append_of_rows_of_slots(shift, hq, hk, D, page, dtype):
+    """Tokens whose slots follow each other, from any place of a word's four on, over the ends of pages, broken off by others, and backwards; and what lies
+    beside them stays."""
+    g = torch.Generator(device="cuda").manual_seed(shift + D)
+    pages = 8
+    rows = [range(shift, shift + 9), range(page - 2 + shift, page + 7), range(2 * page + 5, 2 * page + 5 + shift), [-1, 3 * page + shift], range(4 * page + 12 + shift, 4 * page + 8, -1),
+            range(6 * page - 4, 6 * page + 13 + shift), [pages * page - 1, pages * page, pages * page + 1], range(7 * page + shift, 7 * page + shift + 4)]
+    slots = [s for r in rows for s in r]
+    T = len(slots)
+    buf, row, (q, k, v) = make_heads(g, T, max(hq, 1), hk, D, dtype)
+    k[3, 0], v[5, hk - 1, 2] = 0.0, float("nan")
+    ref = S.Cache(pages, page, hk, D, fill=0x5A)
+    dev = torch.full((ref.data.size + 256,), 0x5A, dtype=torch.uint8, device="cuda")
+    kk, vv = f64(k), f64(v)
+    for t, s in enumerate(slots):
+        for h in range(hk):
+            if 0 <= s < pages * page:
+                ref.write(s, h, kk[t, h], vv[t, h])
+    qo = torch.full((T, max(hq, 1) * D), 7.0, dtype=DT[dtype][0], device="cuda")
+    cache = B.Cache(data=ptr(dev), n_pages=pages, page_tokens=page, n_kv_heads=hk, head_dim=D)
+    heads = B.Heads(q=ptr(q) if hq else 0, q_stride=row, k=ptr(k), k_stride=row, v=ptr(v), v_stride=row, q_out=ptr(qo), q_out_stride=max(hq, 1) * D, dtype=DT[dtype][1], n_tokens=T,
+                    n_q_heads=hq, n_kv_heads=hk, head_dim=D)
+    sl = ints(slots)
+    B.dbf_cache_append(heads, cache, ptr(sl), G.stream_handle())
+    torch.cuda.synchronize()
+    assert torch.equal(qo.view(T, -1, D), q) if hq else (qo == 7).all()
+    got = dev.cpu().numpy()
+    assert (got[ref.data.size:] == 0x5A).all()
+    codes = lambda d: d.reshape(-1, 36 * D)[:, : 32 * D]   # noqa: E731
+    words = lambda d: np.ascontiguousarray(d.reshape(-1, 36 * D)[:, 32 * D:]).view(np.float16)   # noqa: E731
+    assert np.array_equal(words(got[: ref.data.size]), words(ref.data), equal_nan=True)
+    assert np.array_equal(codes(got[: ref.data.size]), codes(ref.data))
+
+
 @pytest.mark.parametrize("T,hq,hk,D,page,rot,inter,dtype", [(1, 4, 4, 128, 64, 128, False, "f16"), (300, 4, 2, 128, 64, 64, True, "bf16"), (77, 0, 2, 64, 32, 64, False, "f16"),
                                                             (90, 3, 1, 256, 128, 256, True, "f16"), (50, 2, 1, 64, 32, 16, False, "bf16")])
 def test_cache_append_with_norm_and_rotation(T, hq, hk, D, page, rot, inter, dtype):
