@@ -167,7 +167,10 @@ __global__ __launch_bounds__(64 * WAVES) void dbf_heads_kernel(const HeadsArgs a
 
 // Heads of 64 N values with pairs of whole quads: a head is 8 N lanes' with two quads (four values) each, so that a pair of quads that turn into each other is one lane's, and
 // 8 / N heads a wavefront's.  Query heads come first, then the key heads (with their values, where those go to the cache); a wavefront has one kind.
-// (A wavefront to a head, values of a lane 64 apart and through LDS: 238 us for 8191 tokens of 40 heads of 128, 165 us for 2047 of 32 + 32 into the cache.)
+// Without a cache bound by the read and the write: 8191 tokens of 32 + 8 heads of 128, 170 MB in 36.5 us (4.65 TB/s; a large copy has 4.95).  (A wavefront to a head, values of a lane 64
+// apart and through LDS: 238 us.)
+// Into the cache: 2047 tokens of 32 + 32 heads of 128 in 29 us, 11 of them the queries' norms and rotation; the rest are the groups' scales and codes (about 350 instructions for 16 values of a
+// lane) and stores: codes of values written a byte at a time were 38 us, divisions and maxima as they are written in C one more.
 template <typename T>
 struct Quad {
     dbf_u2 w;
@@ -191,13 +194,17 @@ __device__ __forceinline__ float head_sum(float v) {
 }
 // The largest of values that are not negative, by their bits (as numbers a maximum makes each of its operands a quiet one first): of the lanes of a head ...
 __device__ __forceinline__ unsigned larger(unsigned v, unsigned w) { return v > w ? v : w; }
+template <int CTRL>   // (nothing stays of the register written, so that the move is part of the maximum's instruction)
+__device__ __forceinline__ unsigned moved(unsigned v) {
+    return (unsigned)__builtin_amdgcn_mov_dpp((int)v, CTRL, 0xF, 0xF, true);
+}
 template <int N>
 __device__ __forceinline__ float head_max(float x) {
     unsigned v = __builtin_bit_cast(unsigned, x);
-    v = larger(v, dbf_dpp_move<0xB1>(v));    // 1 away
-    v = larger(v, dbf_dpp_move<0x4E>(v));    // 2
-    v = larger(v, dbf_dpp_move<0x141>(v));   // 4: the other half of eight lanes, which has one value by now
-    if constexpr (N > 1) v = larger(v, dbf_dpp_move<0x128>(v));   // 8
+    v = larger(v, moved<0xB1>(v));    // 1 away
+    v = larger(v, moved<0x4E>(v));    // 2
+    v = larger(v, moved<0x141>(v));   // 4: the other half of eight lanes, which has one value by now
+    if constexpr (N > 1) v = larger(v, moved<0x128>(v));   // 8
     if constexpr (N > 2) {
         const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
         v = larger(r[0], r[1]);
@@ -208,10 +215,10 @@ __device__ __forceinline__ float head_max(float x) {
 template <int N>
 __device__ __forceinline__ float group_max(float x) {
     unsigned v = __builtin_bit_cast(unsigned, x);
-    v = larger(v, dbf_dpp_move<0xB1>(v));
-    v = larger(v, dbf_dpp_move<0x4E>(v));
-    if constexpr (N == 1) v = larger(v, dbf_dpp_move<0x141>(v));
-    if constexpr (N == 2) v = larger(v, dbf_dpp_move<0x128>(v));
+    v = larger(v, moved<0xB1>(v));
+    v = larger(v, moved<0x4E>(v));
+    if constexpr (N == 1) v = larger(v, moved<0x141>(v));
+    if constexpr (N == 2) v = larger(v, moved<0x128>(v));
     if constexpr (N == 4) {
         const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
         v = larger(r[0], r[1]);
@@ -397,13 +404,13 @@ __global__ __launch_bounds__(64 * WAVES) void dbf_heads_quads_kernel(const Heads
     };
     *reinterpret_cast<uint16_t*>(rec + t * 32 * N + 2 * qa) = pack(v, sa, ia, za);
     *reinterpret_cast<uint16_t*>(rec + t * 32 * N + 2 * qb) = pack(v + 4, sb, ib, zb);
-    const int i0 = __builtin_amdgcn_readfirstlane(slot0 & 3);
+    const int row0 = __builtin_amdgcn_readfirstlane(slot0), i0 = row0 & 3;   // (of a row it is all lanes' first)
     if (TOKENS == 1 || !row || (TOKENS == 2 && (i0 & 1))) {
         if (TOKENS == 2 && row) {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                *place(slot0, 4 * vu + 2 * turn + e) = (uint8_t)(bytes >> 16 * e);
-                *place(slot0 + 1, 4 * vu + 2 * turn + e) = (uint8_t)(bytes >> (16 * e + 8));
+                *place(row0, 4 * vu + 2 * turn + e) = (uint8_t)(bytes >> 16 * e);
+                *place(row0 + 1, 4 * vu + 2 * turn + e) = (uint8_t)(bytes >> (16 * e + 8));
             }
         } else {
             uint8_t* own = place(slot, 4 * vu);
@@ -412,9 +419,9 @@ __global__ __launch_bounds__(64 * WAVES) void dbf_heads_quads_kernel(const Heads
         }
     } else if (TOKENS == 2) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) *reinterpret_cast<uint16_t*>(place(slot0, 4 * vu + 2 * turn + e)) = (uint16_t)(bytes >> 16 * e);
+        for (int e = 0; e < 2; ++e) *reinterpret_cast<uint16_t*>(place(row0, 4 * vu + 2 * turn + e)) = (uint16_t)(bytes >> 16 * e);
     } else {   // from i0 on in one word of four tokens, the rest in the next one
-        uint8_t *one = place(slot0, 4 * vu + turn), *next = place(slot0 + 4 - i0, 4 * vu + turn);
+        uint8_t *one = place(row0, 4 * vu + turn), *next = place(row0 + 4 - i0, 4 * vu + turn);
         if (i0 == 0) *reinterpret_cast<unsigned*>(one) = bytes;
         else if (i0 == 1) *one = (uint8_t)bytes, *reinterpret_cast<uint16_t*>(one + 1) = (uint16_t)(bytes >> 8), *next = (uint8_t)(bytes >> 24);
         else if (i0 == 2) *reinterpret_cast<uint16_t*>(one) = (uint16_t)bytes, *reinterpret_cast<uint16_t*>(next) = (uint16_t)(bytes >> 16);

