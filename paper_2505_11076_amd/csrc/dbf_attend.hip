@@ -26,6 +26,7 @@ constexpr int MOST_SHARES = 1024;
 constexpr int BESIDE = 8;            // records' time that an item takes beside its records (4: batch of 64 in 88 us for 81; 12 and 16 the same)
 constexpr int TILE = 64;             // tokens of a step of many rows
 constexpr int MANY_WAVES = 4;       // wavefronts of a workgroup of many rows, 32 rows each
+constexpr int AHEAD = 4;             // operands read from LDS ahead of their products
 constexpr int LEAST_CHUNK = 512;     // tokens of a part, of many rows, at least: its first tile and the join are paid for
 constexpr int FEW = 16;              // rows (tokens times heads) of a request and key head that are few
 
@@ -513,7 +514,7 @@ __global__ __launch_bounds__(256) void dbf_attend_join_kernel(const AttendArgs a
 //            follow each other are those of a lane's 16 bytes of values in the cache.
 //   output:  V^T p^T, 32 values x 32 columns: the scores' places are the product's operand as they are, since the values' tokens are laid out in that order.
 // Both operands lie in LDS as the lanes take them, 16 bytes a lane one after the other.
-// Measured: 3 prompts of 2048 causal rows of 32 heads of 128 on 2048 .. 3001 tokens, 165 GFLOP in 205 us, 800 TFLOP/s (a large library product of fp16: 1360).  A SIMD's products take 39 %
+// Measured: 3 prompts of 2048 causal rows of 32 heads of 128 on 2048 .. 3001 tokens, 165 GFLOP in 203 us, 810 TFLOP/s (a large library product of fp16: 1360).  A SIMD's products take 39 %
 // of the time, its vector instructions 55 %, operands' reads from LDS half of what LDS gives: a product of 32 clocks takes 8 clocks of LDS for each of four SIMDs, so that products alone
 // keep it busy.  Eight wavefronts a workgroup 214 for 219 us then, and 1.5 times as long for heads of 64 and 256; tiles of 32 tokens for three wavefronts a SIMD 207 for 204; 64 rows a
 // wavefront, one a SIMD, 325 for 222; two halves of a workgroup half a step apart 222 for 211; products and vector instructions of a wavefront alternating 227 for 214.
@@ -604,16 +605,16 @@ struct Share {
     }
 };
 
-// The reads of products' operands from LDS so many products ahead of them.
-template <int PRODUCTS, int AHEAD>
-__device__ __forceinline__ void ahead() {
-    __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+// Order of a block's products and reads of operands from LDS: so many reads ahead of all products, then a read behind each product.
+template <int PRODUCTS, int READS, int AHEAD>
+__device__ __forceinline__ void in_turn() {
+    if constexpr (AHEAD > 0) __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
 #pragma unroll
-    for (int k = 0; k < PRODUCTS - AHEAD; ++k) {
+    for (int k = 0; k < READS - AHEAD; ++k) {
         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
         __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
     }
-    __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
+    __builtin_amdgcn_sched_group_barrier(0x008, PRODUCTS - (READS - AHEAD), 0);
 }
 
 __device__ __forceinline__ float both_max(float v) {   // of a lane and the one 32 on
@@ -629,7 +630,8 @@ __device__ __forceinline__ float both_sum(float v) {
 
 template <typename T, int N, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(N == 4 ? 1 : 2))) void dbf_attend_many_kernel(const AttendArgs a) {
-    constexpr int D = 64 * N;
+    // The values' first operands are under way while the weights are made: 202 -> 199 us for the prompts of 2048, 278 -> 266 for 512 rows on 30000 tokens (heads of 256 have no registers for it)
+    constexpr int D = 64 * N, EARLY = N == 4 ? 0 : AHEAD;
     __shared__ Tiles<N, WAVES> tiles;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hf = lane >> 5, G = a.group;
     // (a request's later rows see more: they come first)
@@ -712,7 +714,10 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(N ==
 #pragma unroll
                 for (int k = 0; k < 4 * N; ++k)
                     x[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(dbf_h8, tiles.k[which][b][k][lane]), q[k], x[b], 0, 0, 0);
-            ahead<8 * N, 6>();
+            dbf_h8 early[EARLY + 1];
+#pragma unroll
+            for (int n = 0; n < EARLY; ++n) early[n] = __builtin_bit_cast(dbf_h8, tiles.v[which][n % (2 * N)][n / (2 * N)][lane]);
+            in_turn<8 * N, 8 * N + EARLY, AHEAD>();
             if (first + TILE > wave_all) {
                 asm volatile("");
 #pragma unroll
@@ -755,8 +760,8 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(N ==
             for (int k = 0; k < 4; ++k)
 #pragma unroll
                 for (int j = 0; j < 2 * N; ++j)
-                    o[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(dbf_h8, tiles.v[which][j][k][lane]), __builtin_bit_cast(dbf_h8, (dbf_u4){weights[k][0], weights[k][1], weights[k][2], weights[k][3]}), o[j], 0, 0, 0);
-            ahead<8 * N, 6>();
+                    o[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(2 * N * k + j < EARLY ? early[2 * N * k + j] : __builtin_bit_cast(dbf_h8, tiles.v[which][j][k][lane]), __builtin_bit_cast(dbf_h8, (dbf_u4){weights[k][0], weights[k][1], weights[k][2], weights[k][3]}), o[j], 0, 0, 0);
+            in_turn<8 * N, 8 * N - EARLY, EARLY ? 0 : AHEAD>();
         }
         if (more) store(first + TILE, which ^ 1);
     }
