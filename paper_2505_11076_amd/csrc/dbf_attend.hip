@@ -7,6 +7,9 @@
 
 namespace {
 
+struct alignas(16) Piece {   // an item that was cut: its head (-1: it was not), shares, rows
+    int head, share, last, row0, rows, unused[3];
+};
 struct AttendArgs {
     const void* q;
     void* out;
@@ -19,7 +22,8 @@ struct AttendArgs {
     float scale;
     float *part_out, *part_stat;   // of a share's first and last piece: sums [share][2][row][head_dim], maximum and sum of the row's weights [..][2]
                                    // (many rows: [request][head][part][row])
-    int* cut;                      // [share][4]: request, head and last share of the item that begins in the share and goes on in others; -1: there is none
+    Piece* cut;                    // of each item, or of each share the item that begins in it and goes on in others
+    int by_item;
 };
 constexpr float LOWEST = -3.0e38f;   // of a running maximum: below all scores, and its difference from one is a number
 constexpr int MOST_SHARES = 1024;
@@ -417,7 +421,7 @@ DBF_FEW_KERNEL(N) void dbf_attend_shares_kernel(const AttendArgs a) {
     before *= a.n_kv;
     total *= a.n_kv;
     const long long size = (total + gridDim.x - 1) / gridDim.x, lo = share * size, hi = min(lo + size, total);
-    if (tid == 0) a.cut[4 * share] = -1;
+    if (tid == 0 && !a.by_item) a.cut[share].head = -1;
     if (lo >= total) return;
     if (lo >= before && lo < before + own * a.n_kv) {
         int i = from;
@@ -438,10 +442,10 @@ DBF_FEW_KERNEL(N) void dbf_attend_shares_kernel(const AttendArgs a) {
         const int first = (int)max(lo - item - BESIDE, 0LL), last = (int)min(hi - item - BESIDE, (long long)n);
         if (n ? last > first : item >= lo) {
             const bool whole = !n || (first == 0 && last == n);   // (an item without records is answered in the share that it begins in, also where its cost goes on in the next)
-            if (!whole && first == 0 && tid == 0) {   // it begins here
-                a.cut[4 * share] = i;
-                a.cut[4 * share + 1] = head;
-                a.cut[4 * share + 2] = (int)((item + cost - 1) / size);
+            if (tid == 0 && first == 0 && (!whole || a.by_item)) {   // it begins here
+                Piece& piece = a.cut[a.by_item ? i * a.n_kv + head : share];
+                piece.head = whole ? -1 : head;
+                piece.share = share, piece.last = (int)((item + cost - 1) / size), piece.row0 = r.row0, piece.rows = r.rows;
             }
             few_rows<T, N>(a, r, i, head, __builtin_amdgcn_readfirstlane(first), __builtin_amdgcn_readfirstlane(last), whole ? -1 : 2LL * share + (first == 0), shared);
         }
@@ -462,11 +466,10 @@ template <typename T>
 __global__ __launch_bounds__(256) void dbf_attend_join_kernel(const AttendArgs a) {
     __shared__ float keep[MOST_SHARES], total[8];
     __shared__ dbf_f4 sums[256];
-    const int tid = threadIdx.x, share = blockIdx.y, col = blockIdx.x, D = a.dim, G = a.group, per = D / 4, lanes = 256 / per;
-    const int req = a.cut[4 * share], head = a.cut[4 * share + 1], parts = a.cut[4 * share + 2] - share + 1;
-    if (req < 0) return;
-    const Request r = request(a, req);
-    if (col >= min(r.rows, a.max_q) * G) return;
+    const int tid = threadIdx.x, col = blockIdx.x, D = a.dim, G = a.group, per = D / 4, lanes = 256 / per;
+    const Piece item = a.cut[blockIdx.y];
+    const int head = item.head, share = item.share, parts = item.last - share + 1;
+    if (head < 0 || col >= item.rows * G) return;   // (rows: not more than max_q, or there were no records)
     const int d = tid % per, turn = tid / per;
     auto piece = [&](int p) { return (long long)(2 * (share + p) + (p == 0)) * FEW + col; };
     float m[MOST_SHARES / 256], l[MOST_SHARES / 256], most = LOWEST, sum = 0.f;
@@ -503,7 +506,7 @@ __global__ __launch_bounds__(256) void dbf_attend_join_kernel(const AttendArgs a
     __syncthreads();
     if (turn) return;
     for (int k = 1; k < lanes; ++k) y += sums[k * per + d];
-    T* out = static_cast<T*>(a.out) + (long long)(r.row0 + col / G) * a.out_stride + (long long)(head * G + col % G) * D + 4 * d;
+    T* out = static_cast<T*>(a.out) + (long long)(item.row0 + col / G) * a.out_stride + (long long)(head * G + col % G) * D + 4 * d;
 #pragma unroll
     for (int i = 0; i < 4; ++i) out[i] = dbf_from_float<T>(sum == 0.f ? 0.f : y[i] / sum);
 }
@@ -826,7 +829,7 @@ int check_attend(const dbf_attend* a, const dbf_cache* c) {
 // How a call is run, and what its workspace holds.
 struct Cut {
     bool few;
-    int shares;         // few rows; 0: a workgroup to an item
+    int shares, joins;  // few rows; 0: a workgroup to an item; of a join's launch, items where they are fewer than shares
     int chunk, parts;   // many rows
     size_t cut_bytes, stat_bytes, out_bytes;
 };
@@ -838,7 +841,8 @@ Cut cut_of(const dbf_attend* a, const dbf_cache* c) {
     // 2400 of 1 .. 2500 90 and 113.  (The sums over all requests and the join of cut items are 8 us.)
     if (k.few && a->max_kv > 2048 + 8LL * a->n_seq * c->n_kv_heads) {
         k.shares = 256 * few_waves(c->head_dim / 64);
-        k.cut_bytes = (size_t)k.shares * 16;
+        k.joins = (int)std::min<long long>(k.shares, (long long)a->n_seq * c->n_kv_heads);
+        k.cut_bytes = ((size_t)k.joins * sizeof(Piece) + 255) / 256 * 256;
         k.stat_bytes = (size_t)k.shares * 2 * FEW * 8;
         k.out_bytes = (size_t)k.shares * 2 * FEW * c->head_dim * 4;
     }
@@ -862,13 +866,13 @@ Cut cut_of(const dbf_attend* a, const dbf_cache* c) {
 }
 
 template <typename T, int N>
-void launch_few(const AttendArgs& a, int shares, hipStream_t stream) {
+void launch_few(const AttendArgs& a, int shares, int joins, hipStream_t stream) {
     if (!shares) {
         hipLaunchKernelGGL((dbf_attend_items_kernel<T, N>), dim3(a.n_kv, a.n_seq), dim3(256), 0, stream, a);
         return;
     }
     hipLaunchKernelGGL((dbf_attend_shares_kernel<T, N>), dim3(shares), dim3(256), 0, stream, a);
-    hipLaunchKernelGGL(dbf_attend_join_kernel<T>, dim3(a.max_q * a.group, shares), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL(dbf_attend_join_kernel<T>, dim3(a.max_q * a.group, joins), dim3(256), 0, stream, a);
 }
 template <typename T>
 bool launch_many(const AttendArgs& a, hipStream_t stream) {
@@ -884,9 +888,9 @@ template <typename T>
 int launch_attend(const AttendArgs& a, const Cut& cut, hipStream_t stream) {
     if (!cut.few) {
         if (!launch_many<T>(a, stream)) return DBF_EINVAL;
-    } else if (a.dim == 64) launch_few<T, 1>(a, cut.shares, stream);
-    else if (a.dim == 128) launch_few<T, 2>(a, cut.shares, stream);
-    else launch_few<T, 4>(a, cut.shares, stream);
+    } else if (a.dim == 64) launch_few<T, 1>(a, cut.shares, cut.joins, stream);
+    else if (a.dim == 128) launch_few<T, 2>(a, cut.shares, cut.joins, stream);
+    else launch_few<T, 4>(a, cut.shares, cut.joins, stream);
     return hipGetLastError() == hipSuccess ? DBF_OK : DBF_EHIP;
 }
 
@@ -917,11 +921,11 @@ extern "C" int dbf_cache_attend(const dbf_attend* attend, const dbf_cache* cache
     if (cut.out_bytes) {
         if (!workspace_dev || dbf_misaligned(workspace_dev, 256) || workspace_bytes < cut.cut_bytes + cut.stat_bytes + cut.out_bytes) return DBF_EWORKSPACE;
         char* at = static_cast<char*>(workspace_dev);
-        a.cut = reinterpret_cast<int*>(at);
+        a.cut = reinterpret_cast<Piece*>(at);
         a.part_stat = reinterpret_cast<float*>(at + cut.cut_bytes);
         a.part_out = reinterpret_cast<float*>(at + cut.cut_bytes + cut.stat_bytes);
     }
-    a.group = a.n_q / a.n_kv;  a.chunk = cut.chunk;  a.parts = cut.parts;
+    a.group = a.n_q / a.n_kv;  a.chunk = cut.chunk;  a.parts = cut.parts;  a.by_item = cut.joins < cut.shares;
     const auto stream = static_cast<hipStream_t>(hip_stream);
     return attend->dtype == DBF_F16 ? launch_attend<_Float16>(a, cut, stream) : launch_attend<dbf_bf16>(a, cut, stream);
 }
