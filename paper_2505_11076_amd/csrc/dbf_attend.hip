@@ -244,8 +244,8 @@ struct Columns {
 //            (nearly all) joins no lanes and touches no sums.  Rounded to fp16 for the product, times 2^7: a weight 2^-21 of the largest still has all its bits.
 //   output:  V^T p^T, 16 values of a group x 16 columns x 32 tokens, of values made exact in fp16.  (Scales on the weights instead of the values were fewer
 //            instructions, but their rounding does not cancel between c and z: values near zero lost three bits.)
-// Bound by the read of the cache, 36 bytes a value of head_dim for 32 tokens: one token over 131071 of 8 heads of 128, 151 MB in 32 us (4.7 TB/s; a large copy has 4.95), and 6 of the
-// join; 64 requests of 1 .. 8192 tokens, 327 MB in 63 and 6.  One request of 333 tokens: 7.1 us, latencies.
+// Bound by the read of the cache, 36 bytes a value of head_dim for 32 tokens: one token over 131071 of 8 heads of 128, 151 MB in 32 us (4.7 TB/s; a large copy has 4.95), and 5 of the
+// join; 64 requests of 1 .. 8192 tokens, 327 MB in 64 and 5.  One request of 333 tokens: 7.1 us, latencies.
 // A record from memory to LDS as it is, under way until vmcnt says that it is not.  (2: read once, so it need not stay in the caches: 75 -> 68 us for the batch of 64.)
 template <int N>
 __device__ __forceinline__ void fetch(const uint8_t* rec, uint8_t* to, int lane) {
@@ -460,8 +460,8 @@ DBF_FEW_KERNEL(N) void dbf_attend_shares_kernel(const AttendArgs a) {
     }
 }
 
-// The pieces of a row of an item that was cut, joined in their order: a workgroup to a row of the item that begins in a share.  How much of each piece counts is
-// made first, then all are read with many loads under way.  (6 us, a launch and four reads that wait for each other; pieces asked for before it is known how much they count: the same.)
+// The pieces of a row of an item that was cut, joined in their order: a workgroup to a row of an item, or of the item that begins in a share.  How much of each piece counts is made
+// first.  (5 us, a launch and the reads of the record, the statistics and the pieces, which wait for each other.)
 template <typename T>
 __global__ __launch_bounds__(256) void dbf_attend_join_kernel(const AttendArgs a) {
     __shared__ float keep[MOST_SHARES], total[8];
@@ -481,6 +481,12 @@ __global__ __launch_bounds__(256) void dbf_attend_join_kernel(const AttendArgs a
         l[k] = p < parts ? at[1] : 0.f;
         most = fmaxf(most, m[k]);
     }
+    const bool many = parts > 4 * lanes;   // then the first are asked for before it is known how much they count: 131071 tokens 38.5 -> 37.4 us (batch of 64, of few pieces: 69 -> 73)
+    constexpr int EARLY = 13;
+    dbf_f4 early[EARLY], y = {0.f, 0.f, 0.f, 0.f};
+    if (many)
+#pragma unroll
+        for (int k = 0; k < EARLY; ++k) early[k] = *reinterpret_cast<const dbf_f4*>(a.part_out + piece(min(turn + k * lanes, parts - 1)) * D + 4 * d);
     most = dbf_wave_max(most);
     if ((tid & 63) == 0) total[tid >> 6] = most;
     __syncthreads();
@@ -495,9 +501,16 @@ __global__ __launch_bounds__(256) void dbf_attend_join_kernel(const AttendArgs a
     if ((tid & 63) == 0) total[4 + (tid >> 6)] = sum;
     __syncthreads();
     sum = (total[4] + total[5]) + (total[6] + total[7]);
-    dbf_f4 y = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-    for (int p = turn; p < parts; p += lanes) {
+    if (many)
+#pragma unroll
+        for (int k = 0; k < EARLY; ++k) {
+            const int p = turn + k * lanes;
+            const float f = p < parts ? keep[p] : 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] = fmaf(f, p < parts ? early[k][i] : 0.f, y[i]);
+        }
+#pragma unroll 4
+    for (int p = many ? turn + EARLY * lanes : turn; p < parts; p += lanes) {
         const dbf_f4 x = *reinterpret_cast<const dbf_f4*>(a.part_out + piece(p) * D + 4 * d);
 #pragma unroll
         for (int i = 0; i < 4; ++i) y[i] = fmaf(keep[p], x[i], y[i]);
