@@ -104,10 +104,10 @@ __device__ __forceinline__ void keys_of_run(const T* x, int i, int n, int base, 
     for (int e = 0; e < RUN; ++e)
         if (at + e >= i) out(key_of(v[e], base + at + e));
 }
+typedef u64 two __attribute__((ext_vector_type(2)));
 // The n-th largest of 64 keys in LDS (0: none); 1 if there are no n.  Every wavefront for itself.  (For 256 keys 64-bit comparisons were 4 us, and a search bit by bit as much: a step of it
 // is a chain from vector compare to scalar count and back.)
 __device__ __forceinline__ u64 bound_of(const u64* keys, int n) {
-    typedef u64 two __attribute__((ext_vector_type(2)));
     const u64 own = keys[threadIdx.x & 63];
     int larger = 0;
 #pragma unroll 8
@@ -120,14 +120,20 @@ __device__ __forceinline__ u64 bound_of(const u64* keys, int n) {
     return __shfl(own, __ffsll((unsigned long long)at) - 1);
 }
 
-// The n largest of keys[0 .. count) (LDS, all different), in order, by how many are larger; out(place, key).
+// The n largest of keys[0 .. count) (LDS, all different), in order, by how many are larger; out(place, key).  (Sixteen to a step, those behind the last looked at for nothing: read one
+// by one 260 keys took 9 us.)
 template <typename Out>
 __device__ __forceinline__ void in_order(const u64* keys, int count, int n, Out out) {
     for (int i = threadIdx.x; i < count; i += THREADS) {
         const u64 own = keys[i];
         int larger = 0;
-#pragma unroll 4
-        for (int k = 0; k < count; ++k) larger += keys[k] > own;
+        for (int k = 0; k < count; k += 16) {
+            two v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = reinterpret_cast<const two*>(keys + k)[e];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) larger += (v[e >> 1][e & 1] > own) & (k + e < count);
+        }
         if (larger < n) out(larger, own);
     }
 }
@@ -135,7 +141,7 @@ __device__ __forceinline__ void in_order(const u64* keys, int count, int n, Out 
 struct Work {
     alignas(16) u64 groups[64];   // largest of four threads each
     u64 keys[THREADS];
-    u64 passed[ROOM];
+    alignas(16) u64 passed[ROOM];   // (a multiple of 16)
     int chosen[THREADS], holders, count;
     Sums sums[THREADS / 64];
 };
@@ -322,7 +328,8 @@ __global__ __launch_bounds__(THREADS) void dbf_logprobs_join_kernel(const Logpro
     const Target target(a, row, static_cast<const T*>(a.x) + row * a.stride, tid == 0);
     u64 first = 0, listed[ROOM / THREADS];
     if (a.n_top) {
-        if (tid < a.slices) first = lists[(long long)tid * a.n_top];
+        const int of_each = min(64 / a.slices, a.n_top);   // (slices <= 64)
+        if (tid < a.slices * of_each) first = lists[(long long)(tid / of_each) * a.n_top + tid % of_each];
 #pragma unroll
         for (int k = 0; k < ROOM / THREADS; ++k) listed[k] = tid + k * THREADS < a.slices * a.n_top ? lists[tid + k * THREADS] : 0;
     }
@@ -337,7 +344,7 @@ __global__ __launch_bounds__(THREADS) void dbf_logprobs_join_kernel(const Logpro
         finish(a, row, s, target, log_s);
     }
     if (!a.n_top) return;
-    // the same bound again: of slices' largest; at most n_top slices have keys that pass
+    // the same bound again: of the slices' largest, as many of each as there is room for (of the largest alone there is none for 13 slices and 20 alternatives: 4 rows of 53000 20.7 us)
     if (tid < 64) work.groups[tid] = first;
     if (tid == 0) work.count = 0;
     __syncthreads();

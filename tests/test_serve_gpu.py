@@ -678,6 +678,18 @@ def test_token_logprobs_of_awkward_rows(vocab, dtype):
     check_logprobs(x, [(7 * i) % vocab for i in range(len(rows))], min(vocab, 40), "awkward rows of %d" % vocab)
 
 
+@pytest.mark.parametrize("rows,vocab,top,dtype", [(4, 53017, 20, "f16"), (9, 12345, 64, "bf16"), (2, 26000, 40, "f32")])
+def test_token_logprobs_of_few_slices(rows, vocab, top, dtype):
+    """Fewer slices than alternatives: spread over all of them, all in the first, all in the last, and in one that ends oddly."""
+    g = torch.Generator(device="cuda").manual_seed(rows + vocab)
+    x = torch.randn(rows, vocab, generator=g, device="cuda")
+    x[0, : 2 * top] += 12
+    x[1, vocab - 70:] += 12
+    if rows > 2:
+        x[2, 4080: 4100] += 12
+    check_logprobs(x.to(DT[dtype][0]), [i * 77 % vocab for i in range(rows)], top, "%d x %d, %d alternatives" % (rows, vocab, top))
+
+
 def test_token_logprobs_strides_and_what_may_be_left_out():
     g = torch.Generator(device="cuda").manual_seed(9)
     buf = torch.randn(50 * 1300 + 7, generator=g, device="cuda").bfloat16()
