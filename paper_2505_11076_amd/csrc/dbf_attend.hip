@@ -398,54 +398,55 @@ DBF_FEW_KERNEL(N) void dbf_attend_items_kernel(const AttendArgs a) {
 template <typename T, int N>
 DBF_FEW_KERNEL(N) void dbf_attend_shares_kernel(const AttendArgs a) {
     __shared__ Shared<N> shared;
-    __shared__ long long waves[4], found_start;
-    __shared__ int found;
+    __shared__ int waves[4], found_start, found;   // (costs of a call are below 2^30)
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, share = blockIdx.x;
-    auto cost_of = [&](int i) { return (long long)records(request(a, i)) + BESIDE; };
+    auto cost_of = [&](int i) { return records(request(a, i)) + BESIDE; };
     const int run = (a.n_seq + 255) / 256, from = min(tid * run, a.n_seq), to = min(from + run, a.n_seq);
-    long long own = 0;
+    int own = 0;
     for (int i = from; i < to; ++i) own += cost_of(i);
-    long long sum = own;
+    int sum = own;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
-        const long long o = __shfl_up(sum, d);
+        const int o = __shfl_up(sum, d);
         if (lane >= d) sum += o;
     }
     if (lane == 63) waves[wave] = sum;
     __syncthreads();
-    long long before = sum - own, total = 0;
+    int before = sum - own, total = 0;
     for (int w = 0; w < 4; ++w) {
         if (w < wave) before += waves[w];
         total += waves[w];
     }
     before *= a.n_kv;
     total *= a.n_kv;
-    const long long size = (total + gridDim.x - 1) / gridDim.x, lo = share * size, hi = min(lo + size, total);
+    total = __builtin_amdgcn_readfirstlane(total);
+    const int size = (unsigned)(total + gridDim.x - 1) / gridDim.x, lo = share * size, hi = min(lo + size, total);
     if (tid == 0 && !a.by_item) a.cut[share].head = -1;
     if (lo >= total) return;
     if (lo >= before && lo < before + own * a.n_kv) {
         int i = from;
-        for (long long c = cost_of(i) * a.n_kv; lo >= before + c; c = cost_of(i) * a.n_kv) {
-            before += c;
-            ++i;
-        }
+        if (run > 1)   // (else it is the thread's one)
+            for (int c = cost_of(i) * a.n_kv; lo >= before + c; c = cost_of(i) * a.n_kv) {
+                before += c;
+                ++i;
+            }
         found = i;
         found_start = before;
     }
     __syncthreads();
     int i = __builtin_amdgcn_readfirstlane(found);
-    const long long begins = found_start;
+    const int begins = __builtin_amdgcn_readfirstlane(found_start);
     Request r = request(a, i);
-    int n = records(r), cost = n + BESIDE, head = __builtin_amdgcn_readfirstlane((int)((lo - begins) / cost));
-    long long item = begins + (long long)head * cost;   // where the item begins
+    int n = records(r), cost = n + BESIDE, head = (unsigned)(lo - begins) / (unsigned)cost;
+    int item = begins + head * cost;   // where the item begins
     while (item < hi) {
-        const int first = (int)max(lo - item - BESIDE, 0LL), last = (int)min(hi - item - BESIDE, (long long)n);
+        const int first = max(lo - item - BESIDE, 0), last = min(hi - item - BESIDE, n);
         if (n ? last > first : item >= lo) {
             const bool whole = !n || (first == 0 && last == n);   // (an item without records is answered in the share that it begins in, also where its cost goes on in the next)
             if (tid == 0 && first == 0 && (!whole || a.by_item)) {   // it begins here
                 Piece& piece = a.cut[a.by_item ? i * a.n_kv + head : share];
                 piece.head = whole ? -1 : head;
-                piece.share = share, piece.last = (int)((item + cost - 1) / size), piece.row0 = r.row0, piece.rows = r.rows;
+                piece.share = share, piece.last = (unsigned)(item + cost - 1) / (unsigned)size, piece.row0 = r.row0, piece.rows = r.rows;
             }
             few_rows<T, N>(a, r, i, head, __builtin_amdgcn_readfirstlane(first), __builtin_amdgcn_readfirstlane(last), whole ? -1 : 2LL * share + (first == 0), shared);
         }
@@ -852,9 +853,10 @@ Cut cut_of(const dbf_attend* a, const dbf_cache* c) {
     // Items are shared out where the longest may be more than a workgroup should have: 2048 tokens, and more the more items there are to fill the chip beside it.  us, an item to a
     // workgroup and shared out: 8 items of 1000 tokens 10.9 and 13.6, of 4000 29 and 17; 256 of 4000 32 and 38; 512 of 1 .. 4000 43 and 40, of 4000 52 and 62, of 1 .. 8192 78 and 69;
     // 2400 of 1 .. 2500 90 and 113.  (The sums over all requests and the join of cut items are 8 us.)
-    if (k.few && a->max_kv > 2048 + 8LL * a->n_seq * c->n_kv_heads) {
+    const long long items = (long long)a->n_seq * c->n_kv_heads;
+    if (k.few && a->max_kv > 2048 + 8 * items && items * (a->max_kv / 32 + 1 + BESIDE) < 1 << 30) {   // (and the sum of all costs fits: no memory holds more, but tables may say so)
         k.shares = 256 * few_waves(c->head_dim / 64);
-        k.joins = (int)std::min<long long>(k.shares, (long long)a->n_seq * c->n_kv_heads);
+        k.joins = (int)std::min<long long>(k.shares, items);
         k.cut_bytes = ((size_t)k.joins * sizeof(Piece) + 255) / 256 * 256;
         k.stat_bytes = (size_t)k.shares * 2 * FEW * 8;
         k.out_bytes = (size_t)k.shares * 2 * FEW * c->head_dim * 4;
