@@ -833,7 +833,7 @@ int check_attend(const dbf_attend* a, const dbf_cache* c) {
     if (!a) return DBF_EINVAL;
     if (const int bad = dbf_cache_check(c)) return bad;
     if (a->dtype != DBF_F16 && a->dtype != DBF_BF16) return DBF_EINVAL;
-    if (a->n_seq < 1 || a->n_seq > 65535 || a->n_tokens < 0 || a->max_q < 0 || a->max_kv < 0 || a->table_stride < 1) return DBF_EINVAL;
+    if (a->n_seq < 1 || a->n_seq > 65535 || a->n_tokens < 0 || a->max_q < 0 || a->max_kv < 0 || a->max_kv > 1 << 30 || a->table_stride < 1) return DBF_EINVAL;
     if (a->n_q_heads < 1 || a->n_q_heads > 65535) return DBF_EINVAL;
     if (a->n_q_heads % c->n_kv_heads) return DBF_ESHAPE;
     if (!(a->scale > -3.0e38f && a->scale < 3.0e38f)) return DBF_EINVAL;

@@ -198,6 +198,15 @@ def test_cache_attend_workspace():
         _refused(B.DBF_EWORKSPACE, B.dbf_cache_attend, _attend(**long_one), _cache(), 0, need)
 
 
+def test_cache_attend_of_the_longest():
+    """More than 2^30 tokens a request are refused, up to there offsets fit; where all requests together are more than the sums of shares hold, there are none."""
+    longest = dict(max_q=1, n_tokens=1, max_kv=1 << 30, table_stride=1 << 25)
+    _refused(B.DBF_EINVAL, B.dbf_cache_attend, _attend(**{**longest, "max_kv": (1 << 30) + 1}), _cache(), P, 1 << 30)
+    assert B.dbf_cache_attend_workspace_bytes(_attend(**{**longest, "max_kv": (1 << 30) + 1}), _cache()) == 0
+    assert B.dbf_cache_attend_workspace_bytes(_attend(**longest), _cache()) > 0
+    assert B.dbf_cache_attend_workspace_bytes(_attend(**{**longest, "n_seq": 16, "n_tokens": 16}), _cache()) == 0
+
+
 def test_token_logprobs_refusals():
     ok = [P, B.F16, 100, 4, 100, P, 5, P, P, P, P, P, 1 << 30]
     for code, at, bad in ((B.DBF_EINVAL, 0, 0), (B.DBF_EINVAL, 1, 3), (B.DBF_EINVAL, 2, 99), (B.DBF_EINVAL, 3, -1), (B.DBF_ESHAPE, 4, 0), (B.DBF_ESHAPE, 4, (1 << 24) + 1),
