@@ -244,7 +244,7 @@ struct Columns {
 //            (nearly all) joins no lanes and touches no sums.  Rounded to fp16 for the product, times 2^7: a weight 2^-21 of the largest still has all its bits.
 //   output:  V^T p^T, 16 values of a group x 16 columns x 32 tokens, of values made exact in fp16.  (Scales on the weights instead of the values were fewer
 //            instructions, but their rounding does not cancel between c and z: values near zero lost three bits.)
-// Bound by the read of the cache, 36 bytes a value of head_dim for 32 tokens: one token over 131071 of 8 heads of 128, 151 MB in 32 us (4.7 TB/s; a large copy has 4.95), and 5 of the
+// Bound by the read of the cache, 36 bytes a value of head_dim for 32 tokens: one token over 131071 of 8 heads of 128, 151 MB in 31 us (4.9 TB/s; a large copy has 4.95), and 5 of the
 // join; 64 requests of 1 .. 8192 tokens, 327 MB in 64 and 5.  One request of 333 tokens: 7.1 us, latencies.
 // A record from memory to LDS as it is, under way until vmcnt says that it is not.  (2: read once, so it need not stay in the caches: 75 -> 68 us for the batch of 64.)
 template <int N>
@@ -394,7 +394,7 @@ DBF_FEW_KERNEL(N) void dbf_attend_items_kernel(const AttendArgs a) {
 
 // An equal share of the whole call to each of as many workgroups as the chip holds at once: items lie one after the other, each its records and a constant for what it
 // costs beside them, and are cut where the shares end.  Lengths are only known here, so each workgroup makes the sums over the requests itself.  (Parts of a length chosen on the host,
-// a workgroup to each: 64 requests of 1 .. 8192 tokens 103 us at the best length, in shares 83; 131071 tokens of 8 heads 39 and 37.)
+// a workgroup to each: 64 requests of 1 .. 8192 tokens 103 us at the best length, in shares 83 then, 69 now; 131071 tokens of 8 heads 39 and 36.)
 template <typename T, int N>
 DBF_FEW_KERNEL(N) void dbf_attend_shares_kernel(const AttendArgs a) {
     __shared__ Shared<N> shared;
@@ -850,11 +850,11 @@ struct Cut {
 Cut cut_of(const dbf_attend* a, const dbf_cache* c) {
     Cut k = {};
     k.few = (long long)a->max_q * (a->n_q_heads / c->n_kv_heads) <= FEW;
-    // Items are shared out where the longest may be more than a workgroup should have: 2048 tokens, and more the more items there are to fill the chip beside it.  us, an item to a
-    // workgroup and shared out: 8 items of 1000 tokens 10.9 and 13.6, of 4000 29 and 17; 256 of 4000 32 and 38; 512 of 1 .. 4000 43 and 40, of 4000 52 and 62, of 1 .. 8192 78 and 69;
-    // 2400 of 1 .. 2500 90 and 113.  (The sums over all requests and the join of cut items are 8 us.)
+    // Items are shared out where the longest may be more than a workgroup should have: 1200 tokens, and more the more items there are to fill the chip beside it.  us, an item to a
+    // workgroup and shared out: 8 items of 1000 tokens 10.7 and 11.4, of 1500 14.1 and 12.6, of 4000 29 and 14; 64 of 2500 20 and 17; 256 of 2500 22 and 27, of 4000 32 and 37; 512 of 1 .. 4000
+    // 43 and 39, of 4000 52 and 62, of 1 .. 8192 79 and 63; 1600 of 1 .. 3000 77 and 84; 2400 of 1 .. 2500 90 and 114.
     const long long items = (long long)a->n_seq * c->n_kv_heads;
-    if (k.few && a->max_kv > 2048 + 8 * items && items * (a->max_kv / 32 + 1 + BESIDE) < 1 << 30) {   // (and the sum of all costs fits: no memory holds more, but tables may say so)
+    if (k.few && a->max_kv > 1200 + 11 * items && items * (a->max_kv / 32 + 1 + BESIDE) < 1 << 30) {   // (and the sum of all costs fits: no memory holds more, but tables may say so)
         k.shares = 256 * few_waves(c->head_dim / 64);
         k.joins = (int)std::min<long long>(k.shares, items);
         k.cut_bytes = ((size_t)k.joins * sizeof(Piece) + 255) / 256 * 256;
