@@ -61,14 +61,16 @@ __device__ __forceinline__ long long dbf_record_at(int slot, int head, int n_hea
 }
 static inline int dbf_page_shift(int page_tokens) { return page_tokens == 32 ? 5 : page_tokens == 64 ? 6 : page_tokens == 128 ? 7 : 8; }
 
-// x / by, correctly rounded, of `inverse` = 1 / by, correctly rounded: the remainder of x times it is exact and corrects it (three instructions for ten of a division).
-__device__ __forceinline__ float dbf_quotient(float x, float by, float inverse) {
-    const float near = x * inverse;
-    return fmaf(fmaf(-near, by, x), inverse, near);
-}
+// 1 / by as the sum of two fp32, and x times it: two instructions for ten of a division, and as correctly rounded where `by` has at most 7 significant bits: the sum is
+// exact to 2^-47, and no quotient by so few bits lies nearer than 2^-33 of itself to the middle of two fp32.
+struct DbfInverse {
+    float most, rest;
+};
+__device__ __forceinline__ float dbf_quotient(float x, const DbfInverse& inverse) { return fmaf(x, inverse.most, x * inverse.rest); }
 // The scale of a group whose values and zero span `range`: over 15, rounded up to 7 significant bits, and to a multiple of 2^-24.
 __device__ __forceinline__ float dbf_group_scale(float range) {
-    const unsigned bits = (__builtin_bit_cast(unsigned, dbf_quotient(range, 15.0f, 1.0f / 15.0f)) + 0x1FFFFu) & ~0x1FFFFu;
+    constexpr DbfInverse fifteenth = {1.0f / 15.0f, (float)(1.0 / 15.0 - (double)(1.0f / 15.0f))};
+    const unsigned bits = (__builtin_bit_cast(unsigned, dbf_quotient(range, fifteenth)) + 0x1FFFFu) & ~0x1FFFFu;
     return ceilf(__builtin_bit_cast(float, bits) * 16777216.0f) * (1.0f / 16777216.0f);
 }
 constexpr float DBF_CACHE_MOST = 57344.0f;   // larger values are held as this: every value held, s / 2 beyond it at most, is finite in fp16

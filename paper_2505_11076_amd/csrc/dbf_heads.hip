@@ -226,13 +226,11 @@ __device__ __forceinline__ float group_max(float x) {
     return __builtin_bit_cast(float, v);
 }
 // A value's code, as a number.  Its quotient has to be correctly rounded: a value of few bits may lie halfway between two codes.
-__device__ __forceinline__ float code_of(float x, float by, float inverse, float z) {
-    return __builtin_amdgcn_fmed3f(rintf(dbf_quotient(x, by, inverse)) + z, 0.f, 15.f);
-}
-// 1 / by of a scale, correctly rounded: one of at most 7 bits, so its product with the approximate inverse is exact in the remainder, and no inverse lies near the middle of two fp32.
-__device__ __forceinline__ float inverse_of(float by) {
-    const float near = __builtin_amdgcn_rcpf(by);
-    return fmaf(fmaf(-by, near, 1.f), near, near);
+__device__ __forceinline__ float code_of(float x, const DbfInverse& inverse, float z) { return __builtin_amdgcn_fmed3f(rintf(dbf_quotient(x, inverse)) + z, 0.f, 15.f); }
+// Of a scale (1 for 0), which has at most 7 bits: its product with the approximate inverse is exact in the remainder.
+__device__ __forceinline__ DbfInverse inverse_of(float scale) {
+    const float by = scale > 0.f ? scale : 1.f, near = __builtin_amdgcn_rcpf(by), most = fmaf(fmaf(-by, near, 1.f), near, near);
+    return {most, fmaf(-by, most, 1.f) * most};
 }
 // Values within what the cache holds; whether all are finite.  (The sum of their sizes says that nothing is to be done, nearly always.)
 __device__ __forceinline__ bool hold(float* x) {
@@ -359,14 +357,16 @@ __global__ __launch_bounds__(64 * WAVES) void dbf_heads_quads_kernel(const Heads
     float ks[N];
     float lo_a = fminf(fminf(v[0], v[1]), fminf(v[2], v[3])), hi_a = fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]));
     float lo_b = fminf(fminf(v[4], v[5]), fminf(v[6], v[7])), hi_b = fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7]));
-    float sa = 0.f, za = 0.f, ia = 0.f, sb = 0.f, zb = 0.f, ib = 0.f, s_own = 0.f, z_own = 0.f;   // scales (1 for 0), zeros, inverses
+    DbfInverse ia = {}, ib = {};
+    float za = 0.f, zb = 0.f, s_own = 0.f, z_own = 0.f;
 #pragma unroll
     for (int p = 0; p < N; ++p) {
         const float low = head_max<N>(fmaxf(fmaxf(ga == p ? -lo_a : 0.f, gb == p ? -lo_b : 0.f), 0.f)), high = head_max<N>(fmaxf(fmaxf(ga == p ? hi_a : 0.f, gb == p ? hi_b : 0.f), 0.f));
         ks[p] = dbf_group_scale(high + low);
-        const float by = ks[p] > 0.f ? ks[p] : 1.f, inverse = inverse_of(by), zero = rintf(dbf_quotient(low, by, inverse));
-        if (ga == p) sa = by, za = zero, ia = inverse;
-        if (gb == p) sb = by, zb = zero, ib = inverse;
+        const DbfInverse inverse = inverse_of(ks[p]);
+        const float zero = rintf(dbf_quotient(low, inverse));
+        if (ga == p) ia = inverse, za = zero;
+        if (gb == p) ib = inverse, zb = zero;
         if (sub == p) s_own = ks[p], z_own = zero;
     }
     // the values' group: lanes of the same vp
@@ -378,10 +378,12 @@ __global__ __launch_bounds__(64 * WAVES) void dbf_heads_quads_kernel(const Heads
     }
     vlo = group_max<N>(vlo);
     vhi = group_max<N>(vhi);
-    const float vs = dbf_group_scale(vhi + vlo), v_by = vs > 0.f ? vs : 1.f, v_inverse = inverse_of(v_by), vz = rintf(dbf_quotient(vlo, v_by, v_inverse));
+    const float vs = dbf_group_scale(vhi + vlo);
+    const DbfInverse v_inverse = inverse_of(vs);
+    const float vz = rintf(dbf_quotient(vlo, v_inverse));
     unsigned bytes = 0;   // of four places, the group's first 4 vu
 #pragma unroll
-    for (int e = 0; e < 4; ++e) bytes |= (unsigned)fmaf(code_of(y[4 + e], v_by, v_inverse, vz), 16.f, code_of(y[e], v_by, v_inverse, vz)) << 8 * e;
+    for (int e = 0; e < 4; ++e) bytes |= (unsigned)fmaf(code_of(y[4 + e], v_inverse, vz), 16.f, code_of(y[e], v_inverse, vz)) << 8 * e;
     if (TOKENS > 1 && row) {   // lane of a token: one place (two of two tokens), its tokens' bytes
         unsigned others = 0;
 #pragma unroll
@@ -398,12 +400,12 @@ __global__ __launch_bounds__(64 * WAVES) void dbf_heads_quads_kernel(const Heads
     auto place = [&](int slot, int l) {   // of a token's byte of the group's place l
         return a.cache + dbf_record_at(slot, head, a.n_kv, a.page_shift, D) + 1024 * N + 1024 * vp + 16 * (16 * (slot >> 2 & 3) + l) + 4 * (2 * vq + (slot >> 4 & 1)) + (slot & 3);
     };
-    auto pack = [](const float* x, float by, float inverse, float zero) {   // four codes, 16 bits: whole numbers below 2^16 in fp32
-        return (uint16_t)(unsigned)fmaf(fmaf(fmaf(code_of(x[3], by, inverse, zero), 16.f, code_of(x[2], by, inverse, zero)), 16.f, code_of(x[1], by, inverse, zero)), 16.f,
-                                        code_of(x[0], by, inverse, zero));
+    auto pack = [](const float* x, const DbfInverse& inverse, float zero) {   // four codes, 16 bits: whole numbers below 2^16 in fp32
+        return (uint16_t)(unsigned)fmaf(fmaf(fmaf(code_of(x[3], inverse, zero), 16.f, code_of(x[2], inverse, zero)), 16.f, code_of(x[1], inverse, zero)), 16.f,
+                                        code_of(x[0], inverse, zero));
     };
-    *reinterpret_cast<uint16_t*>(rec + t * 32 * N + 2 * qa) = pack(v, sa, ia, za);
-    *reinterpret_cast<uint16_t*>(rec + t * 32 * N + 2 * qb) = pack(v + 4, sb, ib, zb);
+    *reinterpret_cast<uint16_t*>(rec + t * 32 * N + 2 * qa) = pack(v, ia, za);
+    *reinterpret_cast<uint16_t*>(rec + t * 32 * N + 2 * qb) = pack(v + 4, ib, zb);
     const int row0 = __builtin_amdgcn_readfirstlane(slot0), i0 = row0 & 3;   // (of a row it is all lanes' first)
     if (TOKENS == 1 || !row || (TOKENS == 2 && (i0 & 1))) {
         if (TOKENS == 2 && row) {
