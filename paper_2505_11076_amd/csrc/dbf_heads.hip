@@ -169,7 +169,7 @@ __global__ __launch_bounds__(64 * WAVES) void dbf_heads_kernel(const HeadsArgs a
 // 8 / N heads a wavefront's.  Query heads come first, then the key heads (with their values, where those go to the cache); a wavefront has one kind.
 // Without a cache bound by the read and the write: 8191 tokens of 32 + 8 heads of 128, 170 MB in 36.5 us (4.65 TB/s; a large copy has 4.95).  (A wavefront to a head, values of a lane 64
 // apart and through LDS: 238 us.)
-// Into the cache: 2047 tokens of 32 + 32 heads of 128 in 29 us, 11 of them the queries' norms and rotation; the rest are the groups' scales and codes (about 350 instructions for 16 values of a
+// Into the cache: 2047 tokens of 32 + 32 heads of 128 in 29 us, 11 of them the queries' norms and rotation; the rest are the groups' scales and codes (about 400 instructions for 16 values of a
 // lane) and stores: codes of values written a byte at a time were 38 us, divisions and maxima as they are written in C one more.
 template <typename T>
 struct Quad {
