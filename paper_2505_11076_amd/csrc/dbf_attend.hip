@@ -718,6 +718,11 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(N ==
     }
     dbf_f16 o[2 * N] = {};
     float m = LOWEST, l = 0.f;
+    // A weight's exponent is one rounding of x kappa + (7 - m), so what m's own rounding lost comes into all weights alike: a factor of 2^(half a unit of m), which nothing notices unless it takes them
+    // out of fp16's range.  So once some |m| is above FAR, x is rounded to the score first, as m is: the largest is then m itself.
+    constexpr float FAR = 0x1p20f;
+    bool far = false;
+    float by = kappa;   // from what x holds to scores
     if (begin < end) store(begin, 0);
     int which = 0;
     for (int first = begin; first < end; first += TILE, which ^= 1) {
@@ -742,6 +747,13 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(N ==
 #pragma unroll
                     for (int i = 0; i < 16; ++i) x[b][i] = first + 32 * b + 16 * (i >> 2 & 1) + 8 * (i >> 3) + 4 * hf + (i & 3) < seen ? x[b][i] : -__builtin_inff();
             }
+            if (far) {
+                asm volatile("");
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[b][i] *= kappa;
+            }
             // Weights by the maximum so far, times 2^7; their sum says whether one of them is too large for fp16 or far above the others' place: then the maximum is raised and they
             // are made again, else nobody looks for it.  (Sums of the rounded weights, which the product below has: subnormal ones count here as they do there.)
             unsigned weights[4][4];
@@ -752,7 +764,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(N ==
                 for (int b = 0; b < 2; ++b)
 #pragma unroll
                     for (int i = 0; i < 16; i += (i & 1) ? 3 : 1) {
-                        const dbf_h2 w = {(_Float16)__builtin_amdgcn_exp2f(fmaf(x[b][i], kappa, from)), (_Float16)__builtin_amdgcn_exp2f(fmaf(x[b][i + 2], kappa, from))};
+                        const dbf_h2 w = {(_Float16)__builtin_amdgcn_exp2f(fmaf(x[b][i], by, from)), (_Float16)__builtin_amdgcn_exp2f(fmaf(x[b][i + 2], by, from))};
                         sum[2 * b + (i & 1)] = __builtin_amdgcn_fdot2(w, (dbf_h2){(_Float16)1.f, (_Float16)1.f}, sum[2 * b + (i & 1)], false);
                         weights[2 * b + (i >> 3)][2 * (i >> 2 & 1) + (i & 1)] = __builtin_bit_cast(unsigned, w);
                     }
@@ -765,11 +777,19 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(N ==
                 for (int b = 0; b < 2; ++b)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) most = fmaxf(most, x[b][i]);
-                const float to = fmaxf(m, both_max(most * kappa)), keep = __builtin_amdgcn_exp2f(m - to);
+                const float to = fmaxf(m, both_max(most * by)), keep = __builtin_amdgcn_exp2f(m - to);
                 m = to;
                 l *= keep;
 #pragma unroll
                 for (int j = 0; j < 2 * N; ++j) o[j] *= keep;
+                if (!far && __any(fabsf(m) > FAR && m != LOWEST)) {
+                    far = true;
+                    by = 1.f;
+#pragma unroll
+                    for (int b = 0; b < 2; ++b)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) x[b][i] *= kappa;
+                }
                 sum = weigh();
             }
             l += sum;

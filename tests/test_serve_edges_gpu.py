@@ -1,0 +1,100 @@
+"""GPU tests of what stands between the layer products at the ends of its ranges, against oracle/serve_oracle.py in 64 bits.
+
+Tolerances (u: half a unit in the last place of the output, relative, as in tests/test_serve_gpu.py):
+  attention with scores so far apart that one token has all the weight: scores are fp32, an error d = 2^-18 sum |q k| scale each.  Where the largest of a row, in 64 bits,
+      is ahead of all others by more than 2 d + 40 it is so in fp32 too and e^-40 of the rest is nothing: the row is that token's values, with the weight's rounding to fp16
+      (2^-10) and the output's (u).  Elsewhere the weights may fall to any of the tokens, but they are weights: the row lies between its tokens' values, and values
+      that are the same for all tokens come back, to the same roundings.
+  log probabilities: as there, 2^-20 (1 + |x - max| + log of the number)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import gpu_util as G
+import test_serve_gpu as T
+from oracle import serve_oracle as S
+from paper_2505_11076_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- attention: large scores ------------------------------------------------------------------------------
+
+
+def write_cache(rng, k, v, page):
+    """A cache of one request's keys and values [tokens, heads, D] (on the GPU), its table, and what it holds."""
+    n, hk, D = k.shape
+    each = -(-n // page)
+    table = rng.permutation(each + 2)[:each][None]
+    slots = T.ints([int(table[0, t // page]) * page + t % page for t in range(n)])
+    data = torch.full((S.cache_bytes(each + 2, page, hk, D),), 0xFF, dtype=torch.uint8, device="cuda")
+    cache = B.Cache(data=T.ptr(data), n_pages=each + 2, page_tokens=page, n_kv_heads=hk, head_dim=D)
+    B.dbf_cache_append(B.Heads(k=T.ptr(k), k_stride=hk * D, v=T.ptr(v), v_stride=hk * D, dtype=B.F16, n_tokens=n, n_kv_heads=hk, head_dim=D), cache, T.ptr(slots), G.stream_handle())
+    ko, vo = (torch.empty(n, hk, D, device="cuda") for _ in range(2))
+    B.dbf_cache_read(cache, T.ptr(slots), n, T.ptr(ko), T.ptr(vo), B.F32, G.stream_handle())
+    torch.cuda.synchronize()
+    return data, each + 2, table, T.f64(ko), T.f64(vo)
+
+
+def check_far_apart(out, q, k, v, dtype, scale, what):
+    """Rows of one request, causal; see the tolerances above."""
+    u, (rows, hq, D), n, hk = T.DT[dtype][2], q.shape, len(k), k.shape[1]
+    got, qq, decided = T.f64(out[:rows]).reshape(rows, hq, D), T.f64(q), 0
+    assert np.isfinite(got).all(), (what, np.argwhere(~np.isfinite(got))[:5])
+    assert (out[rows:] == 7).all()
+    for t in range(rows):
+        seen = n - rows + t + 1
+        for h in range(hq):
+            K, V = k[:seen, h * hk // hq], v[:seen, h * hk // hq]
+            x = K @ qq[t, h] * scale
+            d = 2.0 ** -18 * (np.abs(K) @ np.abs(qq[t, h])).max() * abs(scale)
+            order = np.sort(x)
+            low, high = V.min(0), V.max(0)
+            if seen == 1 or order[-1] - order[-2] > 2 * d + 40:
+                low = high = V[x.argmax()]
+                decided += 1
+            slack = (2.0 ** -10 + u) * np.abs(V).max(0) + 2.0 ** -25
+            bad = ~((got[t, h] >= low - slack) & (got[t, h] <= high + slack))
+            assert not bad.any(), (what, t, h, np.argwhere(bad)[:3], got[t, h][bad][:3], low[bad][:3], high[bad][:3])
+    G.say("%s: %d of %d rows have one token" % (what, decided, rows * hq))
+
+
+def far_keys(rng, n, hk, D):
+    """Keys of the size 2e4 and values of which the first half is 1 for all tokens."""
+    k = torch.from_numpy(rng.choice([-1.0, 1.0], (n, hk, D)) * rng.uniform(0.5, 1.0, (n, hk, D)) * 2e4).cuda().half()
+    v = torch.from_numpy(rng.uniform(0, 1, (n, hk, D))).cuda().half()
+    v[:, :, : D // 2] = 1
+    return k, v
+
+
+@pytest.mark.parametrize("power", [12, 18, 20, 22, 24, 26, 27, 28, 29, 30, 31, 33, 40, 70, 110])
+@pytest.mark.parametrize("rows,n,hq,hk,D", [(1, 300, 4, 2, 64), (3, 200, 8, 2, 128), (60, 300, 2, 1, 64), (130, 257, 2, 2, 128), (40, 150, 1, 1, 256), (20, 2500, 2, 1, 128)])
+def test_cache_attend_of_scores_far_apart(rows, n, hq, hk, D, power):
+    """Scores of about 2^power (to base 2), up to where fp32 tells none apart that lie near each other."""
+    rng = np.random.default_rng(power * 1000 + rows)
+    k, v = far_keys(rng, n, hk, D)
+    data, pages, table, kk, vv = write_cache(rng, k, v, 64)
+    q = torch.from_numpy(rng.choice([-1.0, 1.0], (rows, hq, D)) * rng.uniform(0.5, 1.0, (rows, hq, D)) * 2e4).cuda().half()
+    scale = float(np.float32(2.0 ** power / (2e4 * 2e4 * math.sqrt(D))))
+    out = T.run_attend(data, pages, table, [n], [rows], q, 64, hk, D, "f16", scale, 1)
+    check_far_apart(out, q, kk, vv, "f16", scale, "scores of 2^%d" % power)
+
+
+@pytest.mark.parametrize("rows,D", [(2, 128), (70, 128), (70, 64)])
+@pytest.mark.parametrize("falling", [False, True])
+@pytest.mark.parametrize("power", [24, 30, 34])
+def test_cache_attend_of_scores_that_grow_along_the_tokens(rows, D, falling, power):
+    """From 2^(power - 24) to 2^power, or back: tiles of ordinary scores before and behind those of very large ones."""
+    rng = np.random.default_rng(power + rows)
+    n = 900
+    k, v = far_keys(rng, n, 1, D)
+    size = torch.exp2(torch.linspace(-14, 0, n, device="cuda"))
+    k = (k.float() * (size.flip(0) if falling else size)[:, None, None]).half()
+    data, pages, table, kk, vv = write_cache(rng, k, v, 32)
+    sizes = 2.0 ** rng.uniform(-10, 0, (rows, 2, 1))
+    q = torch.from_numpy(rng.normal(size=(rows, 2, D)) * sizes * 1e4).cuda().half()
+    scale = float(np.float32(2.0 ** power / (2e4 * 2e4 * math.sqrt(D))))
+    out = T.run_attend(data, pages, table, [n], [rows], q, 32, 1, D, "f16", scale, 1)
+    check_far_apart(out, q, kk, vv, "f16", scale, "growing to 2^%d" % power)
