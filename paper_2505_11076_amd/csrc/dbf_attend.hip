@@ -304,7 +304,9 @@ __device__ __forceinline__ void few_rows(const AttendArgs& a, const Request& r, 
         }
         most = column_max(most);
         const int up = most > 0.f && most < __builtin_inff() ? 14 - __builtin_amdgcn_frexp_expf(most) : 0;
-        s.kappa = ldexpf(a.scale * 1.44269504089f, 24 - up);
+        // (no more than 2^100: sums of products are below 2^20 and, where they differ, 2^-72 apart at least, so that no score passes fp32 and those that a larger one would
+        // tell apart are 2^28 apart)
+        s.kappa = fminf(fmaxf(ldexpf(a.scale * 1.44269504089f, 24 - up), -0x1p100f), 0x1p100f);
 #pragma unroll
         for (int p = 0; p < N; ++p) {
             float sum = 0.f;
@@ -704,7 +706,8 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(N ==
         }
         most = both_max(most);
         const int up = most > 0.f && most < __builtin_inff() ? 15 - __builtin_amdgcn_frexp_expf(most) : 0;
-        kappa = fmaxf(ldexpf(fabsf(a.scale) * 1.44269504089f, -up), 0x1p-126f);   // (not 0: what is masked is -infinity times it)
+        // (not 0: what is masked is -infinity times it; no more than 2^80: sums of products are below 2^40 and, where they differ, 2^-48 apart at least, as for few rows)
+        kappa = fminf(fmaxf(ldexpf(fabsf(a.scale) * 1.44269504089f, -up), 0x1p-126f), 0x1p80f);
 #pragma unroll
         for (int k = 0; k < 4 * N; ++k) {
             float v[8];

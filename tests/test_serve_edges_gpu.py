@@ -98,3 +98,20 @@ def test_cache_attend_of_scores_that_grow_along_the_tokens(rows, D, falling, pow
     scale = float(np.float32(2.0 ** power / (2e4 * 2e4 * math.sqrt(D))))
     out = T.run_attend(data, pages, table, [n], [rows], q, 32, 1, D, "f16", scale, 1)
     check_far_apart(out, q, kk, vv, "f16", scale, "growing to 2^%d" % power)
+
+
+@pytest.mark.parametrize("size", [1e30, 1e34, 1e36, 1e38, 3e38])
+@pytest.mark.parametrize("scale", [0.125, -0.125, 3.0, 1e-30])
+@pytest.mark.parametrize("rows", [2, 50])
+def test_cache_attend_of_the_largest_queries(rows, scale, size):
+    """bfloat16 queries up to the type's largest with ordinary keys: a score may be beyond fp32, its row still is its likeliest token's."""
+    rng = np.random.default_rng(rows)
+    n, D = 120, 64
+    k = torch.from_numpy(rng.normal(size=(n, 1, D)) * 3).cuda().half()
+    v = torch.from_numpy(rng.uniform(0, 1, (n, 1, D))).cuda().half()
+    v[:, :, : D // 2] = 1
+    data, pages, table, kk, vv = write_cache(rng, k, v, 32)
+    q = torch.from_numpy(rng.uniform(-1, 1, (rows, 2, D)) * size).cuda().bfloat16()
+    scale = float(np.float32(scale))
+    out = T.run_attend(data, pages, table, [n], [rows], q, 32, 1, D, "bf16", scale, 1)
+    check_far_apart(out, q, kk, vv, "bf16", scale, "queries of %g times %g" % (size, scale))
