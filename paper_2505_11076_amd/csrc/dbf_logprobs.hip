@@ -46,7 +46,7 @@ __device__ __forceinline__ float value_of(u64 key) {
     return __builtin_bit_cast(float, (order >> 31) ? order & 0x7FFFFFFFu : ~order);
 }
 
-constexpr float LEAST = -3.402823466e38f;   // of a maximum: no finite value is below it, and -infinity less it is not a number's absence
+constexpr float LEAST = -3.402823466e38f;   // of a maximum: no finite value is below it (or above -LEAST), and -infinity less it is not a number's absence
 // A difference from the maximum, whose exponential is nothing below -104: held to what a product with nothing leaves nothing.
 __device__ __forceinline__ float below(float d) { return fmaxf(d, -200.f); }
 
@@ -243,7 +243,7 @@ __global__ __launch_bounds__(THREADS) void dbf_logprobs_kernel(const LogprobArgs
         }
         if (top > s.m + 8.f) {   // (rarely, once the first run is read)
             const Sums o = s;
-            s = join(o, (Sums){fminf(top, 3.4e38f), 0.f, 0.f});
+            s = join(o, (Sums){fminf(top, -LEAST), 0.f, 0.f});   // (of a finite row the largest is its maximum as it is)
         }
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k)
@@ -300,7 +300,7 @@ __global__ __launch_bounds__(THREADS) void dbf_logprobs_short_kernel(const Logpr
     Sums s = {LEAST, 0.f, 0.f};
     for (int i = 0; i < a.vocab; ++i) {
         const float v = dbf_to_float(x[i]);
-        s = join(s, (Sums){fminf(fmaxf(v, LEAST), 3.4e38f), v - v == 0.f ? 1.f : v == -__builtin_inff() ? 0.f : __builtin_nanf(""), 0.f});
+        s = join(s, (Sums){fminf(fmaxf(v, LEAST), -LEAST), v - v == 0.f ? 1.f : v == -__builtin_inff() ? 0.f : __builtin_nanf(""), 0.f});
     }
     const float log_s = log_of(s.s);
     finish(a, row, s, Target(a, row, x, true), log_s);

@@ -115,3 +115,37 @@ def test_cache_attend_of_the_largest_queries(rows, scale, size):
     scale = float(np.float32(scale))
     out = T.run_attend(data, pages, table, [n], [rows], q, 32, 1, D, "bf16", scale, 1)
     check_far_apart(out, q, kk, vv, "bf16", scale, "queries of %g times %g" % (size, scale))
+
+
+# ---- log probabilities -------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("vocab", [5, 8, 64, 1000, 9000, 70000])
+def test_token_logprobs_of_the_largest_logits(vocab):
+    """fp32 logits up to the type's largest are numbers like others."""
+    top = float(np.finfo(np.float32).max)
+    g = torch.Generator().manual_seed(vocab)
+    rows = []
+    for value, at in ((top, 0), (top, vocab - 1), (3.401e38, vocab // 2), (-top, 3), (-3.401e38, vocab - 2)):
+        r = torch.randn(vocab, generator=g)
+        r[at] = value
+        rows.append(r)
+    rows += [torch.full((vocab,), top), torch.full((vocab,), -top), torch.full((vocab,), 3.4015e38)]
+    r = torch.full((vocab,), top)
+    r[vocab // 2:] = -top
+    rows.append(r)
+    r = torch.full((vocab,), -math.inf)
+    r[1] = top
+    rows.append(r)
+    r = torch.randn(vocab, generator=g)
+    r[2], r[vocab // 2] = top, math.inf
+    rows.append(r)
+    x = torch.stack(rows).cuda()
+    for targets, n in (([(3 * i) % vocab for i in range(len(rows))], 20), ([0, vocab - 1, vocab // 2, 3, vocab - 2, 1, 1, 2, 0, 1, 2], 3)):
+        got, want = T.run_logprobs(x, targets, min(vocab, n)), S.token_logprobs(T.f64(x), targets, min(vocab, n))
+        assert np.array_equal(got[2], want[2])
+        per = 2.0 ** -20 * (1 + math.log(vocab))
+        for i, what in ((0, "logprob"), (1, "entropy"), (3, "alternatives")):
+            with np.errstate(over="ignore"):
+                w = want[i].astype(np.float32).astype(np.float64)   # (-max less max is -infinity in fp32)
+            T.close(got[i], w, per + 2.0 ** -20 * np.abs(np.nan_to_num(w, neginf=0)), "largest logits of %d, %s" % (vocab, what))
