@@ -425,8 +425,9 @@ int dbf_cache_read(const dbf_cache* cache, const int32_t* slots, int n_tokens, v
  *   kv_len:     device int32 [n_seq]: tokens held for the request, the new ones (its rows) among them
  *   block_table device int32 [n_seq][table_stride]: pages of a request in the order of its tokens
  *   causal:     row t of n sees the first kv_len - n + t + 1 tokens; 0: all rows see all
- *   max_q, max_kv: no request has more rows or tokens, of which 2^30 at most (they choose the launch; a request that has more of either, or a kv_len that is
- *               negative or beyond its table, comes out as no numbers in the rows below max_q; rows from max_q on are not written)
+ *   max_q, max_kv: no request has more rows or tokens, of which 2^30 at most (they choose the launch; a request that has more of either, a kv_len that is
+ *               negative or beyond its table, or rows that are not all in [0, n_tokens), comes out as no numbers in its first max_q rows that are; other rows are
+ *               not written)
  * A row that sees nothing is zero.  A page that the cache does not have makes the rows that see it no numbers.  Scores, statistics and sums are fp32;
  * probabilities are rounded to fp16 relative to a row's largest for the product with the values.
  * workspace_dev: 256-byte aligned, dbf_cache_attend_workspace_bytes(attend, cache) bytes (may be 0), which depends on dtype, n_seq,

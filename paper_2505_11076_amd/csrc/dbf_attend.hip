@@ -44,11 +44,12 @@ struct Request {
 };
 __device__ __forceinline__ Request request(const AttendArgs& a, int i) {
     Request r;
-    const long long from = a.q_start ? a.q_start[i] : i, to = a.q_start ? a.q_start[i + 1] : i + 1;
-    r.row0 = (int)min(max(from, 0LL), (long long)a.n_tokens);
-    r.rows = (int)min(max(to - r.row0, 0LL), (long long)a.n_tokens - r.row0);
+    const int from = a.q_start ? a.q_start[i] : i, to = a.q_start ? a.q_start[i + 1] : i + 1;
+    r.row0 = min(max(from, 0), a.n_tokens);
+    const int end = min(max(to, r.row0), a.n_tokens);
+    r.rows = end - r.row0;
     r.kv = a.kv_len[i];
-    r.ok = r.kv >= 0 && r.kv <= a.max_kv && r.kv <= (long long)a.table_stride << a.page_shift && r.rows <= a.max_q;
+    r.ok = r.kv >= 0 && r.kv <= a.max_kv && r.kv <= (long long)a.table_stride << a.page_shift && r.rows <= a.max_q && r.row0 == from && end == to;   // (rows cut off at the tensor's ends are others than they seem)
     return r;
 }
 

@@ -117,6 +117,40 @@ def test_cache_attend_of_the_largest_queries(rows, scale, size):
     check_far_apart(out, q, kk, vv, "bf16", scale, "queries of %g times %g" % (size, scale))
 
 
+# ---- attention: row starts --------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("few", [True, False])
+@pytest.mark.parametrize("starts,fine", [([0, 3, 6], [0, 1]), ([-2, 3, 6], [1]), ([0, 3, 8], [0]), ([0, 6, 3], [0]), ([-4, -1, 6], []), ([3, 6, 2147483647], [0]), ([-2147483648, 2, 6], [1])])
+def test_row_starts_outside_the_tensor(starts, fine, few):
+    """Starts below 0 or beyond the tokens: which token a row is would be a guess, so what such a request has of the tensor's rows comes out as no numbers, and no others."""
+    rng = np.random.default_rng(16)
+    n_rows = 6 if few else 6 * 20
+    starts = [s if abs(s) > 1000 else s * (n_rows // 6) for s in starts]
+    kv = [190, 170]
+    data, pages, table, k, v = T.make_cache(rng, kv, 32, 1, 64)
+    q = torch.from_numpy(rng.normal(size=(n_rows, 2, 64))).cuda().half()
+    out = torch.full((n_rows + 1, 2 * 64), 7.0, dtype=torch.float16, device="cuda")
+    st, kvd, tab = T.ints(starts), T.ints(kv), T.ints(table)
+    cache = B.Cache(data=T.ptr(data), n_pages=pages, page_tokens=32, n_kv_heads=1, head_dim=64)
+    a = B.Attend(q=T.ptr(q), q_stride=128, out=T.ptr(out), out_stride=128, dtype=B.F16, n_tokens=n_rows, n_seq=2, n_q_heads=2, max_q=n_rows, max_kv=190, q_start=T.ptr(st),
+                 kv_len=T.ptr(kvd), block_table=T.ptr(tab), table_stride=tab.shape[1], scale=0.1, causal=1)
+    ws = torch.empty(max(256, B.dbf_cache_attend_workspace_bytes(a, cache)), dtype=torch.uint8, device="cuda")
+    B.dbf_cache_attend(a, cache, T.ptr(ws), ws.numel(), G.stream_handle())
+    torch.cuda.synchronize()
+    got, mine = T.f64(out), np.full(n_rows + 1, 7.0)
+    for i in range(2):
+        at, end = max(starts[i], 0), min(starts[i + 1], n_rows)
+        if i in fine:
+            o, w, size = S.attend(T.f64(q[at: end]), k[i], v[i], 0.1, True)
+            T.close(got[at: end].reshape(-1, 2, 64), o, 2.0 ** -10 * w + 2.0 ** -11 * np.abs(o) + 2 * 2.0 ** -18 * size[..., None] * w, "request %d of %s" % (i, starts))
+            mine[at: end] = 0
+        elif end > at:
+            assert np.isnan(got[at: end]).all(), (i, starts)
+            mine[at: end] = 0
+    assert (got[mine == 7] == 7).all(), starts
+
+
 # ---- log probabilities -------------------------------------------------------------------------------------
 
 
