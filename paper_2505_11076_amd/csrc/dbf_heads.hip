@@ -3,6 +3,7 @@
 //
 // Norm: x w / sqrt(mean x^2 + eps); rotation: pairs (a cos - b sin, b cos + a sin).  In fp32, rounded once: to 16 bits, or to a code per value with a scale and
 // a zero per 64.
+#include <algorithm>
 #include <initializer_list>
 
 #include "dbf_cache.h"
@@ -11,6 +12,7 @@
 namespace {
 
 constexpr int WAVES = 4, MOST_DIM = 1024;
+constexpr long long MOST_ITEMS = (1LL << 23) * WAVES;   // wavefronts of a launch: of 2^32 threads or more only the remainder would run
 
 struct HeadsArgs {
     const void *q, *k, *v;
@@ -511,19 +513,29 @@ void launch_quads(const HeadsArgs& a, unsigned groups, hipStream_t stream) {
     hipLaunchKernelGGL(kernel, dim3(groups), dim3(64 * WAVES), 0, stream, a);
 }
 template <typename T>
-int launch_heads(const HeadsArgs& a, hipStream_t stream) {
-    if (!a.n_tokens) return DBF_OK;
+int launch_heads(const HeadsArgs& all, hipStream_t stream) {
     // heads of 64, 128 and 256 values that turn by whole quads; any other by the general kernel
-    const bool quads = (a.dim == 64 || a.dim == 128 || a.dim == 256) && a.rot % 8 == 0;
-    const int heads = quads ? 512 / a.dim : 1, together = quads ? tokens_together(a.dim / 64, a.cache) : 1;   // of a wavefront
-    const long long turns = ((long long)a.n_tokens + together - 1) / together;
-    const long long items = turns * ((a.q ? together * ((a.n_q + heads - 1) / heads) : 0) + (a.k ? (a.n_kv * together + heads - 1) / heads : 0)), groups = (items + WAVES - 1) / WAVES;
-    if (groups > INT_MAX / WAVES) return DBF_EINVAL;
-    if (!quads) hipLaunchKernelGGL(dbf_heads_kernel<T>, dim3((unsigned)groups), dim3(64 * WAVES), 0, stream, a);
-    else if (a.dim == 64) launch_quads<T, 1>(a, (unsigned)groups, stream);
-    else if (a.dim == 128) launch_quads<T, 2>(a, (unsigned)groups, stream);
-    else launch_quads<T, 4>(a, (unsigned)groups, stream);
-    return hipGetLastError() == hipSuccess ? DBF_OK : DBF_EHIP;
+    const bool quads = (all.dim == 64 || all.dim == 128 || all.dim == 256) && all.rot % 8 == 0;
+    const int heads = quads ? 512 / all.dim : 1, together = quads ? tokens_together(all.dim / 64, all.cache) : 1;   // of a wavefront
+    const long long per = (all.q ? together * ((all.n_q + heads - 1) / heads) : 0) + (all.k ? (all.n_kv * together + heads - 1) / heads : 0);   // items of so many tokens
+    const long long most = MOST_ITEMS / per * together;
+    for (long long t = 0; t < all.n_tokens; t += most) {
+        HeadsArgs a = all;
+        a.n_tokens = (int)std::min(most, all.n_tokens - t);
+        if (a.q) a.q = static_cast<const T*>(a.q) + t * a.q_stride, a.q_out = static_cast<T*>(a.q_out) + t * a.q_out_stride;
+        if (a.k) a.k = static_cast<const T*>(a.k) + t * a.k_stride;
+        if (a.k_out) a.k_out = static_cast<T*>(a.k_out) + t * a.k_out_stride;
+        if (a.v) a.v = static_cast<const T*>(a.v) + t * a.v_stride;
+        if (a.positions) a.positions += t;
+        if (a.slots) a.slots += t;
+        const unsigned groups = (unsigned)(((a.n_tokens + (long long)together - 1) / together * per + WAVES - 1) / WAVES);
+        if (!quads) hipLaunchKernelGGL(dbf_heads_kernel<T>, dim3(groups), dim3(64 * WAVES), 0, stream, a);
+        else if (a.dim == 64) launch_quads<T, 1>(a, groups, stream);
+        else if (a.dim == 128) launch_quads<T, 2>(a, groups, stream);
+        else launch_quads<T, 4>(a, groups, stream);
+        if (hipGetLastError() != hipSuccess) return DBF_EHIP;
+    }
+    return DBF_OK;
 }
 
 int launch_heads(const HeadsArgs& a, int dtype, hipStream_t stream) {
@@ -533,12 +545,15 @@ int launch_heads(const HeadsArgs& a, int dtype, hipStream_t stream) {
 template <typename T>
 int launch_read(const dbf_cache* c, const int32_t* slots, int n_tokens, void* k_out, void* v_out, hipStream_t stream) {
     const int heads = 512 / c->head_dim;   // of a wavefront
-    const long long groups = ((long long)n_tokens * ((c->n_kv_heads + heads - 1) / heads) + WAVES - 1) / WAVES;
-    if (groups > INT_MAX / WAVES) return DBF_EINVAL;
+    const long long steps = (c->n_kv_heads + heads - 1) / heads, most = MOST_ITEMS / steps, row = (long long)c->n_kv_heads * c->head_dim;
     const auto kernel = c->head_dim == 64 ? dbf_cache_read_kernel<T, 1> : c->head_dim == 128 ? dbf_cache_read_kernel<T, 2> : dbf_cache_read_kernel<T, 4>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(64 * WAVES), 0, stream, static_cast<const uint8_t*>(c->data), slots, n_tokens, c->n_pages * c->page_tokens, c->n_kv_heads,
-                       dbf_page_shift(c->page_tokens), static_cast<T*>(k_out), static_cast<T*>(v_out));
-    return hipGetLastError() == hipSuccess ? DBF_OK : DBF_EHIP;
+    for (long long t = 0; t < n_tokens; t += most) {
+        const int n = (int)std::min(most, n_tokens - t);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((n * steps + WAVES - 1) / WAVES)), dim3(64 * WAVES), 0, stream, static_cast<const uint8_t*>(c->data), slots + t, n, c->n_pages * c->page_tokens,
+                           c->n_kv_heads, dbf_page_shift(c->page_tokens), static_cast<T*>(k_out) + t * row, static_cast<T*>(v_out) + t * row);
+        if (hipGetLastError() != hipSuccess) return DBF_EHIP;
+    }
+    return DBF_OK;
 }
 
 }  // namespace

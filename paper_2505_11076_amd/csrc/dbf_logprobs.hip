@@ -377,18 +377,23 @@ Room room_of(int n_rows, int vocab, int n_top) {
 }
 
 template <typename T>
-int launch(const LogprobArgs& a, hipStream_t stream) {
-    if (a.vocab < RUN) {
-        hipLaunchKernelGGL(dbf_logprobs_short_kernel<T>, dim3((a.n_rows + THREADS - 1) / THREADS), dim3(THREADS), 0, stream, a);
-        return hipGetLastError() == hipSuccess ? DBF_OK : DBF_EHIP;
+int launch(const LogprobArgs& all, hipStream_t stream) {
+    constexpr long long MOST_ROWS = 1 << 23;   // of a launch: of 2^32 threads or more only the remainder would run (more than one slice have only fewer rows)
+    for (long long row = 0; row < all.n_rows; row += MOST_ROWS) {
+        LogprobArgs a = all;
+        a.n_rows = (int)std::min(MOST_ROWS, all.n_rows - row);
+        a.x = static_cast<const T*>(a.x) + row * a.stride;
+        if (a.targets) a.targets += row, a.logprob += row;
+        if (a.entropy) a.entropy += row;
+        if (a.n_top) a.top_ids += row * a.n_top, a.top_logprobs += row * a.n_top;
+        const dim3 grid((unsigned)(a.slices * a.n_rows)), threads(THREADS);
+        if (a.vocab < RUN) hipLaunchKernelGGL(dbf_logprobs_short_kernel<T>, dim3((a.n_rows + THREADS - 1) / THREADS), threads, 0, stream, a);
+        else if (a.n_top) hipLaunchKernelGGL((dbf_logprobs_kernel<T, true>), grid, threads, 0, stream, a);
+        else hipLaunchKernelGGL((dbf_logprobs_kernel<T, false>), grid, threads, 0, stream, a);
+        if (a.slices > 1) hipLaunchKernelGGL(dbf_logprobs_join_kernel<T>, dim3(a.n_rows), threads, 0, stream, a);
+        if (hipGetLastError() != hipSuccess) return DBF_EHIP;
     }
-    const long long groups = (long long)a.slices * a.n_rows;
-    if (groups > INT_MAX) return DBF_EINVAL;
-    const dim3 grid((unsigned)groups), threads(THREADS);
-    if (a.n_top) hipLaunchKernelGGL((dbf_logprobs_kernel<T, true>), grid, threads, 0, stream, a);
-    else hipLaunchKernelGGL((dbf_logprobs_kernel<T, false>), grid, threads, 0, stream, a);
-    if (a.slices > 1) hipLaunchKernelGGL(dbf_logprobs_join_kernel<T>, dim3(a.n_rows), threads, 0, stream, a);
-    return hipGetLastError() == hipSuccess ? DBF_OK : DBF_EHIP;
+    return DBF_OK;
 }
 
 }  // namespace

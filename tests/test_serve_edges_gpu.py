@@ -183,3 +183,58 @@ def test_token_logprobs_of_the_largest_logits(vocab):
             with np.errstate(over="ignore"):
                 w = want[i].astype(np.float32).astype(np.float64)   # (-max less max is -infinity in fp32)
             T.close(got[i], w, per + 2.0 ** -20 * np.abs(np.nan_to_num(w, neginf=0)), "largest logits of %d, %s" % (vocab, what))
+
+
+# ---- calls of more threads than a launch takes ---------------------------------------------------------------
+
+
+def test_calls_of_more_rows_than_a_launch_takes():
+    """A launch takes fewer than 2^32 threads."""
+    n = (1 << 24) + 5
+    x = torch.empty(n, 8, dtype=torch.float16, device="cuda").normal_()
+    lp, h = (torch.full((n + 1,), 7.0, device="cuda") for _ in range(2))
+    t = torch.randint(0, 8, (n,), device="cuda", dtype=torch.int32)
+    ids, tops = torch.full((n + 1, 2), 77, dtype=torch.int32, device="cuda"), torch.full((n + 1, 2), 7.0, device="cuda")
+    B.dbf_token_logprobs(T.ptr(x), B.F16, 8, n, 8, T.ptr(t), 2, T.ptr(lp), T.ptr(h), T.ptr(ids), T.ptr(tops), 0, 0, G.stream_handle())
+    torch.cuda.synchronize()
+    want = torch.log_softmax(x.double(), 1)
+    assert float((lp[:n] - want.gather(1, t.long()[:, None])[:, 0]).abs().max()) <= 2.0 ** -20 * 40
+    assert float((h[:n] + (want.exp() * want).sum(1)).abs().max()) <= 2.0 ** -20 * 40
+    best = want.sort(dim=1, descending=True, stable=True)
+    assert torch.equal(ids[:n].long(), best.indices[:, :2]) and float((tops[:n] - best.values[:, :2]).abs().max()) <= 2.0 ** -20 * 40
+    assert lp[n] == 7 and h[n] == 7 and (ids[n] == 77).all() and (tops[n] == 7).all()
+
+
+@pytest.mark.parametrize("D", [2, 64])
+def test_heads_of_more_tokens_than_a_launch_takes(D):
+    """(a token's head is a wavefront's)"""
+    n, heads = (1 << 26) + 9, 1
+    q = torch.empty(n, heads * D, dtype=torch.float16, device="cuda")
+    q.view(torch.int16).random_(0, 1 << 14)
+    out = torch.full((n + 1, heads * D), 7.0, dtype=torch.float16, device="cuda")
+    pos = torch.arange(n, device="cuda", dtype=torch.int32) % 4
+    rope = torch.tensor([[1.0] * (D // 2) + [0.0] * (D // 2), [0.0] * (D // 2) + [1.0] * (D // 2)] * 2, device="cuda")   # as it is, a quarter of a turn, ...
+    B.dbf_qk_norm_rope(B.Heads(q=T.ptr(q), q_stride=heads * D, q_out=T.ptr(out), q_out_stride=heads * D, dtype=B.F16, n_tokens=n, n_q_heads=heads, head_dim=D, rope=T.ptr(rope),
+                               rope_len=4, rot_dim=D, positions=T.ptr(pos)), G.stream_handle())
+    torch.cuda.synchronize()
+    x, y = q.view(n, heads, D), out[:n].view(n, heads, D)
+    assert torch.equal(y[0::2], x[0::2])
+    assert torch.equal(y[1::2, :, : D // 2], -x[1::2, :, D // 2:]) and torch.equal(y[1::2, :, D // 2:], x[1::2, :, : D // 2])
+    assert (out[n] == 7).all()
+
+
+def test_a_cache_read_of_more_tokens_than_a_launch_takes():
+    n = (1 << 26) + 3
+    rng = np.random.default_rng(1)
+    data = torch.empty(S.cache_bytes(1, 32, 1, 64), dtype=torch.uint8, device="cuda")
+    cache = B.Cache(data=T.ptr(data), n_pages=1, page_tokens=32, n_kv_heads=1, head_dim=64)
+    k, v = (torch.from_numpy(rng.normal(size=(32, 64))).cuda().half() for _ in range(2))
+    slots = torch.arange(n, device="cuda", dtype=torch.int32) % 33
+    B.dbf_cache_append(B.Heads(k=T.ptr(k), k_stride=64, v=T.ptr(v), v_stride=64, dtype=B.F16, n_tokens=32, n_kv_heads=1, head_dim=64), cache, T.ptr(slots), G.stream_handle())
+    ko, vo = (torch.full((n + 1, 64), 7.0, dtype=torch.float16, device="cuda") for _ in range(2))
+    B.dbf_cache_read(cache, T.ptr(slots), n, T.ptr(ko), T.ptr(vo), B.F16, G.stream_handle())
+    torch.cuda.synchronize()
+    for o in (ko, vo):
+        assert (o[n] == 7).all() and (o[32] == 0).all() and (o[:32] != 7).all()
+        whole = (n // 33) * 33
+        assert torch.equal(o[:whole].view(-1, 33, 64), o[:33].expand(whole // 33, 33, 64)) and torch.equal(o[whole: n], o[: n - whole])
