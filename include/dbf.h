@@ -431,7 +431,7 @@ int dbf_cache_read(const dbf_cache* cache, const int32_t* slots, int n_tokens, v
  * A row that sees nothing is zero.  A page that the cache does not have makes the rows that see it no numbers.  Scores, statistics and sums are fp32;
  * probabilities are rounded to fp16 relative to a row's largest for the product with the values.
  * workspace_dev: 256-byte aligned, dbf_cache_attend_workspace_bytes(attend, cache) bytes (may be 0), which depends on dtype, n_seq,
- * n_q_heads, max_q, max_kv and the cache's sizes only; contents need not be anything.
+ * n_q_heads, max_q, max_kv and the cache's sizes only (no pointer has to be set for it, the cache's neither); contents need not be anything.
  * Errors: DBF_EINVAL, DBF_ESHAPE (head_dim, heads that do not divide), DBF_EWORKSPACE, DBF_EHIP. */
 typedef struct dbf_attend {
     const void* q;

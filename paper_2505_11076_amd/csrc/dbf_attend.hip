@@ -853,9 +853,9 @@ __global__ __launch_bounds__(256) void dbf_attend_parts_kernel(const AttendArgs 
     for (int i = 0; i < 4; ++i) out[i] = dbf_from_float<T>(l == 0.f ? 0.f : y[i] / l);
 }
 
-int check_attend(const dbf_attend* a, const dbf_cache* c) {
+int check_attend(const dbf_attend* a, const dbf_cache* c) {   // (sizes: a workspace may be asked for before there are pointers)
     if (!a) return DBF_EINVAL;
-    if (const int bad = dbf_cache_check(c)) return bad;
+    if (const int bad = dbf_cache_check_sizes(c)) return bad;
     if (a->dtype != DBF_F16 && a->dtype != DBF_BF16) return DBF_EINVAL;
     if (a->n_seq < 1 || a->n_seq > 65535 || a->n_tokens < 0 || a->max_q < 0 || a->max_kv < 0 || a->max_kv > 1 << 30 || a->table_stride < 1) return DBF_EINVAL;
     if (a->n_q_heads < 1 || a->n_q_heads > 65535) return DBF_EINVAL;
@@ -942,6 +942,7 @@ extern "C" size_t dbf_cache_attend_workspace_bytes(const dbf_attend* attend, con
 }
 
 extern "C" int dbf_cache_attend(const dbf_attend* attend, const dbf_cache* cache, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+    if (const int bad = dbf_cache_check(cache)) return bad;
     if (const int bad = check_attend(attend, cache)) return bad;
     const long long row = (long long)attend->n_q_heads * cache->head_dim;
     if (!attend->q || !attend->out || !attend->kv_len || !attend->block_table || attend->q_stride < row || attend->out_stride < row) return DBF_EINVAL;

@@ -45,11 +45,15 @@ static inline bool dbf_cache_shape_ok(int n_pages, int page_tokens, int n_kv_hea
     if (head_dim != 64 && head_dim != 128 && head_dim != 256) return false;
     return (long long)n_pages * page_tokens <= INT_MAX;   // (slots are 32-bit)
 }
-// DBF_OK, or what is wrong with it
-static inline int dbf_cache_check(const dbf_cache* c) {
-    if (!c || !c->data || (reinterpret_cast<uintptr_t>(c->data) & 15)) return DBF_EINVAL;
+// DBF_OK, or what is wrong with its sizes, or with it
+static inline int dbf_cache_check_sizes(const dbf_cache* c) {
+    if (!c) return DBF_EINVAL;
     if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return DBF_ESHAPE;
     return dbf_cache_shape_ok(c->n_pages, c->page_tokens, c->n_kv_heads, c->head_dim) ? DBF_OK : DBF_EINVAL;
+}
+static inline int dbf_cache_check(const dbf_cache* c) {
+    if (!c || !c->data || (reinterpret_cast<uintptr_t>(c->data) & 15)) return DBF_EINVAL;
+    return dbf_cache_check_sizes(c);
 }
 static inline bool dbf_misaligned(const void* p, unsigned a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
 
