@@ -432,7 +432,8 @@ int dbf_cache_read(const dbf_cache* cache, const int32_t* slots, int n_tokens, v
  * probabilities are rounded to fp16 relative to a row's largest for the product with the values.
  * workspace_dev: 256-byte aligned, dbf_cache_attend_workspace_bytes(attend, cache) bytes (may be 0), which depends on dtype, n_seq,
  * n_q_heads, max_q, max_kv and the cache's sizes only (no pointer has to be set for it, the cache's neither); contents need not be anything.
- * Errors: DBF_EINVAL, DBF_ESHAPE (head_dim, heads that do not divide), DBF_EWORKSPACE, DBF_EHIP. */
+ * Errors: DBF_EINVAL (also n_seq above 65535, and max_q * n_q_heads / n_kv_heads above 65535 * 128), DBF_ESHAPE (head_dim, heads that do not divide),
+ * DBF_EWORKSPACE, DBF_EHIP. */
 typedef struct dbf_attend {
     const void* q;
     void* out;

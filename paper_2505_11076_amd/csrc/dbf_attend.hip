@@ -30,6 +30,7 @@ constexpr int MOST_SHARES = 1024;
 constexpr int BESIDE = 8;            // records' time that an item takes beside its records (4: batch of 64 in 88 us for 81; 12 and 16 the same)
 constexpr int TILE = 64;             // tokens of a step of many rows
 constexpr int MANY_WAVES = 4;       // wavefronts of a workgroup of many rows, 32 rows each
+constexpr long long MOST_ROWS = 65535LL * 32 * MANY_WAVES;   // of a request and key head: a launch's third dimension
 constexpr int AHEAD = 4;             // operands read from LDS ahead of their products
 constexpr int LEAST_CHUNK = 512;     // tokens of a part, of many rows, at least: its first tile and the join are paid for
 constexpr int FEW = 16;              // rows (tokens times heads) of a request and key head that are few
@@ -860,6 +861,7 @@ int check_attend(const dbf_attend* a, const dbf_cache* c) {   // (sizes: a works
     if (a->n_seq < 1 || a->n_seq > 65535 || a->n_tokens < 0 || a->max_q < 0 || a->max_kv < 0 || a->max_kv > 1 << 30 || a->table_stride < 1) return DBF_EINVAL;
     if (a->n_q_heads < 1 || a->n_q_heads > 65535) return DBF_EINVAL;
     if (a->n_q_heads % c->n_kv_heads) return DBF_ESHAPE;
+    if ((long long)a->max_q * (a->n_q_heads / c->n_kv_heads) > MOST_ROWS) return DBF_EINVAL;
     if (!(a->scale > -3.0e38f && a->scale < 3.0e38f)) return DBF_EINVAL;
     return DBF_OK;
 }
@@ -914,20 +916,17 @@ void launch_few(const AttendArgs& a, int shares, int joins, hipStream_t stream) 
     hipLaunchKernelGGL(dbf_attend_join_kernel<T>, dim3(a.max_q * a.group, joins), dim3(256), 0, stream, a);
 }
 template <typename T>
-bool launch_many(const AttendArgs& a, hipStream_t stream) {
-    const long long rows = (long long)a.max_q * a.group, blocks = (rows + 32 * MANY_WAVES - 1) / (32 * MANY_WAVES), across = (long long)a.n_kv * a.parts;
-    if (blocks > 65535 || across > INT_MAX || rows > INT_MAX) return false;
+void launch_many(const AttendArgs& a, hipStream_t stream) {
+    const int rows = a.max_q * a.group, blocks = (rows + 32 * MANY_WAVES - 1) / (32 * MANY_WAVES), across = a.n_kv * a.parts;   // (parts: one where the blocks of all heads are 512)
     const auto kernel = a.dim == 64 ? dbf_attend_many_kernel<T, 1, MANY_WAVES> : a.dim == 128 ? dbf_attend_many_kernel<T, 2, MANY_WAVES> : dbf_attend_many_kernel<T, 4, MANY_WAVES>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)across, a.n_seq, (unsigned)blocks), dim3(64 * MANY_WAVES), 0, stream, a);
     const int of = 256 / (a.dim / 4);
     if (a.parts > 1) hipLaunchKernelGGL(dbf_attend_parts_kernel<T>, dim3((unsigned)((rows + of - 1) / of), a.n_kv, a.n_seq), dim3(256), 0, stream, a);
-    return true;
 }
 template <typename T>
 int launch_attend(const AttendArgs& a, const Cut& cut, hipStream_t stream) {
-    if (!cut.few) {
-        if (!launch_many<T>(a, stream)) return DBF_EINVAL;
-    } else if (a.dim == 64) launch_few<T, 1>(a, cut.shares, cut.joins, stream);
+    if (!cut.few) launch_many<T>(a, stream);
+    else if (a.dim == 64) launch_few<T, 1>(a, cut.shares, cut.joins, stream);
     else if (a.dim == 128) launch_few<T, 2>(a, cut.shares, cut.joins, stream);
     else launch_few<T, 4>(a, cut.shares, cut.joins, stream);
     return hipGetLastError() == hipSuccess ? DBF_OK : DBF_EHIP;

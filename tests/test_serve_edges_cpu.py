@@ -15,3 +15,14 @@ def test_a_workspace_is_sized_before_there_is_a_cache(kw):
     for bad in (dict(n_pages=0), dict(page_tokens=40), dict(n_kv_heads=0), dict(head_dim=96)):
         assert B.dbf_cache_attend_workspace_bytes(T._attend(**kw), T._cache(data=0, **bad)) == 0
     T._refused(B.DBF_EINVAL, B.dbf_cache_attend, T._attend(**kw), T._cache(data=0), T.P, 1 << 40)
+
+
+def test_more_rows_of_a_request_than_a_launch_takes_are_refused():
+    most = 65535 * 128
+    for hq in (4, 256):
+        rows = most // (hq // 2)
+        kw = dict(n_q_heads=hq, q_stride=hq * 64, out_stride=hq * 64, n_tokens=0)
+        B.dbf_cache_attend(T._attend(**kw, max_q=rows), T._cache(), T.P, 1 << 40)   # (no tokens: nothing to do)
+        for n in (0, rows + 1):
+            T._refused(B.DBF_EINVAL, B.dbf_cache_attend, T._attend(**{**kw, "n_tokens": n}, max_q=rows + 1), T._cache(), T.P, 1 << 40)
+        assert B.dbf_cache_attend_workspace_bytes(T._attend(**kw, max_q=rows + 1, max_kv=100000, table_stride=4000), T._cache()) == 0
