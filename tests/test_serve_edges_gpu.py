@@ -151,6 +151,39 @@ def test_row_starts_outside_the_tensor(starts, fine, few):
     assert (got[mine == 7] == 7).all(), starts
 
 
+# ---- attention: more items than shares ---------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("D,n,dtype,hq", [(256, 300, "f16", 2), (256, 260, "bf16", 6), (128, 400, "f16", 8), (64, 520, "bf16", 2)])
+def test_cache_attend_of_more_items_than_shares(D, n, dtype, hq):
+    """Shared out where there are at least as many items as workgroups (a record is kept for each share, not for each item): requests mostly short, some empty, some without rows,
+    some longer than a share, one much longer."""
+    rng = np.random.default_rng(D + n)
+    hk, page = 2, 32
+    shares = {64: 1024, 128: 768, 256: 512}[D]
+    longest = 1200 + 11 * n * hk + 700
+    assert n * hk >= shares
+    kv = [int(x) for x in rng.choice([0, 1, 31, 32, 33, 64, 90, 500, 1111], n, p=[0.1, 0.1, 0.1, 0.1, 0.1, 0.2, 0.2, 0.07, 0.03])]
+    kv[n // 3], kv[n - 1] = longest, 2222
+    q_len = [int(x) for x in rng.choice([0, 1, 2], n, p=[0.1, 0.8, 0.1])]
+    q_len[n // 3] = q_len[n - 1] = 1
+    data, pages, table, k, v = T.make_cache(rng, kv, page, hk, D)
+    q = torch.from_numpy(rng.normal(size=(sum(q_len), hq, D))).cuda().to(T.DT[dtype][0])
+    a = B.Attend(dtype=T.DT[dtype][1], n_tokens=len(q), n_seq=n, n_q_heads=hq, max_q=2, max_kv=longest, table_stride=table.shape[1], scale=0.1, causal=1)
+    assert B.dbf_cache_attend_workspace_bytes(a, B.Cache(data=T.ptr(data), n_pages=pages, page_tokens=page, n_kv_heads=hk, head_dim=D)) > 0
+    out = T.run_attend(data, pages, table, kv, q_len, q, page, hk, D, dtype, 1 / math.sqrt(D), 1)
+    u, got, qq, at, worst = T.DT[dtype][2], T.f64(out[:-1]).reshape(-1, hq, D), T.f64(q), 0, 0.0
+    for i, m in enumerate(q_len):
+        o, w, size = S.attend(qq[at: at + m], k[i], v[i], 1 / math.sqrt(D), True)
+        bound = 2.0 ** -10 * w + u * np.abs(o) + 2 * 2.0 ** -18 * size[..., None] * w + 2.0 ** -25
+        off = np.abs(got[at: at + m] - o)
+        assert (off <= bound).all(), (i, kv[i], m)
+        worst = max(worst, float((off / bound).max(initial=0)))
+        at += m
+    G.say("%d items on %d shares: worst %.3g of its bound" % (n * hk, shares, worst))
+    assert (out[-1] == 7).all()
+
+
 # ---- log probabilities -------------------------------------------------------------------------------------
 
 
