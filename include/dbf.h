@@ -375,7 +375,9 @@ size_t dbf_cache_bytes(int n_pages, int page_tokens, int n_kv_heads, int head_di
  *   kv_len   [n_seq]: cached + new         positions [max_tokens]: each new token's place in its request
  *   slots    [max_tokens]: its slot in the cache; -1 where free_pages or the table has no page for it
  *   status   [2]: pages taken; pages that were missing
- * Entries of positions and slots behind the last token are 0 and -1 (tokens beyond max_tokens get none).  All arrays are device
+ * Entries of positions and slots behind the last token are 0 and -1.  Tokens beyond max_tokens get none, and pages that begin with such a token are
+ * counted in status but not entered in the table: where q_start[n_seq] is more than max_tokens, call again with room for all, on the same
+ * lengths, free pages and table.  All arrays are device
  * int32, 4-byte aligned; free_pages may be NULL if n_free is 0, positions and slots if max_tokens is 0.
  * Errors: DBF_EINVAL (null, misaligned, n_seq < 1 or > DBF_MAX_DIM, n_free or max_tokens < 0, table_stride < 1, page_tokens), DBF_EHIP. */
 int dbf_block_tables(const int32_t* cached_len, const int32_t* new_len, int n_seq, int page_tokens, const int32_t* free_pages, int n_free,
@@ -425,9 +427,9 @@ int dbf_cache_read(const dbf_cache* cache, const int32_t* slots, int n_tokens, v
  *   kv_len:     device int32 [n_seq]: tokens held for the request, the new ones (its rows) among them
  *   block_table device int32 [n_seq][table_stride]: pages of a request in the order of its tokens
  *   causal:     row t of n sees the first kv_len - n + t + 1 tokens; 0: all rows see all
- *   max_q, max_kv: no request has more rows or tokens, of which 2^30 at most (they choose the launch; a request that has more of either, a kv_len that is
- *               negative or beyond its table, or rows that are not all in [0, n_tokens), comes out as no numbers in its first max_q rows that are; other rows are
- *               not written)
+ *   max_q, max_kv: no request has more rows or tokens, of which 2^30 at most; a request that has more of either, a kv_len that is negative or beyond its
+ *               table, or rows that are not all in [0, n_tokens), comes out as no numbers in its first max_q rows that are, and other rows are not written.
+ *               They choose one form for all requests: single tokens beside long prompts are faster in a call of their own
  * A row that sees nothing is zero.  A page that the cache does not have makes the rows that see it no numbers.  Scores, statistics and sums are fp32;
  * probabilities are rounded to fp16 relative to a row's largest for the product with the values.
  * workspace_dev: 256-byte aligned, dbf_cache_attend_workspace_bytes(attend, cache) bytes (may be 0), which depends on dtype, n_seq,

@@ -246,8 +246,10 @@ struct Columns {
 //            (nearly all) joins no lanes and touches no sums.  Rounded to fp16 for the product, times 2^7: a weight 2^-21 of the largest still has all its bits.
 //   output:  V^T p^T, 16 values of a group x 16 columns x 32 tokens, of values made exact in fp16.  (Scales on the weights instead of the values were fewer
 //            instructions, but their rounding does not cancel between c and z: values near zero lost three bits.)
-// Bound by the read of the cache, 36 bytes a value of head_dim for 32 tokens: one token over 131071 of 8 heads of 128, 151 MB in 31 us (4.9 TB/s; a large copy has 4.95), and 5 of the
-// join; 64 requests of 1 .. 8192 tokens, 327 MB in 64 and 5.  One request of 333 tokens: 7.1 us, latencies.
+// The sum of the weights is of the unrounded ones, which costs what that of the rounded ones would; many rows have the latter from a dot product of two.  Each is within a rounding of the other.
+// It has the cache to read, 36 bytes a value of head_dim for 32 tokens: one token over 131071 of 8 heads of 128, 151 MB in 31 us (4.9 TB/s), and 5 of the join; 64 requests of 1 .. 8192 tokens, 327 MB
+// in 64 (5.1) and 5.  A read of as many bytes and nothing else has 24 and 50 us (6.3 and 6.6 TB/s): between them lie the vector instructions, 66 and 70 % of the time, and waits for their issue.
+// One request of 333 tokens: 7.1 us, latencies.
 // A record from memory to LDS as it is, under way until vmcnt says that it is not.  (2: read once, so it need not stay in the caches: 75 -> 68 us for the batch of 64.)
 template <int N>
 __device__ __forceinline__ void fetch(const uint8_t* rec, uint8_t* to, int lane) {
@@ -487,7 +489,7 @@ __global__ __launch_bounds__(256) void dbf_attend_join_kernel(const AttendArgs a
         most = fmaxf(most, m[k]);
     }
     const bool many = parts > 4 * lanes;   // then the first are asked for before it is known how much they count: 131071 tokens 38.5 -> 37.4 us (batch of 64, of few pieces: 69 -> 73)
-    constexpr int EARLY = 13;
+    constexpr int EARLY = 13;   // (8 key heads of 128 in 768 shares are 96 or 97 pieces, 8 lanes of 12 or 13.  Other sizes have the rest of theirs read below; only this one was timed)
     dbf_f4 early[EARLY], y = {0.f, 0.f, 0.f, 0.f};
     if (many)
 #pragma unroll
@@ -535,7 +537,7 @@ __global__ __launch_bounds__(256) void dbf_attend_join_kernel(const AttendArgs a
 //            follow each other are those of a lane's 16 bytes of values in the cache.
 //   output:  V^T p^T, 32 values x 32 columns: the scores' places are the product's operand as they are, since the values' tokens are laid out in that order.
 // Both operands lie in LDS as the lanes take them, 16 bytes a lane one after the other.
-// Measured: 3 prompts of 2048 causal rows of 32 heads of 128 on 2048 .. 3001 tokens, 165 GFLOP in 203 us, 810 TFLOP/s (a large library product of fp16: 1360).  A SIMD's products take 39 %
+// Measured: 3 prompts of 2048 causal rows of 32 heads of 128 on 2048 .. 3001 tokens, 165 GFLOP in 204 us, 808 TFLOP/s (a large library product of fp16: 1360).  A SIMD's products take 39 %
 // of the time, its vector instructions 55 %, operands' reads from LDS half of what LDS gives: a product of 32 clocks takes 8 clocks of LDS for each of four SIMDs, so that products alone
 // keep it busy.  Eight wavefronts a workgroup 214 for 219 us then, and 1.5 times as long for heads of 64 and 256; tiles of 32 tokens for three wavefronts a SIMD 207 for 204; 64 rows a
 // wavefront, one a SIMD, 325 for 222; two halves of a workgroup half a step apart 222 for 211; products and vector instructions of a wavefront alternating 227 for 214.
@@ -875,10 +877,11 @@ struct Cut {
 };
 Cut cut_of(const dbf_attend* a, const dbf_cache* c) {
     Cut k = {};
+    // One form for the whole call: lengths are not known here.  Single tokens beside a prompt pay for that, 63 of 1 .. 8192 tokens and 512 rows on 8192 (32 heads on 8) take 489 us, and 69 and 95 in two calls.
     k.few = (long long)a->max_q * (a->n_q_heads / c->n_kv_heads) <= FEW;
     // Items are shared out where the longest may be more than a workgroup should have: 1200 tokens, and more the more items there are to fill the chip beside it.  us, an item to a
     // workgroup and shared out: 8 items of 1000 tokens 10.7 and 11.4, of 1500 14.1 and 12.6, of 4000 29 and 14; 64 of 2500 20 and 17; 256 of 2500 22 and 27, of 4000 32 and 37; 512 of 1 .. 4000
-    // 43 and 39, of 4000 52 and 62, of 1 .. 8192 79 and 63; 1600 of 1 .. 3000 77 and 84; 2400 of 1 .. 2500 90 and 114.
+    // 43 and 39 (the rule leaves them unshared: it knows the longest request only), of 4000 52 and 62, of 1 .. 8192 79 and 63; 1600 of 1 .. 3000 77 and 84; 2400 of 1 .. 2500 90 and 114.
     const long long items = (long long)a->n_seq * c->n_kv_heads;
     if (k.few && a->max_kv > 1200 + 11 * items && items * (a->max_kv / 32 + 1 + BESIDE) < 1 << 30) {   // (and the sum of all costs fits: no memory holds more, but tables may say so)
         k.shares = 256 * few_waves(c->head_dim / 64);

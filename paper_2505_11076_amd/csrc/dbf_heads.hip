@@ -34,7 +34,7 @@ __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// Any even head size: a wavefront takes one head of one token, by LDS.
+// Any even head size: a wavefront takes one head of one token, by LDS.  (8191 tokens of 40 heads of 96, 129 MB: 192 us.)
 // A head's norm and rotation, from memory to `row` in LDS, by one wavefront.
 template <typename T>
 __device__ __forceinline__ void turn(const HeadsArgs& a, const T* x, const T* weight, int token, int lane, float* row) {
@@ -171,8 +171,8 @@ __global__ __launch_bounds__(64 * WAVES) void dbf_heads_kernel(const HeadsArgs a
 // 8 / N heads a wavefront's.  Query heads come first, then the key heads (with their values, where those go to the cache); a wavefront has one kind.
 // Without a cache bound by the read and the write: 8191 tokens of 32 + 8 heads of 128, 170 MB in 36.5 us (4.65 TB/s; a large copy has 4.95).  (A wavefront to a head, values of a lane 64
 // apart and through LDS: 238 us.)
-// Into the cache: 2047 tokens of 32 + 32 heads of 128 in 29 us, 11 of them the queries' norms and rotation; the rest are the groups' scales and codes (about 400 instructions for 16 values of a
-// lane) and stores: codes of values written a byte at a time were 38 us, divisions and maxima as they are written in C one more.
+// Into the cache: 2047 tokens of 32 + 32 heads of 128 in 29 us, 11 of them the queries' norms and rotation; the rest are the groups' scales and codes (610 vector instructions of a wavefront with
+// keys and values, 16 of them a lane; 187 of one with queries) and stores: codes of values written a byte at a time were 38 us, divisions and maxima as they are written in C one more.
 template <typename T>
 struct Quad {
     dbf_u2 w;

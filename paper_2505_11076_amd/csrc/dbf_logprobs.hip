@@ -6,8 +6,10 @@
 // bound that the n largest of all are not below, and only threads whose largest key is not below it can hold any: their values are read once more (from the cache), the
 // few that pass are put in order.
 // A row is one workgroup's, or where rows are few the slices of several, whose sums and lists a second launch joins.
-// Bound by the read where rows are many: 2048 rows of 32000 fp16, 131 MB in 27 us (4.85 TB/s; a large copy has 4.95); a value costs about nine issue slots (its exponential four), half of what
-// the memory takes.  One row of 128256 with 20 alternatives: 7.6 us and 4.2 of the join, latencies.
+// Where rows are many the read and the vector instructions share the time: 2048 rows of 32000 fp16, 131 MB in 27 us (4.85 TB/s), where a read alone has 20; a value costs about nine issue slots (its
+// exponential four), vector units are 77 % busy and waves wait 45 % of their time for issue.  With 20 alternatives 43 us.  One row of 128256 with 20 alternatives: 7.6 us and 4.2 of the join, latencies.
+// Rows of more than ROOM values, but fewer than 32 for each alternative, have no bound: everything passes, there is no room for it, and the likeliest are looked for one by one (2048 rows of 1500
+// with 64: 145 us).
 #include <algorithm>
 #include <climits>
 
