@@ -2,6 +2,7 @@
 //
 // One read of the logits, with a maximum m that may lag and the sums s = sum e^(x - m), t = sum e^(x - m) (x - m) of what has been read, in fp32:
 //     log sum e^x = m + log s,      entropy = log s - t / s.
+// 32 terms make a sum of their own, and what is rounded off where that is added is kept for the next.
 // The likeliest tokens: all values have keys (value, then the lower index) that differ.  A thread keeps its largest, four threads theirs; the n-th largest of these 64 is a
 // bound that the n largest of all are not below, and only threads whose largest key is not below it can hold any: their values are read once more (from the cache), the
 // few that pass are put in order.
@@ -199,6 +200,13 @@ __device__ __forceinline__ void likeliest(const T* x, int n, int base, u64 best,
     }
 }
 
+// A sum and what it has lost so far: with one more term, whose rounding goes there.  (Added one by one, equal terms lose the same each time: 3e-5 of a sum of 586, 1e-3 of 65536.)
+__device__ __forceinline__ float add(float sum, float term, float& lost) {
+    const float wanted = term - lost, next = sum + wanted;
+    lost = (next - sum) - wanted;
+    return next;
+}
+
 // A row's target and its logit, asked for before anything else.
 struct Target {
     int id;
@@ -222,7 +230,7 @@ __global__ __launch_bounds__(THREADS) void dbf_logprobs_kernel(const LogprobArgs
     const T* x = static_cast<const T*>(a.x) + row * a.stride + base;
     const Target target(a, row, static_cast<const T*>(a.x) + row * a.stride, tid == 0 && a.slices == 1);
     Sums s = {LEAST, 0.f, 0.f};
-    float most = -__builtin_inff();
+    float most = -__builtin_inff(), lost_s = 0.f, lost_t = 0.f;
     int most_run = INT_MAX;   // the first run that holds it
     constexpr int AHEAD = 4, STEP = THREADS * RUN * AHEAD;
     Run<T> run[AHEAD];
@@ -246,15 +254,19 @@ __global__ __launch_bounds__(THREADS) void dbf_logprobs_kernel(const LogprobArgs
         if (top > s.m + 8.f) {   // (rarely, once the first run is read)
             const Sums o = s;
             s = join(o, (Sums){fminf(top, -LEAST), 0.f, 0.f});   // (of a finite row the largest is its maximum as it is)
+            lost_s = lost_t = 0.f;
         }
+        float add_s = 0.f, add_t = 0.f;
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k)
 #pragma unroll
             for (int e = 0; e < RUN; ++e) {
                 const float d = v[k][e] - s.m, w = __builtin_amdgcn_exp2f(d * 1.44269504089f);
-                s.s += w;
-                s.t = fmaf(w, below(d), s.t);
+                add_s += w;
+                add_t = fmaf(w, below(d), add_t);
             }
+        s.s = add(s.s, add_s, lost_s);
+        s.t = add(s.t, add_t, lost_t);
     }
     const bool number = s.s < __builtin_inff() && s.t == s.t;   // (a logit of +infinity makes the sum that)
     s = wave_join(s);

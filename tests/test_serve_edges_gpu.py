@@ -271,3 +271,29 @@ def test_a_cache_read_of_more_tokens_than_a_launch_takes():
         assert (o[n] == 7).all() and (o[32] == 0).all() and (o[:32] != 7).all()
         whole = (n // 33) * 33
         assert torch.equal(o[:whole].view(-1, 33, 64), o[:33].expand(whole // 33, 33, 64)) and torch.equal(o[whole: n], o[: n - whole])
+
+
+# ---- log probabilities: long sums ---------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("rows,vocab,dtype", [(800, 32000, "bf16"), (800, 150000, "f16"), (800, 1 << 22, "f16"), (1, 1 << 24, "f32"), (5, 1 << 24, "f16"), (800, 128256, "f32")])
+def test_token_logprobs_of_many_equal_logits(rows, vocab, dtype):
+    """A few tokens at 0 and all others alike, further down by another amount in each row: equal terms are rounded the same way each time they are added, so what is lost grows with their number
+    unless sums are kept short or what they lose is kept."""
+    d = torch.linspace(0.03, 9.5, rows, device="cuda").to(T.DT[dtype][0])
+    ones = torch.arange(vocab, device="cuda") % (1 << 18) < 2048
+    x = torch.where(ones, torch.zeros((), dtype=d.dtype, device="cuda"), -d[:, None])
+    lp, h = (torch.full((rows + 1,), 7.0, device="cuda") for _ in range(2))
+    t = torch.where(torch.arange(rows, device="cuda") % 2 == 0, 0, vocab - 1).to(torch.int32)
+    ws = torch.empty(max(256, B.dbf_token_logprobs_workspace_bytes(rows, vocab, 0)), dtype=torch.uint8, device="cuda")
+    B.dbf_token_logprobs(T.ptr(x), T.DT[dtype][1], vocab, rows, vocab, T.ptr(t), 0, T.ptr(lp), T.ptr(h), 0, 0, T.ptr(ws), ws.numel(), G.stream_handle())
+    torch.cuda.synchronize()
+    n, at = int(ones.sum()), T.f64(d)
+    assert not ones[vocab - 1]
+    z = n + (vocab - n) * np.exp(-at)
+    want = np.where(np.arange(rows) % 2 == 0, 0.0, -at) - np.log(z)
+    entropy = np.log(z) + (vocab - n) * np.exp(-at) / z * at
+    per = 2.0 ** -20 * (1 + math.log(vocab))
+    T.close(T.f64(lp[:rows]), want, per + 2.0 ** -20 * np.abs(want), "logprob of %d x %d" % (rows, vocab))
+    T.close(T.f64(h[:rows]), entropy, per + 2.0 ** -20 * entropy, "entropy of %d x %d" % (rows, vocab))
+    assert lp[rows] == 7 and h[rows] == 7
