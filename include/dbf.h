@@ -349,7 +349,7 @@ enum { DBF_F16 = 0, DBF_BF16 = 1, DBF_F32 = 2 };
 /* The cache: pages of page_tokens (32, 64, 128 or 256) tokens, n_kv_heads heads of head_dim (64, 128 or 256) keys and values each, in
  * one block of dbf_cache_bytes bytes (16-byte aligned, caller's).  `slot` = page * page_tokens + place in the page.
  * A value is s (c - z): a code c of 4 bits, and for each group of 64 values of a token and head a scale s and an integer z in 0..15.
- * Group of value d: (d / 16) mod (head_dim / 64).  s is the range of the group's values and zero, over 15, rounded up to 7 significant
+ * Group of value d: (d / 16) mod (head_dim / 64).  s is the range of the group's values and zero (in fp32), over 15, rounded up to 7 significant
  * bits and to a multiple of 2^-24, so that every value held is exact in fp16; z = rint(-lo / s), c = clamp(rint(x / s) + z, 0, 15),
  * ties to even.  Values beyond +-57344 are held as that.  4.5 bits a value in all.
  * Layout: records of 32 tokens, 36 * head_dim bytes, in the order [page][head][page_tokens / 32]:
@@ -378,7 +378,7 @@ size_t dbf_cache_bytes(int n_pages, int page_tokens, int n_kv_heads, int head_di
  * Entries of positions and slots behind the last token are 0 and -1.  Tokens beyond max_tokens get none, and pages that begin with such a token are
  * counted in status but not entered in the table: where q_start[n_seq] is more than max_tokens, call again with room for all, on the same
  * lengths, free pages and table.  All arrays are device
- * int32, 4-byte aligned; free_pages may be NULL if n_free is 0, positions and slots if max_tokens is 0.
+ * int32, 4-byte aligned; free_pages may be NULL if n_free is 0, positions and slots if max_tokens is 0.  What is written overlaps nothing else.
  * Errors: DBF_EINVAL (null, misaligned, n_seq < 1 or > DBF_MAX_DIM, n_free or max_tokens < 0, table_stride < 1, page_tokens), DBF_EHIP. */
 int dbf_block_tables(const int32_t* cached_len, const int32_t* new_len, int n_seq, int page_tokens, const int32_t* free_pages, int n_free,
                      int32_t* block_table, int table_stride, int max_tokens, int32_t* q_start, int32_t* kv_len, int32_t* positions,
@@ -391,7 +391,7 @@ int dbf_block_tables(const int32_t* cached_len, const int32_t* new_len, int n_se
  *             neighbours (2 i, 2 i + 1) if interleaved; rope: device fp32 [rope_len][rot_dim], the cosines, then the sines of a
  *             position's pairs; positions: device int32 [n_tokens].  rope NULL: no rotation.  A token whose position is not in
  *             [0, rope_len) gets no numbers for its rotated values.
- * In fp32, rounded once at the end. */
+ * In fp32, rounded once at the end (a bfloat16 head whose squares pass fp32, from 1.8e19 on, is normed to zeros). */
 typedef struct dbf_heads {
     const void *q, *k, *v;
     long long q_stride, k_stride, v_stride;

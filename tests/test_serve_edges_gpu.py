@@ -297,3 +297,59 @@ def test_token_logprobs_of_many_equal_logits(rows, vocab, dtype):
     T.close(T.f64(lp[:rows]), want, per + 2.0 ** -20 * np.abs(want), "logprob of %d x %d" % (rows, vocab))
     T.close(T.f64(h[:rows]), entropy, per + 2.0 ** -20 * entropy, "entropy of %d x %d" % (rows, vocab))
     assert lp[rows] == 7 and h[rows] == 7
+
+
+# ---- attention: launches that share work out, in a captured graph ---------------------------------------------
+
+
+def test_shared_and_cut_calls_in_a_graph():
+    """Single tokens in equal shares and rows on a long axis in parts, captured once: lengths and queries change between the replays, each of which equals the calls made one by one."""
+    rng = np.random.default_rng(8)
+    kv, page, hk, D = [6000, 900, 64, 2500], 32, 2, 128
+    data, pages, table, k, v = T.make_cache(rng, kv, page, hk, D)
+    tab, cache = T.ints(table), B.Cache(data=T.ptr(data), n_pages=pages, page_tokens=page, n_kv_heads=hk, head_dim=D)
+    g = torch.Generator(device="cuda").manual_seed(4)
+    calls = []
+    for rows in (1, 20):
+        n = 4 * rows
+        q, out = (torch.empty(n, 4 * D, dtype=torch.float16, device="cuda") for _ in range(2))
+        start, length = T.ints([i * rows for i in range(5)]), T.ints(kv)
+        a = B.Attend(q=T.ptr(q), q_stride=4 * D, out=T.ptr(out), out_stride=4 * D, dtype=B.F16, n_tokens=n, n_seq=4, n_q_heads=4, max_q=rows, max_kv=6000, q_start=T.ptr(start),
+                     kv_len=T.ptr(length), block_table=T.ptr(tab), table_stride=tab.shape[1], scale=0.09, causal=1)
+        size = B.dbf_cache_attend_workspace_bytes(a, cache)
+        assert size > 0
+        calls.append((a, q, out, start, length, torch.full((size,), 0xA5, dtype=torch.uint8, device="cuda")))
+
+    def both():
+        for a, _, _, _, _, ws in calls:
+            B.dbf_cache_attend(a, cache, T.ptr(ws), ws.numel(), torch.cuda.current_stream().cuda_stream)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        both()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both()
+    for step in range(12):
+        for _, q, out, start, length, _ in calls:
+            q.normal_(generator=g)
+            rows = len(q) // 4
+            length.copy_(T.ints([int(rng.integers(0, n + 1)) for n in kv]) if step else T.ints(kv))
+            start.copy_(T.ints(np.cumsum([0, rows, int(rng.integers(0, rows + 1)), rows, rows])))
+            out.fill_(7)
+        both()
+        torch.cuda.synchronize()
+        want = [c[2].clone() for c in calls]
+        for c in calls:
+            c[2].fill_(7)
+        graph.replay()
+        torch.cuda.synchronize()
+        for c, w in zip(calls, want):
+            assert torch.equal(c[2], w), step
+            at = T.f64(c[3]).astype(int)
+            for i in range(4):
+                n = int(c[4][i])
+                o, weight, size = S.attend(T.f64(c[1][at[i]: at[i + 1]]).reshape(-1, 4, D), k[i][:n], v[i][:n], 0.09, True)
+                T.close(T.f64(w[at[i]: at[i + 1]]).reshape(-1, 4, D), o, 2.0 ** -10 * weight + 2.0 ** -11 * np.abs(o) + 2 * 2.0 ** -18 * size[..., None] * weight, "step %d" % step)
