@@ -461,6 +461,104 @@ int dbf_token_logprobs(const void* logits, int dtype, long long row_stride, int 
                        float* logprob, float* entropy, int32_t* top_ids, float* top_logprobs, void* workspace_dev, size_t workspace_bytes,
                        void* hip_stream);
 
+/* ---- layers that are not compressed, and layers of experts ----------------------------------
+ * Products with ordinary weights, beside those with DBF layers: what a compression leaves as it is (a decoder's head, the layers that lose most), in 8 bits with
+ * a scale for each block of 128 or in 16 bits (dbf_dense_gemm), experts whose rows are ragged (dbf_grouped_gemm), the rounding of activations and weights to 8
+ * bits (dbf_fp8_quantize), a router's choice of experts and the order of rows that goes with it (dbf_route), and the sum that brings experts' rows back to their
+ * tokens (dbf_combine).  Conventions are those of the section above: asynchronous, nothing allocated, may be captured, results independent of scheduling; element
+ * types are the same, and
+ *   DBF_E4M3: 8 bits, sign, 4 of exponent (bias 7), 3 of mantissa; largest 448; no infinities; 0x7F and 0xFF are no numbers
+ *   DBF_E8M0: a scale as one byte b: 2^(b - 127); 255 is no number */
+enum { DBF_E4M3 = 3, DBF_E8M0 = 4 };
+#define DBF_SCALE_BLOCK 128  /* values of a row that share a scale */
+
+/* dbf_fp8_quantize: x [n_rows][n_cols] of dtype (DBF_F16, DBF_BF16, DBF_F32; rows x_stride values apart, any alignment of the type) as codes in 8 bits, rows
+ * codes_stride bytes apart, and scales, rows scales_stride bytes apart.  A block is 128 values of a row (block_rows 1: activations), or those of 128 rows
+ * (block_rows 128: weights); the last ones of a row, or the last rows, may be fewer.  Its scale is the smallest power of two s, 2^-127 at least, such that no value
+ * is above 448 s (1 for a block of zeros), a code the type's value nearest to x / s, ties to even: the quotient is exact, so both are fully determined.
+ *   codes:  device, 16-byte aligned, codes_stride a multiple of 16; up to the next multiple of 16 a row is filled up with zeros
+ *   scales: device, DBF_E8M0, [ceil(n_rows / block_rows)][ceil(n_cols / 128)]
+ * A block that holds a value which is not finite is all no numbers, with scale 1.  n_rows 0 does nothing.
+ * Errors: DBF_EINVAL (null, misaligned, types, strides, n_rows < 0, block_rows), DBF_ESHAPE (n_cols), DBF_EHIP. */
+int dbf_fp8_quantize(const void* x, int dtype, long long x_stride, int n_rows, int n_cols, int block_rows, void* codes, long long codes_stride,
+                     void* scales, long long scales_stride, void* hip_stream);
+
+/* What a product with ordinary weights reads and writes:  y[r][n] = sum over k of x[row r][k] w[n][k], summed in fp32, rounded once to out_dtype.
+ *   x        [n_x_rows][n_in] of dtype, rows x_stride values apart; x_rows: device int32 [n_rows], row r of y is of row x_rows[r] of x (one that x does not have gives
+ *            a row of zeros); NULL: of row r
+ *   w        [n_out][n_in] of dtype, rows w_stride values apart
+ *   w_up     NULL, or a second matrix like w: y = silu(x w^T) (x w_up^T), silu(g) = g / (1 + e^-g), rounded once
+ *   dtype    DBF_E4M3, or DBF_F16 or DBF_BF16 without scales
+ *   x_scale  DBF_E4M3: DBF_E8M0 [n_x_rows][ceil(n_in / 128)], rows x_scale_stride bytes apart (a multiple of 4, and room for a multiple of 4 blocks; 4-byte aligned)
+ *   w_scale, w_up_scale  DBF_E4M3: [ceil(n_out / 128)][ceil(n_in / 128)] of w_scale_type (DBF_E8M0 or DBF_F32), rows w_scale_stride scales apart
+ *   y        [n_rows][n_out] of out_dtype (DBF_F16, DBF_BF16, DBF_F32), rows y_stride values apart, any alignment of the type
+ * x, w and w_up are 16-byte aligned, and their rows a multiple of 16 bytes apart (what lies between n_in and the next row is not used).
+ * For dbf_grouped_gemm: n_groups matrices, w_group_stride values (w_scale_group_stride scales) from one to the next, in w_up too; starts: device int32
+ * [n_groups + 1], rows starts[g] .. starts[g + 1] - 1 of y are of matrix g (held to 0 .. n_rows; a group that ends before it begins has none; a row may be of one group
+ * only).  Rows before starts[0] or behind starts[n_groups] are left as they were. */
+typedef struct dbf_dense {
+    const void *x, *x_scale;
+    const int32_t* x_rows;
+    const void *w, *w_scale, *w_up, *w_up_scale;
+    void* y;
+    const int32_t* starts;
+    long long x_stride, x_scale_stride, w_stride, w_group_stride, w_scale_stride, w_scale_group_stride, y_stride;
+    int dtype, out_dtype, w_scale_type, n_rows, n_x_rows, n_in, n_out, n_groups;
+} dbf_dense;
+#define DBF_MAX_GROUPS 1024
+
+/* dbf_dense_gemm: one matrix for all rows (starts NULL, n_groups 0; group strides are not used).   dbf_grouped_gemm: a matrix for each group of rows.
+ * workspace_dev: 256-byte aligned, ..._workspace_bytes bytes (may be 0; 0 too if sizes are out of range), which depend on types, sizes and n_groups only; contents need
+ * not be anything, and a workspace serves one call at a time.
+ * Errors: DBF_EINVAL (null, misaligned, types, strides, counts, scales missing or too many), DBF_ESHAPE (n_in or n_out not in 1 .. 2^20), DBF_EWORKSPACE, DBF_EHIP. */
+size_t dbf_dense_gemm_workspace_bytes(const dbf_dense* product);
+int dbf_dense_gemm(const dbf_dense* product, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+size_t dbf_grouped_gemm_workspace_bytes(const dbf_dense* product);
+int dbf_grouped_gemm(const dbf_dense* product, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+
+/* dbf_route: the experts of n_tokens tokens from a router's logits [n_tokens][n_experts] (dtype DBF_F16, DBF_BF16, DBF_F32; rows row_stride values apart).
+ *   score    DBF_SCORE_SOFTMAX: s = softmax over the token's experts; DBF_SCORE_SIGMOID: s = 1 / (1 + e^-x)
+ *   choice   the n_top experts of the largest x, or, with a bias (device fp32 [n_experts]), of the largest s + bias, in this order, ties to the lowest index.  An expert
+ *            whose logit or sum is -infinity or no number is never chosen (nor counts in the softmax, if it is the logit)
+ *   weights  s of the chosen ones, over their sum if renormalise (0 where the sum is 0), times scale
+ * Scores are in 64 bits: what is chosen does not hang on how they are summed.  Out, device:
+ *   expert_ids int32, weights fp32 [n_tokens][n_top]: -1 and 0 where a token has no expert left (a token masked all over has none at all)
+ *   starts     int32 [n_experts + 1]: each expert's first row in the order by experts and, of an expert, by tokens; then the number of all rows
+ *   row_token  int32 [n_tokens * n_top]: each row's token; -1 behind the last row
+ *   token_rows int32 [n_tokens][n_top]: the row of each choice; -1 where there is none
+ * starts and row_token are what dbf_grouped_gemm takes as starts and x_rows, token_rows what dbf_combine does.  n_tokens 0 only clears starts.
+ * workspace_dev: 256-byte aligned, dbf_route_workspace_bytes bytes (may be 0).
+ * Errors: DBF_EINVAL (null, misaligned, types, n_tokens < 0, n_top not in 1 .. 32 or above n_experts, n_tokens * n_top above 2^31 - 1, row_stride), DBF_ESHAPE (n_experts
+ * not in 1 .. DBF_MAX_GROUPS), DBF_EWORKSPACE, DBF_EHIP. */
+enum { DBF_SCORE_SOFTMAX = 0, DBF_SCORE_SIGMOID = 1 };
+typedef struct dbf_router {
+    const void* logits;
+    const float* bias;
+    long long row_stride;
+    int32_t* expert_ids;
+    float* weights;
+    int32_t *starts, *row_token, *token_rows;
+    int dtype, n_tokens, n_experts, n_top, score, renormalise;
+    float scale;
+} dbf_router;
+size_t dbf_route_workspace_bytes(const dbf_router* router);
+int dbf_route(const dbf_router* router, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+
+/* dbf_combine: out[t] = residual[t] + sum over j of weights[t][j] rows[token_rows[t][j]], in fp32, in the order of j, rounded once.  rows [n_rows][n_cols], residual (or
+ * NULL) and out [n_tokens][n_cols] of dtype (DBF_F16, DBF_BF16, DBF_F32), rows strides values apart, any alignment of the type; token_rows: device int32, weights:
+ * device fp32 [n_tokens][n_top].  A row that is not in 0 .. n_rows - 1 counts for nothing.  out may be residual; it overlaps nothing else.
+ * Errors: DBF_EINVAL, DBF_ESHAPE (n_cols not in 1 .. 2^20), DBF_EHIP. */
+typedef struct dbf_combine_rows {
+    const void* rows;
+    const int32_t* token_rows;
+    const float* weights;
+    const void* residual;
+    void* out;
+    long long row_stride, residual_stride, out_stride;
+    int dtype, n_rows, n_tokens, n_top, n_cols;
+} dbf_combine_rows;
+int dbf_combine(const dbf_combine_rows* sum, void* hip_stream);
+
 /* Measurement aid: dbf_stack_gemv with HIP events recorded on `hip_stream` around its
  * launches.  Blocks until the last launch has finished.  *ms_first is the elapsed time of the
  * first kernel (the whole pass for DBF_GEMV_MFMA, the B stage for the two-launch kinds),

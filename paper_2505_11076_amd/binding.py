@@ -26,7 +26,9 @@ GEMM_AUTO, GEMM_I8 = 0, 2
  TUNE_FP4_MAX_ITEMS) = range(16)
 MAX_BATCH = 16
 GEMM_STATIC_BYTES = 32 << 20  # DBF_GEMM_STATIC_BYTES
-F16, BF16, F32 = 0, 1, 2  # element types (DBF_F16, ...)
+F16, BF16, F32, E4M3, E8M0 = range(5)  # element types (DBF_F16, ...)
+SCALE_BLOCK, MAX_GROUPS = 128, 1024  # DBF_SCALE_BLOCK, DBF_MAX_GROUPS
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
 
 EXPORTS = [
     "dbf_pack", "dbf_pack_bits", "dbf_unpack_bits", "dbf_dims", "dbf_free",
@@ -38,6 +40,8 @@ EXPORTS = [
     "dbf_prune_middle", "dbf_svid_workspace_bytes", "dbf_svid", "dbf_admm_workspace_bytes", "dbf_admm_step", "dbf_admm_prepare_workspace_bytes", "dbf_admm_prepare", "dbf_probe_read", "dbf_probe_mfma", "dbf_strerror",
     "dbf_cache_bytes", "dbf_block_tables", "dbf_qk_norm_rope", "dbf_cache_append", "dbf_cache_read",
     "dbf_cache_attend_workspace_bytes", "dbf_cache_attend", "dbf_token_logprobs_workspace_bytes", "dbf_token_logprobs",
+    "dbf_fp8_quantize", "dbf_dense_gemm_workspace_bytes", "dbf_dense_gemm", "dbf_grouped_gemm_workspace_bytes", "dbf_grouped_gemm",
+    "dbf_route_workspace_bytes", "dbf_route", "dbf_combine",
     "dbf_tuning_set", "dbf_tuning_get", "dbf_tuning_reset",
 ]
 
@@ -75,6 +79,31 @@ class Attend(_Described):
                 ("q_start", C.c_void_p), ("kv_len", C.c_void_p), ("block_table", C.c_void_p),
                 ("dtype", C.c_int), ("n_tokens", C.c_int), ("n_seq", C.c_int), ("n_q_heads", C.c_int), ("max_q", C.c_int),
                 ("max_kv", C.c_int), ("table_stride", C.c_int), ("causal", C.c_int), ("scale", C.c_float)]
+
+
+class Dense(_Described):
+    """dbf_dense: a product with ordinary weights, its groups if it has any."""
+    _fields_ = [("x", C.c_void_p), ("x_scale", C.c_void_p), ("x_rows", C.c_void_p), ("w", C.c_void_p), ("w_scale", C.c_void_p), ("w_up", C.c_void_p),
+                ("w_up_scale", C.c_void_p), ("y", C.c_void_p), ("starts", C.c_void_p),
+                ("x_stride", C.c_longlong), ("x_scale_stride", C.c_longlong), ("w_stride", C.c_longlong), ("w_group_stride", C.c_longlong),
+                ("w_scale_stride", C.c_longlong), ("w_scale_group_stride", C.c_longlong), ("y_stride", C.c_longlong),
+                ("dtype", C.c_int), ("out_dtype", C.c_int), ("w_scale_type", C.c_int), ("n_rows", C.c_int), ("n_x_rows", C.c_int), ("n_in", C.c_int),
+                ("n_out", C.c_int), ("n_groups", C.c_int)]
+
+
+class Router(_Described):
+    """dbf_router: a router's logits, and where the choice of experts and the order of rows go."""
+    _fields_ = [("logits", C.c_void_p), ("bias", C.c_void_p), ("row_stride", C.c_longlong), ("expert_ids", C.c_void_p), ("weights", C.c_void_p),
+                ("starts", C.c_void_p), ("row_token", C.c_void_p), ("token_rows", C.c_void_p),
+                ("dtype", C.c_int), ("n_tokens", C.c_int), ("n_experts", C.c_int), ("n_top", C.c_int), ("score", C.c_int), ("renormalise", C.c_int),
+                ("scale", C.c_float)]
+
+
+class Combine(_Described):
+    """dbf_combine_rows: experts' rows, and the sums of them that tokens get."""
+    _fields_ = [("rows", C.c_void_p), ("token_rows", C.c_void_p), ("weights", C.c_void_p), ("residual", C.c_void_p), ("out", C.c_void_p),
+                ("row_stride", C.c_longlong), ("residual_stride", C.c_longlong), ("out_stride", C.c_longlong),
+                ("dtype", C.c_int), ("n_rows", C.c_int), ("n_tokens", C.c_int), ("n_top", C.c_int), ("n_cols", C.c_int)]
 
 
 class DbfError(RuntimeError):
@@ -145,6 +174,15 @@ def lib() -> C.CDLL:
     L.dbf_token_logprobs_workspace_bytes.argtypes = [i32, i32, i32]
     L.dbf_token_logprobs_workspace_bytes.restype = sz
     L.dbf_token_logprobs.argtypes = [vp, i32, C.c_longlong, i32, i32, vp, i32, vp, vp, vp, vp, vp, sz, vp]
+    L.dbf_fp8_quantize.argtypes = [vp, i32, C.c_longlong, i32, i32, i32, vp, C.c_longlong, vp, C.c_longlong, vp]
+    for name in ("dbf_dense_gemm", "dbf_grouped_gemm"):
+        getattr(L, name + "_workspace_bytes").argtypes = [C.POINTER(Dense)]
+        getattr(L, name + "_workspace_bytes").restype = sz
+        getattr(L, name).argtypes = [C.POINTER(Dense), vp, sz, vp]
+    L.dbf_route_workspace_bytes.argtypes = [C.POINTER(Router)]
+    L.dbf_route_workspace_bytes.restype = sz
+    L.dbf_route.argtypes = [C.POINTER(Router), vp, sz, vp]
+    L.dbf_combine.argtypes = [C.POINTER(Combine), vp]
     L.dbf_tuning_set.argtypes = [i32, i32]
     L.dbf_tuning_get.argtypes = [i32]
     L.dbf_tuning_reset.argtypes = []
@@ -436,6 +474,42 @@ def dbf_token_logprobs(logits_ptr: int, dtype: int, row_stride: int, n_rows: int
                        entropy_ptr: int, top_ids_ptr: int, top_logprobs_ptr: int, ws_ptr: int, ws_bytes: int, stream: int = 0) -> None:
     _check(lib().dbf_token_logprobs(logits_ptr, dtype, row_stride, n_rows, vocab, targets_ptr, n_top, logprob_ptr, entropy_ptr, top_ids_ptr,
                                     top_logprobs_ptr, ws_ptr, ws_bytes, stream), "dbf_token_logprobs")
+
+
+# ---- layers that are not compressed, and layers of experts ------------------------------------------------
+
+
+def dbf_fp8_quantize(x_ptr: int, dtype: int, x_stride: int, n_rows: int, n_cols: int, block_rows: int, codes_ptr: int, codes_stride: int, scales_ptr: int,
+                     scales_stride: int, stream: int = 0) -> None:
+    _check(lib().dbf_fp8_quantize(x_ptr, dtype, x_stride, n_rows, n_cols, block_rows, codes_ptr, codes_stride, scales_ptr, scales_stride, stream), "dbf_fp8_quantize")
+
+
+def dbf_dense_gemm_workspace_bytes(product: Dense) -> int:
+    return int(lib().dbf_dense_gemm_workspace_bytes(product))
+
+
+def dbf_dense_gemm(product: Dense, ws_ptr: int = 0, ws_bytes: int = 0, stream: int = 0) -> None:
+    _check(lib().dbf_dense_gemm(product, ws_ptr, ws_bytes, stream), "dbf_dense_gemm")
+
+
+def dbf_grouped_gemm_workspace_bytes(product: Dense) -> int:
+    return int(lib().dbf_grouped_gemm_workspace_bytes(product))
+
+
+def dbf_grouped_gemm(product: Dense, ws_ptr: int = 0, ws_bytes: int = 0, stream: int = 0) -> None:
+    _check(lib().dbf_grouped_gemm(product, ws_ptr, ws_bytes, stream), "dbf_grouped_gemm")
+
+
+def dbf_route_workspace_bytes(router: Router) -> int:
+    return int(lib().dbf_route_workspace_bytes(router))
+
+
+def dbf_route(router: Router, ws_ptr: int = 0, ws_bytes: int = 0, stream: int = 0) -> None:
+    _check(lib().dbf_route(router, ws_ptr, ws_bytes, stream), "dbf_route")
+
+
+def dbf_combine(rows: Combine, stream: int = 0) -> None:
+    _check(lib().dbf_combine(rows, stream), "dbf_combine")
 
 
 def dbf_probe_read(src_ptr: int, nbytes: int, sink_ptr: int = 0, stream: int = 0) -> None:

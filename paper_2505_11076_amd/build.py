@@ -33,6 +33,9 @@ SOURCES = [
     "dbf_heads.hip",
     "dbf_attend.hip",
     "dbf_logprobs.hip",
+    "dbf_fp8.hip",
+    "dbf_dense.hip",
+    "dbf_route.hip",
 ]
 
 FLAGS = [
