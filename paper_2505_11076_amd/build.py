@@ -35,6 +35,7 @@ SOURCES = [
     "dbf_logprobs.hip",
     "dbf_fp8.hip",
     "dbf_dense.hip",
+    "dbf_dense_tiles.hip",
     "dbf_route.hip",
 ]
 

@@ -1,0 +1,155 @@
+// What the kernels of products with ordinary weights share: arguments, tiles of ragged groups, a step of a product, the output (device code and launch rules).
+#ifndef DBF_DENSE_H
+#define DBF_DENSE_H
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "dbf_cache.h"
+#include "dbf_internal.h"
+
+namespace {
+
+typedef int v8i __attribute__((ext_vector_type(8)));
+typedef __bf16 v8b __attribute__((ext_vector_type(8)));
+
+constexpr int STEP = 128;   // bytes of a row to a step
+
+struct DenseArgs {
+    const uint8_t *x, *x_scale, *w, *w_up;
+    const void *w_scale, *w_up_scale;
+    const int32_t *x_rows, *starts;
+    void* y;
+    long long x_row, x_scale_row, w_row, w_group, w_scale_row, w_scale_group, y_stride;   // bytes; of the weights' scales: scales; of y: values
+    int out_dtype, n_rows, n_x_rows, k_bytes, n_out, n_groups, quads;
+};
+
+// Which rows a tile has: tiles of a group's rows, group after group.
+struct Tile {
+    int group, row, rows;   // rows 0: there is no such tile
+};
+__device__ __forceinline__ Tile tile_of(const DenseArgs& a, int tile, int of_rows) {
+    if (!a.starts) {
+        const long long row = (long long)tile * of_rows;
+        return {0, (int)row, (int)max(min((long long)of_rows, a.n_rows - row), 0LL)};
+    }
+    const int lane = threadIdx.x & 63;
+    int before = 0;
+    for (int g0 = 0; g0 < a.n_groups; g0 += 64) {
+        const int g = g0 + lane;
+        int from = 0, to = 0;
+        if (g < a.n_groups) {
+            from = min(max(a.starts[g], 0), a.n_rows);
+            to = min(max(a.starts[g + 1], 0), a.n_rows);
+        }
+        const int tiles = to > from ? (to - from - 1) / of_rows + 1 : 0;
+        int upto = tiles;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int other = __shfl_up(upto, d);
+            if (lane >= d) upto += other;
+        }
+        const unsigned long long past = __ballot(before + upto > tile);
+        if (past) {
+            const int l = __builtin_ctzll(past);
+            const int row = __builtin_amdgcn_readlane(from, l) + (tile - before - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(tiles, l))) * of_rows;
+            return {g0 + l, row, min(of_rows, __builtin_amdgcn_readlane(to, l) - row)};
+        }
+        before += __builtin_amdgcn_readlane(upto, 63);
+    }
+    return {0, 0, 0};
+}
+
+// The 16 bytes of a row from byte `at` on, of which those from byte `end` of the row on are zeros.
+__device__ __forceinline__ dbf_u4 piece(const uint8_t* row, int at, int end) {
+    if (at >= end) return (dbf_u4){0, 0, 0, 0};
+    dbf_u4 v = *reinterpret_cast<const dbf_u4*>(row + at);
+    if (at + 16 > end) {
+        const int have = end - at;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = have >= 4 * i + 4 ? v[i] : have <= 4 * i ? 0u : v[i] & (0xFFFFFFFFu >> (32 - 8 * (have - 4 * i)));
+    }
+    return v;
+}
+
+__device__ __forceinline__ v8i both(dbf_u4 a, dbf_u4 b) { return __builtin_bit_cast(v8i, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7)); }
+__device__ __forceinline__ dbf_u4 first(v8i v) { return __builtin_bit_cast(dbf_u4, __builtin_shufflevector(v, v, 0, 1, 2, 3)); }
+__device__ __forceinline__ dbf_u4 second(v8i v) { return __builtin_bit_cast(dbf_u4, __builtin_shufflevector(v, v, 4, 5, 6, 7)); }
+
+// acc += w x over a step.  TYPE: DBF_E4M3, DBF_F16 or DBF_BF16; FLOAT: weights' scales are fp32 numbers.
+template <int TYPE, bool FLOAT>
+__device__ __forceinline__ void multiply(dbf_f4& acc, const v8i& w, const v8i& x, int w_scale, int x_scale) {
+    if constexpr (TYPE == DBF_E4M3) {
+        if constexpr (FLOAT) {
+            const dbf_f4 none = {0.f, 0.f, 0.f, 0.f};
+            const dbf_f4 p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, none, 0, 0, 0, 127, 0, x_scale);
+            const float s = __builtin_bit_cast(float, w_scale);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[i] = fmaf(s, p[i], acc[i]);
+        } else {
+            acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, acc, 0, 0, 0, w_scale, 0, x_scale);
+        }
+    } else if constexpr (TYPE == DBF_F16) {
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(dbf_h8, first(w)), __builtin_bit_cast(dbf_h8, first(x)), acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(dbf_h8, second(w)), __builtin_bit_cast(dbf_h8, second(x)), acc, 0, 0, 0);
+    } else {
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8b, first(w)), __builtin_bit_cast(v8b, first(x)), acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8b, second(w)), __builtin_bit_cast(v8b, second(x)), acc, 0, 0, 0);
+    }
+}
+
+// The bytes of two pieces as 16 + 16 values in fp16, exactly.
+__device__ __forceinline__ void widen(v8i in, dbf_h8 (&out)[4]) {
+    typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int h = 0; h < 4; ++h)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const v2h lo = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(in[2 * h + i], 1.f, false);
+            const v2h hi = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(in[2 * h + i], 1.f, true);
+            out[h][4 * i] = lo[0];
+            out[h][4 * i + 1] = lo[1];
+            out[h][4 * i + 2] = hi[0];
+            out[h][4 * i + 3] = hi[1];
+        }
+}
+// The number that a byte of a scale stands for (255: no number; 0: 2^-127, which only a subnormal number is).
+__device__ __forceinline__ float scale_of(int byte) {
+    return __builtin_bit_cast(float, byte == 255 ? 0x7FC00000u : byte ? (unsigned)byte << 23 : 0x00400000u);
+}
+
+__device__ __forceinline__ float gate(float g, float up) { return g / (1.f + expf(-g)) * up; }
+
+// Four neighbouring outputs of a row, from column n on.
+template <typename T>
+__device__ __forceinline__ void store4_as(T* at, const dbf_f4& v, int have, bool whole) {
+    T out[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[i] = dbf_from_float<T>(v[i]);
+    if (whole && have >= 4) {
+        typedef std::conditional_t<sizeof(T) == 4, dbf_u4, dbf_u2> Words;
+        Words w;
+        __builtin_memcpy(&w, out, sizeof(w));
+        *reinterpret_cast<Words*>(at) = w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < have) at[i] = out[i];
+    }
+}
+__device__ __forceinline__ void store4(const DenseArgs& a, int row, int n, const dbf_f4& v) {
+    const long long at = row * a.y_stride + n;
+    const int have = a.n_out - n;
+    if (a.out_dtype == DBF_F16) store4_as(static_cast<_Float16*>(a.y) + at, v, have, a.quads);
+    else if (a.out_dtype == DBF_BF16) store4_as(static_cast<dbf_bf16*>(a.y) + at, v, have, a.quads);
+    else store4_as(static_cast<float*>(a.y) + at, v, have, a.quads);
+}
+
+}  // namespace
+
+// 0: done; else DBF_EHIP.  (dbf_dense_tiles.hip)
+int dbf_dense_tiles(const void* args, int type, bool float_scales, hipStream_t stream);
+
+#endif  // DBF_DENSE_H

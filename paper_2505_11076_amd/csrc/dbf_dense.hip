@@ -4,128 +4,9 @@
 // y^T = W x^T on the matrix cores: the weights are the operand of the result's rows, so that a lane has four neighbouring outputs of one row of y.  A step is 128 bytes of
 // a row: in 8 bits one instruction over a block of 128 (exactly one scale of each operand, powers of two applied by the instruction; fp32 scales of weights on its
 // result), in 16 bits two over 32 values each.  Of a step's eight 16-byte pieces lane group q = lane / 16 has pieces q and q + 4, of both operands: any order of k does.
-#include <hip/hip_runtime.h>
-
-#include <algorithm>
-#include <type_traits>
-
-#include "dbf_cache.h"
-#include "dbf_internal.h"
+#include "dbf_dense.h"
 
 namespace {
-
-typedef int v8i __attribute__((ext_vector_type(8)));
-typedef __bf16 v8b __attribute__((ext_vector_type(8)));
-
-constexpr int STEP = 128;   // bytes of a row to a step
-
-struct DenseArgs {
-    const uint8_t *x, *x_scale, *w, *w_up;
-    const void *w_scale, *w_up_scale;
-    const int32_t *x_rows, *starts;
-    void* y;
-    long long x_row, x_scale_row, w_row, w_group, w_scale_row, w_scale_group, y_stride;   // bytes; of the weights' scales: scales; of y: values
-    int out_dtype, n_rows, n_x_rows, k_bytes, n_out, n_groups, quads;
-};
-
-// Which rows a tile has: tiles of a group's rows, group after group.
-struct Tile {
-    int group, row, rows;   // rows 0: there is no such tile
-};
-__device__ __forceinline__ Tile tile_of(const DenseArgs& a, int tile, int of_rows) {
-    if (!a.starts) {
-        const long long row = (long long)tile * of_rows;
-        return {0, (int)row, (int)max(min((long long)of_rows, a.n_rows - row), 0LL)};
-    }
-    const int lane = threadIdx.x & 63;
-    int before = 0;
-    for (int g0 = 0; g0 < a.n_groups; g0 += 64) {
-        const int g = g0 + lane;
-        int from = 0, to = 0;
-        if (g < a.n_groups) {
-            from = min(max(a.starts[g], 0), a.n_rows);
-            to = min(max(a.starts[g + 1], 0), a.n_rows);
-        }
-        const int tiles = to > from ? (to - from - 1) / of_rows + 1 : 0;
-        int upto = tiles;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int other = __shfl_up(upto, d);
-            if (lane >= d) upto += other;
-        }
-        const unsigned long long past = __ballot(before + upto > tile);
-        if (past) {
-            const int l = __builtin_ctzll(past);
-            const int row = __builtin_amdgcn_readlane(from, l) + (tile - before - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(tiles, l))) * of_rows;
-            return {g0 + l, row, min(of_rows, __builtin_amdgcn_readlane(to, l) - row)};
-        }
-        before += __builtin_amdgcn_readlane(upto, 63);
-    }
-    return {0, 0, 0};
-}
-
-// The 16 bytes of a row from byte `at` on, of which those from byte `end` of the row on are zeros.
-__device__ __forceinline__ dbf_u4 piece(const uint8_t* row, int at, int end) {
-    if (at >= end) return (dbf_u4){0, 0, 0, 0};
-    dbf_u4 v = *reinterpret_cast<const dbf_u4*>(row + at);
-    if (at + 16 > end) {
-        const int have = end - at;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = have >= 4 * i + 4 ? v[i] : have <= 4 * i ? 0u : v[i] & (0xFFFFFFFFu >> (32 - 8 * (have - 4 * i)));
-    }
-    return v;
-}
-
-// acc += w x over a step.  TYPE: DBF_E4M3, DBF_F16 or DBF_BF16; FLOAT: weights' scales are fp32 numbers.
-template <int TYPE, bool FLOAT>
-__device__ __forceinline__ void multiply(dbf_f4& acc, const dbf_u4 (&w)[2], const dbf_u4 (&x)[2], int w_scale, int x_scale) {
-    if constexpr (TYPE == DBF_E4M3) {
-        const v8i a = {(int)w[0][0], (int)w[0][1], (int)w[0][2], (int)w[0][3], (int)w[1][0], (int)w[1][1], (int)w[1][2], (int)w[1][3]};
-        const v8i b = {(int)x[0][0], (int)x[0][1], (int)x[0][2], (int)x[0][3], (int)x[1][0], (int)x[1][1], (int)x[1][2], (int)x[1][3]};
-        if constexpr (FLOAT) {
-            const dbf_f4 none = {0.f, 0.f, 0.f, 0.f};
-            const dbf_f4 p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, none, 0, 0, 0, 127, 0, x_scale);
-            const float s = __builtin_bit_cast(float, w_scale);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[i] = fmaf(s, p[i], acc[i]);
-        } else {
-            acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc, 0, 0, 0, w_scale, 0, x_scale);
-        }
-    } else {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            if constexpr (TYPE == DBF_F16) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(dbf_h8, w[h]), __builtin_bit_cast(dbf_h8, x[h]), acc, 0, 0, 0);
-            else acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8b, w[h]), __builtin_bit_cast(v8b, x[h]), acc, 0, 0, 0);
-        }
-    }
-}
-
-__device__ __forceinline__ float gate(float g, float up) { return g / (1.f + expf(-g)) * up; }
-
-// Four neighbouring outputs of a row, from column n on.
-template <typename T>
-__device__ __forceinline__ void store4_as(T* at, const dbf_f4& v, int have, bool whole) {
-    T out[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) out[i] = dbf_from_float<T>(v[i]);
-    if (whole && have >= 4) {
-        typedef std::conditional_t<sizeof(T) == 4, dbf_u4, dbf_u2> Words;
-        Words w;
-        __builtin_memcpy(&w, out, sizeof(w));
-        *reinterpret_cast<Words*>(at) = w;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < have) at[i] = out[i];
-    }
-}
-__device__ __forceinline__ void store4(const DenseArgs& a, int row, int n, const dbf_f4& v) {
-    const long long at = row * a.y_stride + n;
-    const int have = a.n_out - n;
-    if (a.out_dtype == DBF_F16) store4_as(static_cast<_Float16*>(a.y) + at, v, have, a.quads);
-    else if (a.out_dtype == DBF_BF16) store4_as(static_cast<dbf_bf16*>(a.y) + at, v, have, a.quads);
-    else store4_as(static_cast<float*>(a.y) + at, v, have, a.quads);
-}
 
 // 16 outputs of 16 rows to a wavefront.
 constexpr int ROWS = 16, WAVES = 4;
@@ -152,11 +33,11 @@ __global__ __launch_bounds__(64 * WAVES) void dbf_dense_kernel(const DenseArgs a
         dbf_f4 acc = {0.f, 0.f, 0.f, 0.f}, acc_up = {0.f, 0.f, 0.f, 0.f};
         for (int k = 0, b = 0; k < a.k_bytes; k += STEP, ++b) {
             const int at0 = k + 16 * q, at1 = at0 + 64;
-            const dbf_u4 xs[2] = {piece(x, at0, a.k_bytes), piece(x, at1, a.k_bytes)}, ws[2] = {piece(w, at0, a.k_bytes), piece(w, at1, a.k_bytes)};
+            const v8i xs = both(piece(x, at0, a.k_bytes), piece(x, at1, a.k_bytes)), ws = both(piece(w, at0, a.k_bytes), piece(w, at1, a.k_bytes));
             const int sx = TYPE == DBF_E4M3 ? x_scale[b] : 0;
             multiply<TYPE, FLOAT>(acc, ws, xs, TYPE == DBF_E4M3 ? scale(a.w_scale, b) : 0, sx);
             if constexpr (GATED) {
-                const dbf_u4 us[2] = {piece(up, at0, a.k_bytes), piece(up, at1, a.k_bytes)};
+                const v8i us = both(piece(up, at0, a.k_bytes), piece(up, at1, a.k_bytes));
                 multiply<TYPE, FLOAT>(acc_up, us, xs, TYPE == DBF_E4M3 ? scale(a.w_up_scale, b) : 0, sx);
             }
         }
@@ -179,6 +60,9 @@ int launch(const DenseArgs& a, hipStream_t stream) {
     return a.w_up ? launch<TYPE, FLOAT, true>(a, stream) : launch<TYPE, FLOAT, false>(a, stream);
 }
 
+constexpr long long MOST_STRIDE = 1 << 22;   // values of a row of x or weights: a tile's bytes have 32-bit offsets
+constexpr long long MOST_GATHERED = 1LL << 32;   // bytes of x whose rows are given: the same
+
 bool types_ok(const dbf_dense* p) {
     if (p->dtype != DBF_E4M3 && p->dtype != DBF_F16 && p->dtype != DBF_BF16) return false;
     if (p->out_dtype != DBF_F16 && p->out_dtype != DBF_BF16 && p->out_dtype != DBF_F32) return false;
@@ -191,9 +75,10 @@ int check(const dbf_dense* p, bool grouped) {
     if (p->n_in < 1 || p->n_in > DBF_MAX_DIM || p->n_out < 1 || p->n_out > DBF_MAX_DIM) return DBF_ESHAPE;
     if (p->n_rows < 0 || p->n_x_rows < 0 || (!p->x_rows && p->n_x_rows < p->n_rows) || (p->n_rows && !p->n_x_rows)) return DBF_EINVAL;
     if (grouped ? !p->starts || p->n_groups < 1 || p->n_groups > DBF_MAX_GROUPS : p->starts || p->n_groups) return DBF_EINVAL;
+    if (p->x_rows && (p->n_x_rows * p->x_stride * (p->dtype == DBF_E4M3 ? 1 : 2) > MOST_GATHERED || p->n_x_rows * p->x_scale_stride > MOST_GATHERED)) return DBF_EINVAL;
     const int per = p->dtype == DBF_E4M3 ? 16 : 8, kb = (p->n_in + DBF_SCALE_BLOCK - 1) / DBF_SCALE_BLOCK;
     if (p->x_stride < p->n_in || p->x_stride % per || p->w_stride < p->n_in || p->w_stride % per || p->y_stride < p->n_out) return DBF_EINVAL;
-    if (p->x_stride > (1 << 24) || p->w_stride > (1 << 24) || p->y_stride > (1LL << 32)) return DBF_EINVAL;
+    if (p->x_stride > MOST_STRIDE || p->w_stride > MOST_STRIDE || p->y_stride > (1LL << 32)) return DBF_EINVAL;
     if (grouped && (p->w_group_stride < 0 || p->w_group_stride % per)) return DBF_EINVAL;
     if (dbf_misaligned(p->x, 16) || dbf_misaligned(p->w, 16) || dbf_misaligned(p->w_up, 16) || dbf_misaligned(p->x_rows, 4) || dbf_misaligned(p->starts, 4)) return DBF_EINVAL;
     if (dbf_misaligned(p->y, p->out_dtype == DBF_F32 ? 4 : 2)) return DBF_EINVAL;
@@ -234,6 +119,7 @@ int run(const dbf_dense* p, bool grouped, hipStream_t stream) {
     a.n_out = p->n_out;
     a.n_groups = grouped ? p->n_groups : 0;
     a.quads = p->y_stride % 4 == 0 && !dbf_misaligned(p->y, quad);
+    if (a.n_rows > 16 * std::max(a.n_groups, 1)) return dbf_dense_tiles(&a, p->dtype, p->w_scale_type == DBF_F32, stream);
     if (p->dtype == DBF_F16) return launch<DBF_F16, false>(a, stream);
     if (p->dtype == DBF_BF16) return launch<DBF_BF16, false>(a, stream);
     return p->w_scale_type == DBF_F32 ? launch<DBF_E4M3, true>(a, stream) : launch<DBF_E4M3, false>(a, stream);

@@ -1,0 +1,250 @@
+// Products with ordinary weights, many rows: tiles of weights and rows in LDS (include/dbf.h: dbf_dense_gemm, dbf_grouped_gemm; dbf_dense.h: the instructions).
+#include "dbf_dense.h"
+
+namespace {
+
+typedef const __attribute__((address_space(1))) unsigned* Global;
+typedef __attribute__((address_space(3))) unsigned* Shared;
+
+// A tile is BN rows of weights (gated: 16 of w, 16 of w_up, in turn) times BM rows of x, WN x WM wavefronts.  A step is 128 bytes of all rows; LDS holds two, of which a
+// row is 128 bytes, its piece p at place p ^ (row % 8): the 64 pieces that a wavefront reads at once lie in all banks evenly.
+// A wavefront has its weights of a step in registers and its rows of x in pairs of 16.  Before a step's last pair all have read what the step has in LDS: there they meet,
+// the next step but one sets out for its place, and as each of the weights has done its last product the next step's comes from LDS into its registers: reads and loads are
+// under way beside products at all times.
+template <int TYPE, bool FLOAT, bool GATED, bool EXACT, int BN, int BM, int WN, int WM, int EACH>
+__global__ __launch_bounds__(64 * WN * WM) __attribute__((amdgpu_waves_per_eu(EACH, EACH))) void dbf_dense_tiles_kernel(const DenseArgs a, int n_tiles, int m_tiles) {
+    constexpr int WAVES = WN * WM, NS = BN / WN / 16, MS = BM / WM / 16, OUTS = GATED ? BN / 2 : BN;
+    constexpr int W_LOADS = BN / 8 / WAVES, X_LOADS = BM / 8 / WAVES;
+    static_assert(W_LOADS * 8 * WAVES == BN && X_LOADS * 8 * WAVES == BM && MS % 2 == 0, "whole loads");
+    static_assert((64 * WAVES) % BM == 0 && BM % 64 == 0, "a thread or more for each scale's word");
+    constexpr int SCALES = (BN + BM) * STEP, ROOM = SCALES + (TYPE == DBF_E4M3 ? 4 * BM : 0);   // behind the rows x's scales, a word each: the step's and its neighbours'
+    // (objects of their own: the compiler then knows that a load into one is not read from another)
+    __shared__ __align__(16) uint8_t s0[ROOM], s1[ROOM];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, q = lane >> 4;
+    const int wn = wave % WN, wm = wave / WN;
+    // a compute die (workgroup modulo 8) has neighbouring tiles, up to 8 tiles of rows with the same weights
+    const int total = n_tiles * m_tiles, die = blockIdx.x & 7, slot = blockIdx.x >> 3, per = total >> 3, extra = total & 7;
+    const int id = die * per + min(die, extra) + slot, band = id / (8 * n_tiles), in_band = id - band * 8 * n_tiles, high = min(8, m_tiles - 8 * band);
+    const Tile tile = tile_of(a, 8 * band + in_band % high, BM);
+    if (!tile.rows) return;
+    const int out0 = in_band / high * OUTS;
+    const int steps = a.k_bytes / (2 * STEP) * 2;   // in rounds of two; what is left is done without a lead
+
+    // where a lane's pieces lie, in bytes: of the weights behind the tile's first row, of x behind the tile's first or, where rows are given, behind x's
+    auto x_from = [&](int row) -> int {
+        if (!a.x_rows) return row;
+        const int from = a.x_rows[tile.row + row];
+        return (unsigned)from < (unsigned)a.n_x_rows ? from : 0;
+    };
+    unsigned w_at[W_LOADS], x_at[X_LOADS];
+    const int place = 16 * ((lane & 7) ^ (lane >> 3));
+    const long long x0 = a.x_rows ? 0 : tile.row, w0 = tile.group * a.w_group + out0 * a.w_row;
+#pragma unroll
+    for (int i = 0; i < W_LOADS; ++i) {
+        const int row = 8 * (WAVES * i + wave) + (lane >> 3), n = GATED ? row / 32 * 16 + row % 16 : row;
+        w_at[i] = (unsigned)(min(n, a.n_out - 1 - out0) * (int)a.w_row + place);
+    }
+#pragma unroll
+    for (int i = 0; i < X_LOADS; ++i) {
+        const int row = min(8 * (WAVES * i + wave) + (lane >> 3), tile.rows - 1);
+        x_at[i] = (unsigned)x_from(row) * (unsigned)a.x_row + place;
+    }
+    auto fetch = [&](uint8_t* to, int step, int back) {
+#pragma unroll
+        for (int i = 0; i < W_LOADS; ++i) {
+            const int row = 8 * (WAVES * i + wave);
+            const uint8_t* from = (GATED && row / 16 % 2 ? a.w_up : a.w) + w0 + step * STEP;
+            __builtin_amdgcn_global_load_lds((Global)(from + (w_at[i] - back)), (Shared)(to + row * STEP), 16, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < X_LOADS; ++i) {
+            const uint8_t* from = a.x + x0 * a.x_row + step * STEP;
+            __builtin_amdgcn_global_load_lds((Global)(from + (x_at[i] - back)), (Shared)(to + (BN + 8 * (WAVES * i + wave)) * STEP), 16, 0, 0);
+        }
+    };
+    // scales: those of the rows go through LDS, the words that have a step's bytes; the weights' are the wavefront's
+    unsigned x_scale_at = 0;
+    const uint8_t *w_scale = nullptr, *up_scale = nullptr;
+    if constexpr (TYPE == DBF_E4M3) {
+        x_scale_at = (unsigned)x_from(min((int)threadIdx.x % BM, tile.rows - 1)) * (unsigned)a.x_scale_row;
+        const long long block = tile.group * a.w_scale_group + (min(out0 + (GATED ? 8 : 16) * NS * wn, a.n_out - 1) / DBF_SCALE_BLOCK) * a.w_scale_row;
+        w_scale = static_cast<const uint8_t*>(a.w_scale) + block * (FLOAT ? 4 : 1);
+        up_scale = static_cast<const uint8_t*>(a.w_up_scale) + block * (FLOAT ? 4 : 1);
+    }
+    // (by all wavefronts and in every step, without a branch: it would end the block of instructions, and the compiler then moves products behind it, where the operands
+    // of all of them are alive at once)
+    auto fetch_x_scales = [&](uint8_t* to, int step) {
+        if (TYPE == DBF_E4M3)
+            __builtin_amdgcn_global_load_lds((Global)(a.x_scale + x0 * a.x_scale_row + (step & ~3) + x_scale_at), (Shared)(to + SCALES + 256 * (wave % (BM / 64))), 4, 0, 0);
+    };
+    int ws = 0, us = 0, ws_next = 0, us_next = 0;
+    auto fetch_w_scales = [&](int step) {
+        if constexpr (TYPE == DBF_E4M3) {
+            ws_next = FLOAT ? reinterpret_cast<const int*>(w_scale)[step] : w_scale[step];
+            if constexpr (GATED) us_next = FLOAT ? reinterpret_cast<const int*>(up_scale)[step] : up_scale[step];
+        }
+    };
+    dbf_f4 acc[NS][MS];
+#pragma unroll
+    for (int i = 0; i < NS; ++i)
+#pragma unroll
+        for (int j = 0; j < MS; ++j) acc[i][j] = (dbf_f4){0.f, 0.f, 0.f, 0.f};
+    // pieces q and q + 4 of a row (row % 8 is c % 8)
+    const int at0 = c * STEP + 16 * (q ^ (c & 7)), at1 = at0 ^ 64;
+    auto read = [&](const uint8_t* from) -> v8i { return both(*reinterpret_cast<const dbf_u4*>(from + at0), *reinterpret_cast<const dbf_u4*>(from + at1)); };
+    v8i w[NS], x[3];
+    int xs[3];
+    auto read_w = [&](const uint8_t* from, int i) { w[i] = read(from + 16 * (NS * wn + i) * STEP); };
+    auto read_x = [&](const uint8_t* from, int s, int j, int to) {
+        x[to] = read(from + (BN + 16 * (MS * wm + j)) * STEP);
+        if constexpr (TYPE == DBF_E4M3) {
+            int scale_at = 4 * (16 * MS * wm + c) + (s & 3);
+            asm("" : "+v"(scale_at));   // (rows by the instruction's offset: not an address for each, kept for all steps)
+            xs[to] = from[SCALES + scale_at + 64 * j];
+        } else {
+            xs[to] = 0;
+        }
+    };
+    auto product = [&](int i, int j, int of) {
+        dbf_f4& sum = acc[i][j];
+        const int scale = GATED && i % 2 ? us : ws;
+        if constexpr (EXACT) {
+            dbf_h8 wide[4], rows[4];
+            widen(w[i], wide);
+            widen(x[of], rows);
+            dbf_f4 p = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) p = __builtin_amdgcn_mfma_f32_16x16x32_f16(wide[k], rows[k], p, 0, 0, 0);
+            const float by = FLOAT ? __builtin_bit_cast(float, scale) : scale_of(scale), row_scale = scale_of(xs[of]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[e] = fmaf(p[e] * row_scale, by, sum[e]);
+        } else {
+            multiply<TYPE, FLOAT>(sum, w[i], x[of], scale, xs[of]);
+        }
+    };
+    auto meet = [&]() {
+        __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt = 0, lgkmcnt = 0
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    // In rows of 16: a step's first is in place ODD of x, the next one in the other, and so on in turn; the last in place 2, so that the next step's first has the place of
+    // the last but two.
+    auto step = [&](uint8_t* now, uint8_t* next, int s, auto odd) {
+        constexpr int ODD = decltype(odd)::value;
+        const int after = min(s + 1, steps - 1);   // (behind the last step that one again, so that no round has other loads under way than another)
+        fetch_w_scales(after);
+#pragma unroll
+        for (int j = 0; j + 2 < MS; ++j) {
+            read_x(now, s, j + 1, (j + 1) % 2 ^ ODD);
+            if (j + 3 == MS) read_x(now, s, MS - 1, 2);
+#pragma unroll
+            for (int i = 0; i < NS; ++i) product(i, j, j % 2 ^ ODD);
+            __builtin_amdgcn_sched_barrier(0);   // (else all reads go first, and their registers are too many)
+        }
+        meet();
+        fetch(now, min(s + 2, steps - 1), 0);
+        fetch_x_scales(now, min(s + 2, steps - 1));
+        read_x(next, after, 0, 1 - ODD);
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+            product(i, MS - 2, ODD);
+            product(i, MS - 1, 2);
+            read_w(next, i);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        ws = ws_next;
+        us = us_next;
+    };
+    static_assert(MS % 2 == 0 && MS >= 4, "");
+    if (steps) {
+        fetch_w_scales(0);
+        fetch(s0, 0, 0);
+        fetch_x_scales(s0, 0);
+        meet();
+        fetch(s1, 1, 0);
+        fetch_x_scales(s1, 1);
+        ws = ws_next;
+        us = us_next;
+        read_x(s0, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < NS; ++i) read_w(s0, i);
+        for (int s = 0; s < steps; s += 2) {
+            step(s0, s1, s, std::integral_constant<int, 0>());
+            step(s1, s0, s + 1, std::integral_constant<int, 1>());
+        }
+    }
+    for (int s = steps; s * STEP < a.k_bytes; ++s) {
+        // What is behind the rows' end becomes zeros, of both (a code there may be no number).  Pieces that lie there are not read: the row's first of the step in their place.
+        const int rest = a.k_bytes - s * STEP;
+        meet();
+        fetch(s0, s, place < rest ? 0 : place);
+        fetch_x_scales(s0, s);
+        fetch_w_scales(s);
+        meet();
+        for (int i = threadIdx.x; i < (BN + BM) * 8; i += 64 * WAVES) {
+            const int row = i >> 3, have = rest - 16 * ((i ^ row) & 7);
+            if (have < 16) {
+                dbf_u4 v = *reinterpret_cast<dbf_u4*>(s0 + 16 * i);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = have <= 4 * e ? 0u : have >= 4 * e + 4 ? v[e] : v[e] & (0xFFFFFFFFu >> (32 - 8 * (have - 4 * e)));
+                *reinterpret_cast<dbf_u4*>(s0 + 16 * i) = v;
+            }
+        }
+        __syncthreads();
+        ws = ws_next;
+        us = us_next;
+#pragma unroll
+        for (int i = 0; i < NS; ++i) read_w(s0, i);
+#pragma unroll
+        for (int j = 0; j < MS; ++j) {
+            read_x(s0, s, j, 0);
+#pragma unroll
+            for (int i = 0; i < NS; ++i) product(i, j, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    __builtin_amdgcn_s_waitcnt(0x0070);
+#pragma unroll
+    for (int j = 0; j < MS; ++j) {
+        const int r = 16 * (MS * wm + j) + c, row = tile.row + r;
+        if (r >= tile.rows) continue;
+        const bool known = !a.x_rows || (unsigned)a.x_rows[row] < (unsigned)a.n_x_rows;
+#pragma unroll
+        for (int i = 0; i < NS; i += GATED ? 2 : 1) {
+            const int n = out0 + (GATED ? 8 * NS * wn + 8 * i : 16 * (NS * wn + i)) + 4 * q;
+            dbf_f4 v = acc[i][j];
+            if constexpr (GATED) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = gate(v[e], acc[i + 1][j][e]);
+            }
+            if (!known) v = (dbf_f4){0.f, 0.f, 0.f, 0.f};
+            if (n < a.n_out) store4(a, row, n, v);
+        }
+    }
+}
+
+template <int TYPE, bool FLOAT, bool GATED, bool EXACT, int BN, int BM, int WN, int WM, int EACH>
+int launch(const DenseArgs& a, hipStream_t stream) {
+    constexpr int OUTS = GATED ? BN / 2 : BN;
+    const long long m_tiles = (a.n_rows + BM - 1LL) / BM + (a.starts ? std::min(a.n_groups, a.n_rows) : 0), n_tiles = (a.n_out + OUTS - 1) / OUTS;
+    if (m_tiles * n_tiles > INT_MAX / 512) return DBF_EINVAL;
+    hipLaunchKernelGGL((dbf_dense_tiles_kernel<TYPE, FLOAT, GATED, EXACT, BN, BM, WN, WM, EACH>), dim3((unsigned)(m_tiles * n_tiles)), dim3(64 * WN * WM), 0, stream, a, (int)n_tiles,
+                       (int)m_tiles);
+    return hipGetLastError() == hipSuccess ? DBF_OK : DBF_EHIP;
+}
+template <int TYPE, bool FLOAT, bool EXACT>
+int launch(const DenseArgs& a, hipStream_t stream) {
+    constexpr int BN = EXACT ? 128 : 256, BM = EXACT ? 128 : FLOAT ? 256 : 256, WN = EXACT ? 2 : 4, EACH = EXACT ? 1 : 2;
+    return a.w_up ? launch<TYPE, FLOAT, true, EXACT, BN, BM, WN, 2, EACH>(a, stream) : launch<TYPE, FLOAT, false, EXACT, BN, BM, WN, 2, EACH>(a, stream);
+}
+
+}  // namespace
+
+int dbf_dense_tiles(const void* args, int type, bool float_scales, hipStream_t stream) {
+    const DenseArgs& a = *static_cast<const DenseArgs*>(args);
+    if (type == DBF_F16) return launch<DBF_F16, false, false>(a, stream);
+    if (type == DBF_BF16) return launch<DBF_BF16, false, false>(a, stream);
+    if (a.out_dtype == DBF_F32) return float_scales ? launch<DBF_E4M3, true, true>(a, stream) : launch<DBF_E4M3, false, true>(a, stream);
+    return float_scales ? launch<DBF_E4M3, true, false>(a, stream) : launch<DBF_E4M3, false, false>(a, stream);
+}
