@@ -8,52 +8,161 @@
 
 namespace {
 
-// 16 outputs of 16 rows to a wavefront.
-constexpr int ROWS = 16, WAVES = 4;
-template <int TYPE, bool FLOAT, bool GATED>
-__global__ __launch_bounds__(64 * WAVES) void dbf_dense_kernel(const DenseArgs a) {
+// Few rows: a workgroup has 16 NS weights (gated: of each matrix) and 16 MS rows; its wavefronts have every KW-th four steps of them, and their sums meet in LDS.  Operands come
+// straight from memory as the matrix cores take them: of four steps 512 bytes of a row, four steps' loads under way at a time.
+constexpr int GROUP = 4;   // steps
+template <int TYPE, bool FLOAT, bool GATED, bool EXACT, int NS, int MS, int KW>
+__global__ __launch_bounds__(64 * KW) void dbf_dense_few_kernel(const DenseArgs a) {
+    constexpr int ROWS = 16 * MS, N = GATED ? 2 * NS : NS;   // N: sets of 16 weights
+    __shared__ dbf_f4 sums[KW > 1 ? KW - 1 : 1][N * MS][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, q = lane >> 4;
-    const int n0 = 16 * (WAVES * blockIdx.x + wave);
+    const int out0 = 16 * NS * blockIdx.x;
     for (int t = blockIdx.y;; t += gridDim.y) {
         const Tile tile = tile_of(a, t, ROWS);
         if (!tile.rows) return;
-        if (n0 >= a.n_out) continue;
-        const int row = tile.row + min(c, tile.rows - 1);
-        int from = a.x_rows ? a.x_rows[row] : row;
-        const bool known = (unsigned)from < (unsigned)a.n_x_rows;
-        if (!known) from = 0;
-        const uint8_t* x = a.x + from * a.x_row;
-        const uint8_t* x_scale = a.x_scale + from * a.x_scale_row;
-        const long long n = min(n0 + c, a.n_out - 1), block = tile.group * a.w_scale_group + (n0 / DBF_SCALE_BLOCK) * a.w_scale_row;
-        const uint8_t* w = a.w + tile.group * a.w_group + n * a.w_row;
-        const uint8_t* up = GATED ? a.w_up + tile.group * a.w_group + n * a.w_row : nullptr;
-        auto scale = [&](const void* s, int b) -> int {
-            return FLOAT ? static_cast<const int*>(s)[block + b] : static_cast<const uint8_t*>(s)[block + b];
+        const uint8_t *x[MS], *x_scale[MS], *w[N];
+        const uint8_t* w_scale[N];
+#pragma unroll
+        for (int j = 0; j < MS; ++j) {
+            const int row = tile.row + min(16 * j + c, tile.rows - 1);
+            int from = a.x_rows ? a.x_rows[row] : row;
+            if ((unsigned)from >= (unsigned)a.n_x_rows) from = 0;
+            x[j] = a.x + from * a.x_row;
+            x_scale[j] = a.x_scale + from * a.x_scale_row;
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int n0 = out0 + 16 * (GATED ? i / 2 : i);
+            const bool up = GATED && i % 2;
+            w[i] = (up ? a.w_up : a.w) + tile.group * a.w_group + min(n0 + c, a.n_out - 1) * a.w_row;
+            const long long block = tile.group * a.w_scale_group + (min(n0, a.n_out - 1) / DBF_SCALE_BLOCK) * a.w_scale_row;
+            w_scale[i] = static_cast<const uint8_t*>(up ? a.w_up_scale : a.w_scale) + block * (FLOAT ? 4 : 1);
+        }
+        dbf_f4 acc[N][MS];
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int j = 0; j < MS; ++j) acc[i][j] = (dbf_f4){0.f, 0.f, 0.f, 0.f};
+        // (scales as they lie: bytes, or fp32 numbers' bits)
+        auto products = [&](const v8i (&ws)[N], const v8i (&xs)[MS], const int (&scale_w)[N], const int (&scale_x)[MS]) {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+#pragma unroll
+                for (int j = 0; j < MS; ++j) {
+                    if constexpr (EXACT) multiply_exactly<FLOAT>(acc[i][j], ws[i], xs[j], scale_w[i], scale_x[j]);
+                    else multiply<TYPE, FLOAT>(acc[i][j], ws[i], xs[j], scale_w[i], scale_x[j]);
+                }
         };
-        dbf_f4 acc = {0.f, 0.f, 0.f, 0.f}, acc_up = {0.f, 0.f, 0.f, 0.f};
-        for (int k = 0, b = 0; k < a.k_bytes; k += STEP, ++b) {
-            const int at0 = k + 16 * q, at1 = at0 + 64;
-            const v8i xs = both(piece(x, at0, a.k_bytes), piece(x, at1, a.k_bytes)), ws = both(piece(w, at0, a.k_bytes), piece(w, at1, a.k_bytes));
-            const int sx = TYPE == DBF_E4M3 ? x_scale[b] : 0;
-            multiply<TYPE, FLOAT>(acc, ws, xs, TYPE == DBF_E4M3 ? scale(a.w_scale, b) : 0, sx);
-            if constexpr (GATED) {
-                const v8i us = both(piece(up, at0, a.k_bytes), piece(up, at1, a.k_bytes));
-                multiply<TYPE, FLOAT>(acc_up, us, xs, TYPE == DBF_E4M3 ? scale(a.w_up_scale, b) : 0, sx);
+        auto weight_scale = [&](int i, int s) -> int {
+            if constexpr (TYPE != DBF_E4M3) return 0;
+            return FLOAT ? reinterpret_cast<const int*>(w_scale[i])[s] : w_scale[i][s];
+        };
+        const int steps = a.k_bytes / STEP;
+        int s = GROUP * wave;
+        for (; s + GROUP <= steps; s += GROUP * KW) {
+            v8i ws[GROUP][N], xs[GROUP][MS];
+            int scale_w[GROUP][N];
+            unsigned word[MS];
+#pragma unroll
+            for (int g = 0; g < GROUP; ++g) {
+                const int at = (s + g) * STEP + 16 * q;
+#pragma unroll
+                for (int i = 0; i < N; ++i) ws[g][i] = both(*reinterpret_cast<const dbf_u4*>(w[i] + at), *reinterpret_cast<const dbf_u4*>(w[i] + at + 64));
+#pragma unroll
+                for (int j = 0; j < MS; ++j) xs[g][j] = both(*reinterpret_cast<const dbf_u4*>(x[j] + at), *reinterpret_cast<const dbf_u4*>(x[j] + at + 64));
+#pragma unroll
+                for (int i = 0; i < N; ++i) scale_w[g][i] = weight_scale(i, s + g);
+            }
+            if constexpr (TYPE == DBF_E4M3) {
+#pragma unroll
+                for (int j = 0; j < MS; ++j) word[j] = *reinterpret_cast<const unsigned*>(x_scale[j] + s);
+            }
+#pragma unroll
+            for (int g = 0; g < GROUP; ++g) {
+                int scale_x[MS];
+#pragma unroll
+                for (int j = 0; j < MS; ++j) scale_x[j] = TYPE == DBF_E4M3 ? word[j] >> (8 * g) & 255 : 0;
+                products(ws[g], xs[g], scale_w[g], scale_x);
             }
         }
-        if constexpr (GATED)
-            for (int i = 0; i < 4; ++i) acc[i] = gate(acc[i], acc_up[i]);
-        if (!known) acc = (dbf_f4){0.f, 0.f, 0.f, 0.f};
-        if (c < tile.rows && n0 + 4 * q < a.n_out) store4(a, tile.row + c, n0 + 4 * q, acc);
+        // what is left of the wavefront's last four steps
+        for (int g = 0; g < GROUP && (s + g) * STEP < a.k_bytes; ++g) {
+            const int at = (s + g) * STEP + 16 * q;
+            v8i ws[N], xs[MS];
+            int scale_w[N], scale_x[MS];
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                ws[i] = both(piece(w[i], at, a.k_bytes), piece(w[i], at + 64, a.k_bytes));
+                scale_w[i] = weight_scale(i, s + g);
+            }
+#pragma unroll
+            for (int j = 0; j < MS; ++j) {
+                xs[j] = both(piece(x[j], at, a.k_bytes), piece(x[j], at + 64, a.k_bytes));
+                scale_x[j] = TYPE == DBF_E4M3 ? x_scale[j][s + g] : 0;
+            }
+            products(ws, xs, scale_w, scale_x);
+        }
+        if (KW > 1) {
+            if (wave) {
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+#pragma unroll
+                    for (int j = 0; j < MS; ++j) sums[wave - 1][i * MS + j][lane] = acc[i][j];
+            }
+            __syncthreads();
+            if (!wave) {
+#pragma unroll
+                for (int k = 0; k < KW - 1; ++k)
+#pragma unroll
+                    for (int i = 0; i < N; ++i)
+#pragma unroll
+                        for (int j = 0; j < MS; ++j) acc[i][j] += sums[k][i * MS + j][lane];
+            }
+        }
+        if (!wave) {
+#pragma unroll
+            for (int j = 0; j < MS; ++j) {
+                const int r = 16 * j + c, row = tile.row + r;
+                if (r >= tile.rows) continue;
+                const bool known = !a.x_rows || (unsigned)a.x_rows[row] < (unsigned)a.n_x_rows;
+#pragma unroll
+                for (int i = 0; i < NS; ++i) {
+                    const int n = out0 + 16 * i + 4 * q;
+                    dbf_f4 v = acc[GATED ? 2 * i : i][j];
+                    if constexpr (GATED) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[e] = gate(v[e], acc[2 * i + 1][j][e]);
+                    }
+                    if (!known) v = (dbf_f4){0.f, 0.f, 0.f, 0.f};
+                    if (n < a.n_out) store4(a, row, n, v);
+                }
+            }
+        }
+        if (KW > 1) __syncthreads();   // (the sums have been read)
     }
 }
 
+template <int TYPE, bool FLOAT, bool GATED, bool EXACT, int NS, int MS, int KW>
+int launch(const DenseArgs& a, hipStream_t stream) {
+    const long long tiles = (a.n_rows + 16LL * MS - 1) / (16 * MS) + (a.starts ? std::min(a.n_groups, a.n_rows) : 0);
+    const dim3 grid((unsigned)((a.n_out + 16 * NS - 1) / (16 * NS)), (unsigned)std::min(tiles, 4096LL));
+    hipLaunchKernelGGL((dbf_dense_few_kernel<TYPE, FLOAT, GATED, EXACT, NS, MS, KW>), grid, dim3(64 * KW), 0, stream, a);
+    return hipGetLastError() == hipSuccess ? DBF_OK : DBF_EHIP;
+}
+template <int TYPE, bool FLOAT, bool GATED, bool EXACT>
+int launch(const DenseArgs& a, hipStream_t stream) {
+    const long long each = a.starts ? (a.n_rows + a.n_groups - 1) / a.n_groups : a.n_rows;
+    const long long units = (a.n_out + 15) / 16 * (a.starts ? std::min(a.n_groups, a.n_rows) : 1);   // of 16 outputs
+    if (each > 32) return launch<TYPE, FLOAT, GATED, EXACT, 1, 4, 4>(a, stream);
+    if (each > 16) return launch<TYPE, FLOAT, GATED, EXACT, 1, 2, 4>(a, stream);
+    if (units >= 2048) return launch<TYPE, FLOAT, GATED, EXACT, GATED ? 1 : 2, 1, 4>(a, stream);
+    return launch<TYPE, FLOAT, GATED, EXACT, 1, 1, 8>(a, stream);
+}
 template <int TYPE, bool FLOAT, bool GATED>
 int launch(const DenseArgs& a, hipStream_t stream) {
-    const long long tiles = (a.n_rows + ROWS - 1LL) / ROWS + (a.starts ? std::min(a.n_groups, a.n_rows) : 0);
-    const dim3 grid((unsigned)((a.n_out + 16 * WAVES - 1) / (16 * WAVES)), (unsigned)std::min(tiles, 4096LL));
-    hipLaunchKernelGGL((dbf_dense_kernel<TYPE, FLOAT, GATED>), grid, dim3(64 * WAVES), 0, stream, a);
-    return hipGetLastError() == hipSuccess ? DBF_OK : DBF_EHIP;
+    if constexpr (TYPE == DBF_E4M3)
+        if (a.out_dtype == DBF_F32) return launch<TYPE, FLOAT, GATED, true>(a, stream);
+    return launch<TYPE, FLOAT, GATED, false>(a, stream);
 }
 template <int TYPE, bool FLOAT>
 int launch(const DenseArgs& a, hipStream_t stream) {
@@ -119,7 +228,7 @@ int run(const dbf_dense* p, bool grouped, hipStream_t stream) {
     a.n_out = p->n_out;
     a.n_groups = grouped ? p->n_groups : 0;
     a.quads = p->y_stride % 4 == 0 && !dbf_misaligned(p->y, quad);
-    if (a.n_rows > 16 * std::max(a.n_groups, 1)) return dbf_dense_tiles(&a, p->dtype, p->w_scale_type == DBF_F32, stream);
+    if (a.n_rows > 64 * std::max(a.n_groups, 1)) return dbf_dense_tiles(&a, p->dtype, p->w_scale_type == DBF_F32, stream);
     if (p->dtype == DBF_F16) return launch<DBF_F16, false>(a, stream);
     if (p->dtype == DBF_BF16) return launch<DBF_BF16, false>(a, stream);
     return p->w_scale_type == DBF_F32 ? launch<DBF_E4M3, true>(a, stream) : launch<DBF_E4M3, false>(a, stream);

@@ -23,10 +23,11 @@ __global__ __launch_bounds__(64 * WN * WM) __attribute__((amdgpu_waves_per_eu(EA
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, q = lane >> 4;
     const int wn = wave % WN, wm = wave / WN;
     // a compute die (workgroup modulo 8) has neighbouring tiles, up to 8 tiles of rows with the same weights
+    if (a.starts) m_tiles = tiles_of(a, BM);
     const int total = n_tiles * m_tiles, die = blockIdx.x & 7, slot = blockIdx.x >> 3, per = total >> 3, extra = total & 7;
+    if (slot >= per + (die < extra ? 1 : 0)) return;
     const int id = die * per + min(die, extra) + slot, band = id / (8 * n_tiles), in_band = id - band * 8 * n_tiles, high = min(8, m_tiles - 8 * band);
     const Tile tile = tile_of(a, 8 * band + in_band % high, BM);
-    if (!tile.rows) return;
     const int out0 = in_band / high * OUTS;
     const int steps = a.k_bytes / (2 * STEP) * 2;   // in rounds of two; what is left is done without a lead
 
@@ -108,19 +109,8 @@ __global__ __launch_bounds__(64 * WN * WM) __attribute__((amdgpu_waves_per_eu(EA
     auto product = [&](int i, int j, int of) {
         dbf_f4& sum = acc[i][j];
         const int scale = GATED && i % 2 ? us : ws;
-        if constexpr (EXACT) {
-            dbf_h8 wide[4], rows[4];
-            widen(w[i], wide);
-            widen(x[of], rows);
-            dbf_f4 p = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int k = 0; k < 4; ++k) p = __builtin_amdgcn_mfma_f32_16x16x32_f16(wide[k], rows[k], p, 0, 0, 0);
-            const float by = FLOAT ? __builtin_bit_cast(float, scale) : scale_of(scale), row_scale = scale_of(xs[of]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) sum[e] = fmaf(p[e] * row_scale, by, sum[e]);
-        } else {
-            multiply<TYPE, FLOAT>(sum, w[i], x[of], scale, xs[of]);
-        }
+        if constexpr (EXACT) multiply_exactly<FLOAT>(sum, w[i], x[of], scale, xs[of]);
+        else multiply<TYPE, FLOAT>(sum, w[i], x[of], scale, xs[of]);
     };
     auto meet = [&]() {
         __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt = 0, lgkmcnt = 0
