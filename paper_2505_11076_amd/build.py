@@ -36,6 +36,7 @@ SOURCES = [
     "dbf_fp8.hip",
     "dbf_dense.hip",
     "dbf_dense_tiles.hip",
+    "dbf_dense_stream.hip",
     "dbf_route.hip",
 ]
 

@@ -56,7 +56,7 @@ __device__ __forceinline__ Tile tile_of(const DenseArgs& a, int tile, int of_row
         if (past) {
             const int l = __builtin_ctzll(past);
             const int row = __builtin_amdgcn_readlane(from, l) + (tile - before - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(tiles, l))) * of_rows;
-            return {g0 + l, row, min(of_rows, __builtin_amdgcn_readlane(to, l) - row)};
+            return {g0 + l, row, min(of_rows, __builtin_amdgcn_readlane(to, l) - row)};   // (scalars)
         }
         before += __builtin_amdgcn_readlane(upto, 63);
     }
@@ -163,7 +163,9 @@ __device__ __forceinline__ void store4(const DenseArgs& a, int row, int n, const
 
 }  // namespace
 
-// 0: done; else DBF_EHIP.  (dbf_dense_tiles.hip)
+// What launches them: `args` is a DenseArgs, `type` that of the operands.
 int dbf_dense_tiles(const void* args, int type, bool float_scales, hipStream_t stream);
+int dbf_dense_stream(const void* args, int type, bool float_scales, hipStream_t stream);
+bool dbf_dense_streams(int k_bytes);   // whether rows of so many bytes fit the latter
 
 #endif  // DBF_DENSE_H

@@ -153,7 +153,6 @@ template <int TYPE, bool FLOAT, bool GATED, bool EXACT>
 int launch(const DenseArgs& a, hipStream_t stream) {
     const long long each = a.starts ? (a.n_rows + a.n_groups - 1) / a.n_groups : a.n_rows;
     const long long units = (a.n_out + 15) / 16 * (a.starts ? std::min(a.n_groups, a.n_rows) : 1);   // of 16 outputs
-    if (each > 32) return launch<TYPE, FLOAT, GATED, EXACT, 1, 4, 4>(a, stream);
     if (each > 16) return launch<TYPE, FLOAT, GATED, EXACT, 1, 2, 4>(a, stream);
     if (units >= 2048) return launch<TYPE, FLOAT, GATED, EXACT, GATED ? 1 : 2, 1, 4>(a, stream);
     return launch<TYPE, FLOAT, GATED, EXACT, 1, 1, 8>(a, stream);
@@ -228,10 +227,17 @@ int run(const dbf_dense* p, bool grouped, hipStream_t stream) {
     a.n_out = p->n_out;
     a.n_groups = grouped ? p->n_groups : 0;
     a.quads = p->y_stride % 4 == 0 && !dbf_misaligned(p->y, quad);
-    if (a.n_rows > 64 * std::max(a.n_groups, 1)) return dbf_dense_tiles(&a, p->dtype, p->w_scale_type == DBF_F32, stream);
+    const bool fp32_scales = p->w_scale_type == DBF_F32;
+    const double weights = (double)std::min(std::max(a.n_groups, 1), a.n_rows) * a.n_out * a.k_bytes * (a.w_up ? 2 : 1);
+    // (us, 8 bits)  Weights that no cache holds stream past few rows: 4 rows, 64 MB 15.4 for 17.1 by the kernel for few rows, 134 MB 25 for 33, but 32 MB 10.1 for 10.0.  Of groups with 4 rows on
+    // average some have more than 16, whose weights are read twice: 268 MB of 64 groups with 4 rows each 44.2 for 43.8 by tiles, with 8 49 for 45, with 1 26.5 for 28 (147 MB).
+    const long long each = a.starts ? (a.n_rows + a.n_groups - 1LL) / a.n_groups : a.n_rows;
+    if (each <= (a.starts ? 4 : 16) && weights >= (64 << 20) && dbf_dense_streams(a.k_bytes)) return dbf_dense_stream(&a, p->dtype, fp32_scales, stream);
+    // Few rows' operands straight from memory: 24 rows of 4096 x 4096 9.4 for 11.7 by tiles, 48 rows 13.0 for 12.3, 24 rows of 16384 x 4096 23.4 for 19.9.
+    if (each > 32 || (each > 16 && weights > (32 << 20)) || (a.starts && each > 4 && weights > (32 << 20))) return dbf_dense_tiles(&a, p->dtype, fp32_scales, stream);
     if (p->dtype == DBF_F16) return launch<DBF_F16, false>(a, stream);
     if (p->dtype == DBF_BF16) return launch<DBF_BF16, false>(a, stream);
-    return p->w_scale_type == DBF_F32 ? launch<DBF_E4M3, true>(a, stream) : launch<DBF_E4M3, false>(a, stream);
+    return fp32_scales ? launch<DBF_E4M3, true>(a, stream) : launch<DBF_E4M3, false>(a, stream);
 }
 
 }  // namespace

@@ -1,6 +1,8 @@
 // Products with ordinary weights, many rows: tiles of weights and rows in LDS (include/dbf.h: dbf_dense_gemm, dbf_grouped_gemm; dbf_dense.h: the instructions).
 #include "dbf_dense.h"
 
+#include <cmath>
+
 namespace {
 
 typedef const __attribute__((address_space(1))) unsigned* Global;
@@ -223,10 +225,30 @@ int launch(const DenseArgs& a, hipStream_t stream) {
                        (int)m_tiles);
     return hipGetLastError() == hipSuccess ? DBF_OK : DBF_EHIP;
 }
+// What a launch costs, in us a step, by how many tiles it has: `full` where all places of the chip have one, `alone` for the first; measured with 4096 values in 8 bits (24 .. 2048 rows by 4096 and
+// 16384 outputs).  256 x 256: 512 rows by 16384 53 us, 1024 63, 2048 120.  128 x 128: 27 / 75 / 143 (512 rows 40).  128 x 64: 64 rows by 16384 26, 256 28, 512 52.  64 x 64: 64 rows by 4096 13,
+// 512 21, 1024 34, 128 rows by 16384 22.  Of a group's last tile half is taken to be empty.
+double cost_of(const DenseArgs& a, int outs, int rows, int places, double alone, double full) {
+    const double groups = a.starts ? std::min(a.n_groups, a.n_rows) : 1, each = a.n_rows / groups;
+    const double m_tiles = groups * (a.starts ? std::max(1.0, each / rows + 0.5) : std::ceil(each / rows));
+    const double tiles = m_tiles * ((a.n_out + outs - 1) / outs), rounds = std::floor(tiles / places), left = tiles / places - rounds;
+    return rounds * full + (left > 0 ? alone + (full - alone) * left : 0);
+}
+template <int TYPE, bool FLOAT, bool GATED, bool EXACT>
+int launch(const DenseArgs& a, hipStream_t stream) {
+    constexpr int OF = GATED ? 2 : 1;
+    const double large = EXACT ? 1e30 : cost_of(a, 256 / OF, 256, 256, 1.5, 1.85), square = cost_of(a, 128 / OF, 128, 512, 0.75, 1.2);
+    const double low = cost_of(a, 128 / OF, 64, 768, 0.62, 1.1), small = cost_of(a, 64 / OF, 64, 1024, 0.4, 1.0);
+    const double least = std::min({large, square, low, small});
+    if constexpr (!EXACT)   // (in fp16 its operands have no registers)
+        if (large <= least) return launch<TYPE, FLOAT, GATED, EXACT, 256, 256, 4, 2, 2>(a, stream);
+    if (square <= least) return launch<TYPE, FLOAT, GATED, EXACT, 128, 128, 2, 2, EXACT ? 1 : 2>(a, stream);
+    if (low <= least) return launch<TYPE, FLOAT, GATED, EXACT, 128, 64, 4, 1, 2>(a, stream);
+    return launch<TYPE, FLOAT, GATED, EXACT, 64, 64, 2, 1, 2>(a, stream);
+}
 template <int TYPE, bool FLOAT, bool EXACT>
 int launch(const DenseArgs& a, hipStream_t stream) {
-    constexpr int BN = EXACT ? 128 : 256, BM = EXACT ? 128 : FLOAT ? 256 : 256, WN = EXACT ? 2 : 4, EACH = EXACT ? 1 : 2;
-    return a.w_up ? launch<TYPE, FLOAT, true, EXACT, BN, BM, WN, 2, EACH>(a, stream) : launch<TYPE, FLOAT, false, EXACT, BN, BM, WN, 2, EACH>(a, stream);
+    return a.w_up ? launch<TYPE, FLOAT, true, EXACT>(a, stream) : launch<TYPE, FLOAT, false, EXACT>(a, stream);
 }
 
 }  // namespace
