@@ -31,7 +31,7 @@ __global__ __launch_bounds__(64 * WN * WM) __attribute__((amdgpu_waves_per_eu(EA
     const int id = die * per + min(die, extra) + slot, band = id / (8 * n_tiles), in_band = id - band * 8 * n_tiles, high = min(8, m_tiles - 8 * band);
     const Tile tile = tile_of(a, 8 * band + in_band % high, BM);
     const int out0 = in_band / high * OUTS;
-    const int steps = a.k_bytes / (2 * STEP) * 2;   // in rounds of two; what is left is done without a lead
+    const int steps = a.k_bytes / (2 * STEP) * 2, all_steps = (a.k_bytes + STEP - 1) / STEP, last = all_steps - 1;   // steps: in rounds of two; up to two are left
 
     // where a lane's pieces lie, in bytes: of the weights behind the tile's first row, of x behind the tile's first or, where rows are given, behind x's
     auto x_from = [&](int row) -> int {
@@ -52,7 +52,10 @@ __global__ __launch_bounds__(64 * WN * WM) __attribute__((amdgpu_waves_per_eu(EA
         const int row = min(8 * (WAVES * i + wave) + (lane >> 3), tile.rows - 1);
         x_at[i] = (unsigned)x_from(row) * (unsigned)a.x_row + place;
     }
-    auto fetch = [&](uint8_t* to, int step, int back) {
+    // (of the last step the pieces behind the rows' end are not read: the row's first of the step in their place, which zeros overwrite)
+    const int behind = last * STEP + place < a.k_bytes ? 0 : place;
+    auto fetch = [&](uint8_t* to, int step) {
+        const int back = step == last ? behind : 0;
 #pragma unroll
         for (int i = 0; i < W_LOADS; ++i) {
             const int row = 8 * (WAVES * i + wave);
@@ -124,7 +127,7 @@ __global__ __launch_bounds__(64 * WN * WM) __attribute__((amdgpu_waves_per_eu(EA
     // the last but two.
     auto step = [&](uint8_t* now, uint8_t* next, int s, auto odd) {
         constexpr int ODD = decltype(odd)::value;
-        const int after = min(s + 1, steps - 1);   // (behind the last step that one again, so that no round has other loads under way than another)
+        const int after = min(s + 1, last);   // (behind the last step that one again, so that no round has other loads under way than another)
         fetch_w_scales(after);
 #pragma unroll
         for (int j = 0; j + 2 < MS; ++j) {
@@ -135,8 +138,8 @@ __global__ __launch_bounds__(64 * WN * WM) __attribute__((amdgpu_waves_per_eu(EA
             __builtin_amdgcn_sched_barrier(0);   // (else all reads go first, and their registers are too many)
         }
         meet();
-        fetch(now, min(s + 2, steps - 1), 0);
-        fetch_x_scales(now, min(s + 2, steps - 1));
+        fetch(now, min(s + 2, last));
+        fetch_x_scales(now, min(s + 2, last));
         read_x(next, after, 0, 1 - ODD);
 #pragma unroll
         for (int i = 0; i < NS; ++i) {
@@ -149,12 +152,12 @@ __global__ __launch_bounds__(64 * WN * WM) __attribute__((amdgpu_waves_per_eu(EA
         us = us_next;
     };
     static_assert(MS % 2 == 0 && MS >= 4, "");
+    fetch_w_scales(0);
+    fetch(s0, 0);
+    fetch_x_scales(s0, 0);
     if (steps) {
-        fetch_w_scales(0);
-        fetch(s0, 0, 0);
-        fetch_x_scales(s0, 0);
         meet();
-        fetch(s1, 1, 0);
+        fetch(s1, 1);
         fetch_x_scales(s1, 1);
         ws = ws_next;
         us = us_next;
@@ -165,37 +168,41 @@ __global__ __launch_bounds__(64 * WN * WM) __attribute__((amdgpu_waves_per_eu(EA
             step(s0, s1, s, std::integral_constant<int, 0>());
             step(s1, s0, s + 1, std::integral_constant<int, 1>());
         }
+    } else {
+        fetch(s1, min(1, last));
+        fetch_x_scales(s1, min(1, last));
     }
-    for (int s = steps; s * STEP < a.k_bytes; ++s) {
-        // What is behind the rows' end becomes zeros, of both (a code there may be no number).  Pieces that lie there are not read: the row's first of the step in their place.
-        const int rest = a.k_bytes - s * STEP;
-        meet();
-        fetch(s0, s, place < rest ? 0 : place);
-        fetch_x_scales(s0, s);
+    // What is left, which has set out already.  Behind the rows' end it becomes zeros, of both operands (a code there may be no number).
+    auto left = [&](uint8_t* of, int s) {
+        const int have_all = a.k_bytes - s * STEP;
         fetch_w_scales(s);
         meet();
-        for (int i = threadIdx.x; i < (BN + BM) * 8; i += 64 * WAVES) {
-            const int row = i >> 3, have = rest - 16 * ((i ^ row) & 7);
-            if (have < 16) {
-                dbf_u4 v = *reinterpret_cast<dbf_u4*>(s0 + 16 * i);
+        if (have_all < STEP) {
+            for (int i = threadIdx.x; i < (BN + BM) * 8; i += 64 * WAVES) {
+                const int row = i >> 3, have = have_all - 16 * ((i ^ row) & 7);
+                if (have < 16) {
+                    dbf_u4 v = *reinterpret_cast<dbf_u4*>(of + 16 * i);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = have <= 4 * e ? 0u : have >= 4 * e + 4 ? v[e] : v[e] & (0xFFFFFFFFu >> (32 - 8 * (have - 4 * e)));
-                *reinterpret_cast<dbf_u4*>(s0 + 16 * i) = v;
+                    for (int e = 0; e < 4; ++e) v[e] = have <= 4 * e ? 0u : have >= 4 * e + 4 ? v[e] : v[e] & (0xFFFFFFFFu >> (32 - 8 * (have - 4 * e)));
+                    *reinterpret_cast<dbf_u4*>(of + 16 * i) = v;
+                }
             }
+            __syncthreads();
         }
-        __syncthreads();
         ws = ws_next;
         us = us_next;
 #pragma unroll
-        for (int i = 0; i < NS; ++i) read_w(s0, i);
+        for (int i = 0; i < NS; ++i) read_w(of, i);
 #pragma unroll
         for (int j = 0; j < MS; ++j) {
-            read_x(s0, s, j, 0);
+            read_x(of, s, j, 0);
 #pragma unroll
             for (int i = 0; i < NS; ++i) product(i, j, 0);
             __builtin_amdgcn_sched_barrier(0);
         }
-    }
+    };
+    if (steps < all_steps) left(s0, steps);
+    if (steps + 1 < all_steps) left(s1, steps + 1);
     __builtin_amdgcn_s_waitcnt(0x0070);
 #pragma unroll
     for (int j = 0; j < MS; ++j) {
