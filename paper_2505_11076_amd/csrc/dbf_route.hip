@@ -13,7 +13,7 @@ typedef unsigned long long u64;
 
 // ---- the choice ------------------------------------------------------------------------------------------------
 
-constexpr int THREADS = 512, WAVES = THREADS / 64, CHUNK = 32, MOST_TOP = 32;   // CHUNK: tokens of a workgroup; a bit of a word for each
+constexpr int THREADS = 1024, CHOOSERS = 512, CHUNK = 32, MOST_TOP = 32;   // CHUNK: tokens of a workgroup; a bit of a word for each
 constexpr int MOST_CHUNKS = 256;   // whose counts every workgroup of the second launch adds up itself; from more a launch between makes sums
 
 struct RouteArgs {
@@ -37,19 +37,33 @@ __device__ __forceinline__ u64 move64(u64 v) {
 __device__ __forceinline__ u64 lane64(u64 v, int lane) {
     return (u64)(unsigned)__builtin_amdgcn_readlane((int)(unsigned)(v >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((int)(unsigned)v, lane);
 }
-__device__ __forceinline__ u64 wave_max(u64 v) {
+// Of the L lanes (16 or 64) of a token, the same in all of them.
+template <int L>
+__device__ __forceinline__ u64 most_of(u64 v) {
     v = max(v, move64<0xB1>(v));
     v = max(v, move64<0x4E>(v));
     v = max(v, move64<0x124>(v));
     v = max(v, move64<0x128>(v));
-    return max(max(lane64(v, 0), lane64(v, 16)), max(lane64(v, 32), lane64(v, 48)));
+    return L == 16 ? v : max(max(lane64(v, 0), lane64(v, 16)), max(lane64(v, 32), lane64(v, 48)));
 }
-__device__ __forceinline__ double wave_sum(double d) {
+template <int L>
+__device__ __forceinline__ unsigned most_of(unsigned v) {
+    v = max(v, (unsigned)dbf_dpp_move<0xB1>((int)v));
+    v = max(v, (unsigned)dbf_dpp_move<0x4E>((int)v));
+    v = max(v, (unsigned)dbf_dpp_move<0x124>((int)v));
+    v = max(v, (unsigned)dbf_dpp_move<0x128>((int)v));
+    if (L == 16) return v;
+    auto lane = [&](int l) { return (unsigned)__builtin_amdgcn_readlane((int)v, l); };
+    return max(max(lane(0), lane(16)), max(lane(32), lane(48)));
+}
+template <int L>
+__device__ __forceinline__ double sum_of(double d) {
     auto sum = [](double a, u64 b) { return a + __builtin_bit_cast(double, b); };
     d = sum(d, move64<0xB1>(__builtin_bit_cast(u64, d)));
     d = sum(d, move64<0x4E>(__builtin_bit_cast(u64, d)));
     d = sum(d, move64<0x124>(__builtin_bit_cast(u64, d)));
     d = sum(d, move64<0x128>(__builtin_bit_cast(u64, d)));
+    if (L == 16) return d;
     const u64 b = __builtin_bit_cast(u64, d);
     return (__builtin_bit_cast(double, lane64(b, 0)) + __builtin_bit_cast(double, lane64(b, 16))) +
            (__builtin_bit_cast(double, lane64(b, 32)) + __builtin_bit_cast(double, lane64(b, 48)));
@@ -60,83 +74,74 @@ __device__ __forceinline__ u64 in_order(double v) {
     return b >> 63 ? ~b : b | 1ULL << 63;
 }
 
-// Experts of a token: lane l has l, l + 64, ... .  Lane j comes back with the j-th choice (-1: there is none) and its weight.
-template <typename T, int PER, bool SIGMOID>
-__device__ __forceinline__ void choose(const RouteArgs& a, int token, int lane, int& id, float& weight) {
+// The experts of a token, L lanes to it: lane l has l, l + L, ... .  Lane l comes back with the l-th choice, and with 16 lanes with the (l + 16)-th too (-1: there is none),
+// and their weights.  (A wavefront to a token took 20 us for 8191 tokens of 256 experts, whose chains of eight maxima wait for themselves: 16 lanes to each of four share them.)
+template <typename T, int L, int PER, bool SIGMOID>
+__device__ __forceinline__ void choose(const RouteArgs& a, int token, int l, int (&id)[2], float (&weight)[2]) {
     const T* row = static_cast<const T*>(a.logits) + token * a.stride;
     const float none = -__builtin_inff();
     float x[PER];
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        const int e = lane + 64 * i;
+        const int e = l + L * i;
         x[i] = e < a.n_experts ? dbf_to_float(row[e]) : none;
-        if (!(x[i] > none)) x[i] = none;
     }
     float most = none;
-    if (!SIGMOID) {
 #pragma unroll
-        for (int i = 0; i < PER; ++i) most = fmaxf(most, x[i]);
-        most = dbf_wave_max(most);
+    for (int i = 0; i < PER; ++i) {
+        if (!(x[i] > none)) x[i] = none;
+        most = fmaxf(most, x[i]);
     }
+    if (!SIGMOID) most = L == 16 ? dbf_row16_max(most) : dbf_wave_max(most);
     // (an infinite logit has all there is, shared with others of its kind)
     auto score = [&](float v) -> double { return SIGMOID ? 1.0 / (1.0 + exp(-(double)v)) : v == most ? 1.0 : exp((double)v - (double)most); };
-    // where there is no bias the order is that of the logits, and only the chosen ones' scores are needed but for a softmax's sum
-    double s[PER], total = 1.0;
+    // Where there is no bias the order is that of the logits, and only the chosen ones' scores are needed but for a softmax's sum.
+    double total = 1.0;
     u64 key[PER];
-    const bool sum = !SIGMOID && (a.bias || !a.renormalise);
-    if (sum) {
+    if (!SIGMOID && (a.bias || !a.renormalise)) {
         total = 0.0;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            s[i] = x[i] > none ? score(x[i]) : 0.0;
-            total += s[i];
-        }
-        total = wave_sum(total);
+        for (int i = 0; i < PER; ++i) total += x[i] > none ? score(x[i]) : 0.0;
+        total = sum_of<L>(total);
     }
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         key[i] = 0;
         if (x[i] > none) {
-            if (a.bias) {
-                if (SIGMOID) s[i] = score(x[i]);
-                else s[i] /= total;
-                const double v = s[i] + (double)a.bias[lane + 64 * i];
-                if (v > -__builtin_inf()) key[i] = in_order(v);
-            } else {
-                key[i] = in_order((double)x[i]);
-            }
+            const double v = a.bias ? score(x[i]) / total + (double)a.bias[l + L * i] : (double)x[i];
+            if (v > -__builtin_inf()) key[i] = in_order(v);
         }
     }
-    id = -1;
-    double mine = 0.0, chosen = 0.0;
+    id[0] = id[1] = -1;
+    unsigned last = ~0u;
     for (int j = 0; j < a.n_top; ++j) {
         u64 best = 0;
-        int at = 0;
+        unsigned e = 0;
 #pragma unroll
-        for (int i = PER - 1; i >= 0; --i)
-            if (key[i] >= best) best = key[i], at = i;
-        const u64 top = wave_max(best);
-        if (!top) break;
+        for (int i = PER - 1; i >= 0; --i) {
+            if (last == (unsigned)(l + L * i)) key[i] = 0;
+            if (key[i] >= best) best = key[i], e = l + L * i;
+        }
+        const u64 top = most_of<L>(best);
         // of equal ones the lowest index
-        const u64 lowest = ~wave_max(best == top ? ~(u64)(lane + 64 * at) : 0);
-        const int e = (int)lowest;
-        float v = 0.f;
-        double si = 0.0;
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (e == lane + 64 * i) {
-                key[i] = 0;
-                v = x[i];
-                si = s[i];
-            }
-        const u64 packed = lane64(__builtin_bit_cast(u64, si), e & 63);
-        double p = __builtin_bit_cast(double, packed);
-        if (!a.bias) p = score(__builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), e & 63))) / total;
-        chosen += p;
-        if (lane == j) id = e, mine = p;
+        last = ~most_of<L>(best == top ? ~e : 0u);
+        const int now = top ? (int)last : -1;
+        if (j == l) id[0] = now;
+        if (L == 16 && j == l + 16) id[1] = now;
     }
-    if (a.renormalise) mine = chosen > 0.0 ? mine / chosen : 0.0;
-    weight = (float)(mine * (double)a.scale);
+    double mine[2], chosen = 0.0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        mine[h] = 0.0;
+        if (id[h] >= 0) mine[h] = score(dbf_to_float(row[id[h]])) / total;
+        chosen += mine[h];
+    }
+    chosen = sum_of<L>(chosen);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        if (a.renormalise) mine[h] = chosen > 0.0 ? mine[h] / chosen : 0.0;
+        weight[h] = (float)(mine[h] * (double)a.scale);
+    }
 }
 
 // ---- the order by experts -----------------------------------------------------------------------------------------
@@ -145,22 +150,17 @@ struct Places {
     unsigned tokens[DBF_MAX_GROUPS];   // a chunk's tokens that chose an expert, a bit each
     int first[DBF_MAX_GROUPS];         // an expert's first row of the chunk
     int total[DBF_MAX_GROUPS];
-    int sums[2];
+    int all;
+    int ids[CHUNK * MOST_TOP];            // the chunk's choices
 };
 
 // total[e] -> the rows of the experts before e; returns the number of all.  first[e] grows by it.
 __device__ __forceinline__ int add_up(const RouteArgs& a, Places& p) {
-    constexpr int EACH = DBF_MAX_GROUPS / 64;
     __syncthreads();
     if (threadIdx.x < 64) {
-        const int lane = threadIdx.x;
-        int v[EACH], sum = 0;
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            const int e = EACH * lane + i;
-            v[i] = e < a.n_experts ? p.total[e] : 0;
-            sum += v[i];
-        }
+        const int lane = threadIdx.x, each = (a.n_experts + 63) / 64, from = min(each * lane, a.n_experts), to = min(from + each, a.n_experts);
+        int sum = 0;
+        for (int e = from; e < to; ++e) sum += p.total[e];
         int upto = sum;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
@@ -168,19 +168,16 @@ __device__ __forceinline__ int add_up(const RouteArgs& a, Places& p) {
             if (lane >= d) upto += other;
         }
         int at = upto - sum;
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            const int e = EACH * lane + i;
-            if (e < a.n_experts) {
-                p.total[e] = at;
-                p.first[e] += at;
-            }
-            at += v[i];
+        for (int e = from; e < to; ++e) {
+            const int n = p.total[e];
+            p.total[e] = at;
+            p.first[e] += at;
+            at += n;
         }
-        if (lane == 63) p.sums[0] = at;
+        if (lane == 63) p.all = upto;
     }
     __syncthreads();
-    return p.sums[0];
+    return p.all;
 }
 
 __device__ __forceinline__ void mark(const RouteArgs& a, Places& p, int token0) {
@@ -189,6 +186,7 @@ __device__ __forceinline__ void mark(const RouteArgs& a, Places& p, int token0) 
     const int entries = min(CHUNK, a.n_tokens - token0) * a.n_top;
     for (int i = threadIdx.x; i < entries; i += blockDim.x) {
         const int id = a.ids[(long long)token0 * a.n_top + i];
+        p.ids[i] = id;
         if (id >= 0) atomicOr(&p.tokens[id], 1u << (i / a.n_top));
     }
     __syncthreads();
@@ -198,7 +196,7 @@ __device__ __forceinline__ void place(const RouteArgs& a, const Places& p, int t
     const int entries = min(CHUNK, a.n_tokens - token0) * a.n_top;
     for (int i = threadIdx.x; i < entries; i += blockDim.x) {
         const long long at = (long long)token0 * a.n_top + i;
-        const int id = a.ids[at], t = i / a.n_top;
+        const int id = p.ids[i], t = i / a.n_top;
         int row = -1;
         if (id >= 0) {
             row = p.first[id] + __popc(p.tokens[id] & ((1u << t) - 1));
@@ -211,27 +209,38 @@ __device__ __forceinline__ void place(const RouteArgs& a, const Places& p, int t
         for (int e = threadIdx.x; e <= a.n_experts; e += blockDim.x) a.starts[e] = e < a.n_experts ? p.total[e] : all;
 }
 
-template <typename T, int PER, bool SIGMOID>
-__global__ __launch_bounds__(THREADS) void dbf_route_choose_kernel(const RouteArgs a) {
+template <typename T, int L, int PER, bool SIGMOID>
+__global__ __launch_bounds__(CHOOSERS) void dbf_route_choose_kernel(const RouteArgs a) {
     __shared__ Places p;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), token0 = blockIdx.x * CHUNK;
-    for (int t = wave; t < CHUNK && token0 + t < a.n_tokens; t += WAVES) {
-        int id;
-        float weight;
-        choose<T, PER, SIGMOID>(a, token0 + t, lane, id, weight);
-        if (lane < a.n_top) {
-            const long long at = (long long)(token0 + t) * a.n_top + lane;
-            a.ids[at] = id;
-            a.weights[at] = weight;
+    const int l = threadIdx.x & (L - 1), at_once = blockDim.x / L, token0 = blockIdx.x * CHUNK;
+    for (int e = threadIdx.x; e < a.n_experts; e += blockDim.x) p.tokens[e] = 0;
+    __syncthreads();
+    // (all lanes of a wavefront go on while one of its tokens is there)
+    for (int t0 = 0; t0 < CHUNK; t0 += at_once) {
+        const int t = t0 + threadIdx.x / L;
+        if (token0 + t0 + (int)(threadIdx.x & ~63) / L >= a.n_tokens) break;
+        int id[2];
+        float weight[2];
+        choose<T, L, PER, SIGMOID>(a, min(token0 + t, a.n_tokens - 1), l, id, weight);
+        if (token0 + t < a.n_tokens) {
+#pragma unroll
+            for (int h = 0; h < (L == 16 ? 2 : 1); ++h) {
+                const int j = l + 16 * h;
+                if (j >= a.n_top) continue;
+                const long long at = (long long)(token0 + t) * a.n_top + j;
+                a.ids[at] = id[h];
+                a.weights[at] = weight[h];
+                p.ids[t * a.n_top + j] = id[h];
+                if (id[h] >= 0) atomicOr(&p.tokens[id[h]], 1u << t);
+            }
         }
     }
     __syncthreads();
-    mark(a, p, token0);
     if (gridDim.x > 1) {
-        for (int e = threadIdx.x; e < a.padded; e += THREADS) a.counts[(long long)blockIdx.x * a.padded + e] = e < a.n_experts ? (uint8_t)__popc(p.tokens[e]) : 0;
+        for (int e = threadIdx.x; e < a.padded; e += blockDim.x) a.counts[(long long)blockIdx.x * a.padded + e] = e < a.n_experts ? (uint8_t)__popc(p.tokens[e]) : 0;
         return;
     }
-    for (int e = threadIdx.x; e < a.n_experts; e += THREADS) {
+    for (int e = threadIdx.x; e < a.n_experts; e += blockDim.x) {
         p.total[e] = __popc(p.tokens[e]);
         p.first[e] = 0;
     }
@@ -281,14 +290,19 @@ __global__ __launch_bounds__(THREADS) void dbf_route_place_kernel(const RouteArg
         const int words = a.padded / 4, slices = THREADS / words, w = threadIdx.x % words, slice = threadIdx.x / words;
         if (slice < slices) {
             int sum[4] = {0, 0, 0, 0}, mine[4] = {0, 0, 0, 0};
-            for (int c = slice; c < chunks; c += slices) {
-                const unsigned v = *reinterpret_cast<const unsigned*>(a.counts + (long long)c * a.padded + 4 * w);
+            constexpr int AT_ONCE = 8;
+            for (int c0 = slice; c0 < chunks; c0 += AT_ONCE * slices) {
+                unsigned v[AT_ONCE];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int n = v >> (8 * i) & 255;
-                    sum[i] += n;
-                    if (c < chunk) mine[i] += n;
-                }
+                for (int k = 0; k < AT_ONCE; ++k) v[k] = c0 + k * slices < chunks ? *reinterpret_cast<const unsigned*>(a.counts + (long long)(c0 + k * slices) * a.padded + 4 * w) : 0;
+#pragma unroll
+                for (int k = 0; k < AT_ONCE; ++k)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int n = v[k] >> (8 * i) & 255;
+                        sum[i] += n;
+                        mine[i] += c0 + k * slices < chunk ? n : 0;
+                    }
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -315,18 +329,18 @@ Room room_of(const dbf_router* r) {
     return {(chunks * padded + 255) / 256 * 256, chunks > MOST_CHUNKS ? (chunks + 1) * padded * 4 : 0};
 }
 
-template <typename T, int PER>
+template <typename T, int L, int PER>
 void choose(const RouteArgs& a, int score, dim3 grid, hipStream_t stream) {
-    if (score == DBF_SCORE_SIGMOID) hipLaunchKernelGGL((dbf_route_choose_kernel<T, PER, true>), grid, dim3(THREADS), 0, stream, a);
-    else hipLaunchKernelGGL((dbf_route_choose_kernel<T, PER, false>), grid, dim3(THREADS), 0, stream, a);
+    const dim3 threads(std::min(CHOOSERS, std::max(64, (a.n_tokens * L + 63) / 64 * 64)));   // (no more wavefronts than tokens)
+    if (score == DBF_SCORE_SIGMOID) hipLaunchKernelGGL((dbf_route_choose_kernel<T, L, PER, true>), grid, threads, 0, stream, a);
+    else hipLaunchKernelGGL((dbf_route_choose_kernel<T, L, PER, false>), grid, threads, 0, stream, a);
 }
 template <typename T>
 void choose(const RouteArgs& a, int score, dim3 grid, hipStream_t stream) {
-    const int per = (a.n_experts + 63) / 64;
-    if (per <= 1) choose<T, 1>(a, score, grid, stream);
-    else if (per <= 2) choose<T, 2>(a, score, grid, stream);
-    else if (per <= 4) choose<T, 4>(a, score, grid, stream);
-    else choose<T, 16>(a, score, grid, stream);
+    if (a.n_experts <= 64) choose<T, 16, 4>(a, score, grid, stream);
+    else if (a.n_experts <= 128) choose<T, 16, 8>(a, score, grid, stream);
+    else if (a.n_experts <= 256) choose<T, 16, 16>(a, score, grid, stream);
+    else choose<T, 64, 16>(a, score, grid, stream);
 }
 
 __global__ void dbf_route_nothing_kernel(int32_t* starts, int n) {
