@@ -96,8 +96,11 @@ __device__ __forceinline__ void multiply(dbf_f4& acc, const v8i& w, const v8i& x
     if constexpr (TYPE == DBF_E4M3) {
         if constexpr (FLOAT) {
             const dbf_f4 none = {0.f, 0.f, 0.f, 0.f};
-            const dbf_f4 p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, none, 0, 0, 0, 127, 0, x_scale);
-            const float s = __builtin_bit_cast(float, w_scale);
+            // The number's power of two is the instruction's, beside the rows' scale, so that neither alone takes the sum out of fp32's range; what is left of it, 1 .. 2, comes
+            // on the sum.  (0, and subnormal numbers as 0: no power; infinities and no numbers: 255, no number)
+            const int power = w_scale >> 23 & 255;
+            const dbf_f4 p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, none, 0, 0, 0, power, 0, x_scale);
+            const float s = __builtin_bit_cast(float, power ? (w_scale & 0x807FFFFF) | 0x3F800000 : 0);
 #pragma unroll
             for (int i = 0; i < 4; ++i) acc[i] = fmaf(s, p[i], acc[i]);
         } else {
@@ -129,9 +132,12 @@ __device__ __forceinline__ void multiply_exactly(dbf_f4& acc, v8i w, v8i x, int 
     dbf_f4 p = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int k = 0; k < 4; ++k) p = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen(w, k), widen(x, k), p, 0, 0, 0);
+    // (the smaller scale first: the other way round a sum of 2^25 leaves fp32's range where the result does not.  Sums are multiples of 2^-18, so 2^-127 of one is exact)
     const float by = FLOAT ? __builtin_bit_cast(float, w_scale) : scale_of(w_scale), of_row = scale_of(x_scale);
+    const bool first = fabsf(by) < of_row;
+    const float a = first ? by : of_row, b = first ? of_row : by;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) acc[e] = fmaf(p[e] * of_row, by, acc[e]);
+    for (int e = 0; e < 4; ++e) acc[e] = fmaf(p[e] * a, b, acc[e]);
 }
 
 __device__ __forceinline__ float gate(float g, float up) { return g / (1.f + expf(-g)) * up; }

@@ -44,7 +44,7 @@ __device__ __forceinline__ unsigned load_values(const T* row, int at, int n_cols
 }
 
 // The codes of sixteen values, which go where they belong in their row; its last sixteen may be fewer, and are filled up with zeros.
-__device__ __forceinline__ void store_codes(const float (&v)[OF_LANE], unsigned most, int byte, uint8_t* to) {
+__device__ __forceinline__ void store_codes(const float (&v)[OF_LANE], unsigned most, int byte, uint8_t* to, int have) {
     const float up = __builtin_bit_cast(float, (unsigned)(254 - byte) << 23);   // 2^(127 - byte)
     dbf_u4 w;
 #pragma unroll
@@ -52,7 +52,10 @@ __device__ __forceinline__ void store_codes(const float (&v)[OF_LANE], unsigned 
         int p = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i] * up, v[4 * i + 1] * up, 0, false);
         w[i] = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i + 2] * up, v[4 * i + 3] * up, p, true);
     }
-    if (most >= 0x7F800000u) w = (dbf_u4){0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu, 0x7F7F7F7Fu};
+    if (most >= 0x7F800000u) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = have >= 4 * i + 4 ? 0x7F7F7F7Fu : have <= 4 * i ? 0u : 0x7F7F7F7Fu >> (32 - 8 * (have - 4 * i));
+    }
     *reinterpret_cast<dbf_u4*>(to) = w;
 }
 
@@ -80,7 +83,7 @@ __global__ __launch_bounds__(THREADS) void dbf_fp8_rows_kernel(const QuantizeArg
         float v[OF_LANE];
         const unsigned most = lanes8_max(load_values(static_cast<const T*>(a.x) + row * a.x_stride, at, a.n_cols, v));
         const int byte = most >= 0x7F800000u ? 127 : scale_byte(most);
-        if (at < a.n_cols) store_codes(v, most, byte, a.codes + row * a.codes_stride + at);
+        if (at < a.n_cols) store_codes(v, most, byte, a.codes + row * a.codes_stride + at, a.n_cols - at);
         if (lane == 0) a.scales[row * a.scales_stride + b] = (uint8_t)byte;
     }
 }
@@ -111,7 +114,7 @@ __global__ __launch_bounds__(THREADS) void dbf_fp8_squares_kernel(const Quantize
 #pragma unroll
         for (int t = 0; t < TURNS; ++t) {
             const long long row = (long long)rb * BLOCK + t * (THREADS / LANES) + line;
-            if (row < a.n_rows && at < a.n_cols) store_codes(v[t], most, byte, a.codes + row * a.codes_stride + at);
+            if (row < a.n_rows && at < a.n_cols) store_codes(v[t], most, byte, a.codes + row * a.codes_stride + at, a.n_cols - at);
         }
         if (threadIdx.x == 0) a.scales[rb * a.scales_stride + b] = (uint8_t)byte;
     }
