@@ -464,7 +464,7 @@ int dbf_token_logprobs(const void* logits, int dtype, long long row_stride, int 
 /* ---- layers that are not compressed, and layers of experts ----------------------------------
  * Products with ordinary weights, beside those with DBF layers: what a compression leaves as it is (a decoder's head, the layers that lose most), in 8 bits with
  * a scale for each block of 128 or in 16 bits (dbf_dense_gemm), experts whose rows are ragged (dbf_grouped_gemm), the rounding of activations and weights to 8
- * bits (dbf_fp8_quantize), a router's choice of experts and the order of rows that goes with it (dbf_route), and the sum that brings experts' rows back to their
+ * bits (dbf_quantize), a router's choice of experts and the order of rows that goes with it (dbf_route), and the sum that brings experts' rows back to their
  * tokens (dbf_combine).  Conventions are those of the section above: asynchronous, nothing allocated, may be captured, results independent of scheduling; element
  * types are the same, and
  *   DBF_E4M3: 8 bits, sign, 4 of exponent (bias 7), 3 of mantissa; largest 448; no infinities; 0x7F and 0xFF are no numbers
@@ -472,7 +472,7 @@ int dbf_token_logprobs(const void* logits, int dtype, long long row_stride, int 
 enum { DBF_E4M3 = 3, DBF_E8M0 = 4 };
 #define DBF_SCALE_BLOCK 128  /* values of a row that share a scale */
 
-/* dbf_fp8_quantize: x [n_rows][n_cols] of dtype (DBF_F16, DBF_BF16, DBF_F32; rows x_stride values apart, any alignment of the type) as codes in 8 bits, rows
+/* dbf_quantize: x [n_rows][n_cols] of dtype (DBF_F16, DBF_BF16, DBF_F32; rows x_stride values apart, any alignment of the type) as codes in 8 bits, rows
  * codes_stride bytes apart, and scales, rows scales_stride bytes apart.  A block is 128 values of a row (block_rows 1: activations), or those of 128 rows
  * (block_rows 128: weights); the last ones of a row, or the last rows, may be fewer.  Its scale is the smallest power of two s, 2^-127 at least, such that no value
  * is above 448 s (1 for a block of zeros), a code the type's value nearest to x / s, ties to even: the quotient is exact, so both are fully determined.
@@ -480,7 +480,7 @@ enum { DBF_E4M3 = 3, DBF_E8M0 = 4 };
  *   scales: device, DBF_E8M0, [ceil(n_rows / block_rows)][ceil(n_cols / 128)]
  * A block that holds a value which is not finite is all no numbers, with scale 1.  n_rows 0 does nothing.
  * Errors: DBF_EINVAL (null, misaligned, types, strides, n_rows < 0, block_rows), DBF_ESHAPE (n_cols), DBF_EHIP. */
-int dbf_fp8_quantize(const void* x, int dtype, long long x_stride, int n_rows, int n_cols, int block_rows, void* codes, long long codes_stride,
+int dbf_quantize(const void* x, int dtype, long long x_stride, int n_rows, int n_cols, int block_rows, void* codes, long long codes_stride,
                      void* scales, long long scales_stride, void* hip_stream);
 
 /* What a product with ordinary weights reads and writes:  y[r][n] = sum over k of x[row r][k] w[n][k], summed in fp32, rounded once to out_dtype.

@@ -40,7 +40,7 @@ EXPORTS = [
     "dbf_prune_middle", "dbf_svid_workspace_bytes", "dbf_svid", "dbf_admm_workspace_bytes", "dbf_admm_step", "dbf_admm_prepare_workspace_bytes", "dbf_admm_prepare", "dbf_probe_read", "dbf_probe_mfma", "dbf_strerror",
     "dbf_cache_bytes", "dbf_block_tables", "dbf_qk_norm_rope", "dbf_cache_append", "dbf_cache_read",
     "dbf_cache_attend_workspace_bytes", "dbf_cache_attend", "dbf_token_logprobs_workspace_bytes", "dbf_token_logprobs",
-    "dbf_fp8_quantize", "dbf_dense_gemm_workspace_bytes", "dbf_dense_gemm", "dbf_grouped_gemm_workspace_bytes", "dbf_grouped_gemm",
+    "dbf_quantize", "dbf_dense_gemm_workspace_bytes", "dbf_dense_gemm", "dbf_grouped_gemm_workspace_bytes", "dbf_grouped_gemm",
     "dbf_route_workspace_bytes", "dbf_route", "dbf_combine",
     "dbf_tuning_set", "dbf_tuning_get", "dbf_tuning_reset",
 ]
@@ -174,7 +174,7 @@ def lib() -> C.CDLL:
     L.dbf_token_logprobs_workspace_bytes.argtypes = [i32, i32, i32]
     L.dbf_token_logprobs_workspace_bytes.restype = sz
     L.dbf_token_logprobs.argtypes = [vp, i32, C.c_longlong, i32, i32, vp, i32, vp, vp, vp, vp, vp, sz, vp]
-    L.dbf_fp8_quantize.argtypes = [vp, i32, C.c_longlong, i32, i32, i32, vp, C.c_longlong, vp, C.c_longlong, vp]
+    L.dbf_quantize.argtypes = [vp, i32, C.c_longlong, i32, i32, i32, vp, C.c_longlong, vp, C.c_longlong, vp]
     for name in ("dbf_dense_gemm", "dbf_grouped_gemm"):
         getattr(L, name + "_workspace_bytes").argtypes = [C.POINTER(Dense)]
         getattr(L, name + "_workspace_bytes").restype = sz
@@ -479,9 +479,9 @@ def dbf_token_logprobs(logits_ptr: int, dtype: int, row_stride: int, n_rows: int
 # ---- layers that are not compressed, and layers of experts ------------------------------------------------
 
 
-def dbf_fp8_quantize(x_ptr: int, dtype: int, x_stride: int, n_rows: int, n_cols: int, block_rows: int, codes_ptr: int, codes_stride: int, scales_ptr: int,
+def dbf_quantize(x_ptr: int, dtype: int, x_stride: int, n_rows: int, n_cols: int, block_rows: int, codes_ptr: int, codes_stride: int, scales_ptr: int,
                      scales_stride: int, stream: int = 0) -> None:
-    _check(lib().dbf_fp8_quantize(x_ptr, dtype, x_stride, n_rows, n_cols, block_rows, codes_ptr, codes_stride, scales_ptr, scales_stride, stream), "dbf_fp8_quantize")
+    _check(lib().dbf_quantize(x_ptr, dtype, x_stride, n_rows, n_cols, block_rows, codes_ptr, codes_stride, scales_ptr, scales_stride, stream), "dbf_quantize")
 
 
 def dbf_dense_gemm_workspace_bytes(product: Dense) -> int:

@@ -1,4 +1,4 @@
-// Rounding to 8 bits with a scale for each block of 128 values (include/dbf.h: dbf_fp8_quantize).
+// Rounding to 8 bits with a scale for each block of 128 values (include/dbf.h: dbf_quantize).
 //
 // A block's scale is the smallest power of two that brings its largest value to 448 or less, so a value over its scale is exact in fp32 and the conversion to the
 // type is its only rounding: codes do not hang on how a quotient is made.
@@ -132,7 +132,7 @@ int launch(const QuantizeArgs& a, int block_rows, hipStream_t stream) {
 
 }  // namespace
 
-extern "C" int dbf_fp8_quantize(const void* x, int dtype, long long x_stride, int n_rows, int n_cols, int block_rows, void* codes, long long codes_stride,
+extern "C" int dbf_quantize(const void* x, int dtype, long long x_stride, int n_rows, int n_cols, int block_rows, void* codes, long long codes_stride,
                                 void* scales, long long scales_stride, void* hip_stream) {
     if (!x || !codes || !scales || (dtype != DBF_F16 && dtype != DBF_BF16 && dtype != DBF_F32)) return DBF_EINVAL;
     if (n_cols < 1 || n_cols > DBF_MAX_DIM) return DBF_ESHAPE;

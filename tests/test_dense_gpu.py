@@ -361,7 +361,7 @@ def test_rounding_to_8_bits(rows, cols, extra, block_rows, dtype):
     codes = torch.full((rows, up(cols, 16) + 16), 0x55, dtype=torch.uint8, device="cuda")
     kb = -(-cols // 128)
     scales = torch.full((-(-rows // block_rows), kb + 2), 0x66, dtype=torch.uint8, device="cuda")
-    B.dbf_fp8_quantize(t.data_ptr(), dtype, cols + extra, rows, cols, block_rows, codes.data_ptr(), codes.shape[1], scales.data_ptr(), scales.shape[1], G.stream_handle())
+    B.dbf_quantize(t.data_ptr(), dtype, cols + extra, rows, cols, block_rows, codes.data_ptr(), codes.shape[1], scales.data_ptr(), scales.shape[1], G.stream_handle())
     torch.cuda.synchronize()
     want, want_scales = O.quantize(t[:, :cols].double().cpu().numpy(), block_rows)
     got = codes.cpu().numpy()
@@ -517,9 +517,9 @@ class Experts:
     def run(self):
         s, R = torch.cuda.current_stream().cuda_stream, self.T * self.n_top
         B.dbf_route(self.router, self.ws.data_ptr(), self.ws.numel(), s)
-        B.dbf_fp8_quantize(self.x.data_ptr(), B.BF16, self.hidden, self.T, self.hidden, 1, self.xq.data_ptr(), self.xq.shape[1], self.xs.data_ptr(), self.xs.shape[1], s)
+        B.dbf_quantize(self.x.data_ptr(), B.BF16, self.hidden, self.T, self.hidden, 1, self.xq.data_ptr(), self.xq.shape[1], self.xs.data_ptr(), self.xs.shape[1], s)
         B.dbf_grouped_gemm(self.up_gate, 0, 0, s)
-        B.dbf_fp8_quantize(self.h.data_ptr(), B.BF16, self.inner, R, self.inner, 1, self.hq.data_ptr(), self.hq.shape[1], self.hs.data_ptr(), self.hs.shape[1], s)
+        B.dbf_quantize(self.h.data_ptr(), B.BF16, self.inner, R, self.inner, 1, self.hq.data_ptr(), self.hq.shape[1], self.hs.data_ptr(), self.hs.shape[1], s)
         B.dbf_grouped_gemm(self.down, 0, 0, s)
         B.dbf_combine(self.sum, s)
         return self.out
@@ -619,8 +619,8 @@ def test_a_head_in_8_bits_before_log_probabilities():
     codes, scales = torch.empty(vocab, hidden, dtype=torch.uint8, device="cuda"), torch.empty(8, 2, dtype=torch.uint8, device="cuda")
     xq, xs = torch.empty(rows, hidden, dtype=torch.uint8, device="cuda"), torch.empty(rows, 4, dtype=torch.uint8, device="cuda")
     s = G.stream_handle()
-    B.dbf_fp8_quantize(w.data_ptr(), B.F32, hidden, vocab, hidden, 128, codes.data_ptr(), hidden, scales.data_ptr(), 2, s)
-    B.dbf_fp8_quantize(x.data_ptr(), B.F16, hidden, rows, hidden, 1, xq.data_ptr(), hidden, xs.data_ptr(), 4, s)
+    B.dbf_quantize(w.data_ptr(), B.F32, hidden, vocab, hidden, 128, codes.data_ptr(), hidden, scales.data_ptr(), 2, s)
+    B.dbf_quantize(x.data_ptr(), B.F16, hidden, rows, hidden, 1, xq.data_ptr(), hidden, xs.data_ptr(), 4, s)
     logits = torch.empty(rows, vocab, device="cuda")
     B.dbf_dense_gemm(B.Dense(x=xq.data_ptr(), x_scale=xs.data_ptr(), x_stride=hidden, x_scale_stride=4, n_x_rows=rows, w=codes.data_ptr(), w_scale=scales.data_ptr(), w_stride=hidden, w_scale_stride=2,
                              y=logits.data_ptr(), y_stride=vocab, dtype=B.E4M3, out_dtype=B.F32, w_scale_type=B.E8M0, n_rows=rows, n_in=hidden, n_out=vocab), 0, 0, s)

@@ -92,7 +92,7 @@ def test_groups_are_refused_where_they_do_not_belong():
     (B.DBF_EINVAL, dict(scales_stride=1)), (B.DBF_ESHAPE, dict(cols=0)), (B.DBF_ESHAPE, dict(cols=(1 << 20) + 1)), (B.DBF_EINVAL, dict(dtype=B.F32, x=P + 2))])
 def test_rounding_refuses(code, args):
     a = {**dict(x=P, dtype=B.F16, x_stride=200, rows=3, cols=200, block=1, codes=P, codes_stride=208, scales=P, scales_stride=2), **args}
-    _refused(code, B.dbf_fp8_quantize, a["x"], a["dtype"], a["x_stride"], a["rows"], a["cols"], a["block"], a["codes"], a["codes_stride"], a["scales"], a["scales_stride"])
+    _refused(code, B.dbf_quantize, a["x"], a["dtype"], a["x_stride"], a["rows"], a["cols"], a["block"], a["codes"], a["codes_stride"], a["scales"], a["scales_stride"])
 
 
 def _router(**kw):
