@@ -287,7 +287,7 @@ def _own(s):
         B.dbf_route(s["desc"], s["ws"].data_ptr(), s["ws"].numel(), stream)
         return [s["ids"], s["weights"], s["starts"], s["row_token"], s["token_rows"]]
     if kind == "quantize":
-        B.dbf_fp8_quantize(s["x"].data_ptr(), s["type"], case["cols"], case["rows"], case["cols"], case["rows_of_block"], s["codes"].data_ptr(), s["codes"].shape[1],
+        B.dbf_quantize(s["x"].data_ptr(), s["type"], case["cols"], case["rows"], case["cols"], case["rows_of_block"], s["codes"].data_ptr(), s["codes"].shape[1],
                            s["scales"].data_ptr(), s["scales"].shape[1], stream)
         return [s["codes"][:, : case["cols"]], s["scales"][:, : -(-case["cols"] // BLOCK)]]
     if kind == "combine":
