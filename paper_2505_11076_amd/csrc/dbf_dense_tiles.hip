@@ -19,7 +19,7 @@ __global__ __launch_bounds__(64 * WN * WM) __attribute__((amdgpu_waves_per_eu(EA
     constexpr int W_LOADS = BN / 8 / WAVES, X_LOADS = BM / 8 / WAVES;
     static_assert(W_LOADS * 8 * WAVES == BN && X_LOADS * 8 * WAVES == BM && MS % 2 == 0, "whole loads");
     static_assert((64 * WAVES) % BM == 0 && BM % 64 == 0, "a thread or more for each scale's word");
-    constexpr int SCALES = (BN + BM) * STEP, ROOM = SCALES + (TYPE == DBF_E4M3 ? 4 * BM : 0);   // behind the rows x's scales, a word each: the step's and its neighbours'
+    constexpr int SCALES = (BN + BM) * STEP, ROOM = SCALES + (TYPE == DBF_E4M3 ? 4 * BM + 256 : 0);   // behind the rows x's scales, a word each: of four steps
     // (objects of their own: the compiler then knows that a load into one is not read from another)
     __shared__ __align__(16) uint8_t s0[ROOM], s1[ROOM];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, q = lane >> 4;
@@ -77,11 +77,16 @@ __global__ __launch_bounds__(64 * WN * WM) __attribute__((amdgpu_waves_per_eu(EA
         w_scale = static_cast<const uint8_t*>(a.w_scale) + block * (FLOAT ? 4 : 1);
         up_scale = static_cast<const uint8_t*>(a.w_up_scale) + block * (FLOAT ? 4 : 1);
     }
-    // (by all wavefronts and in every step, without a branch: it would end the block of instructions, and the compiler then moves products behind it, where the operands
-    // of all of them are alive at once)
+    // A word has the bytes of four steps and stays for the two of them that its place is used for: in the other two, and in wavefronts without rows of their own, all lanes load one word to
+    // where nobody reads.  (Each lane's word is a cache line of its own: all words in every step were a quarter of what the second cache was asked for.  No branch: it would end the block of
+    // instructions, and the compiler then moves products behind it, where the operands of all of them are alive at once.)
     auto fetch_x_scales = [&](uint8_t* to, int step) {
-        if (TYPE == DBF_E4M3)
-            __builtin_amdgcn_global_load_lds((Global)(a.x_scale + x0 * a.x_scale_row + (step & ~3) + x_scale_at), (Shared)(to + SCALES + 256 * (wave % (BM / 64))), 4, 0, 0);
+        if constexpr (TYPE == DBF_E4M3) {
+            const bool needed = (step & 2) == 0 && wave < BM / 64;
+            unsigned lanes = needed ? ~0u : 0u;
+            asm("" : "+v"(lanes));
+            __builtin_amdgcn_global_load_lds((Global)(a.x_scale + x0 * a.x_scale_row + (step & ~3) + (x_scale_at & lanes)), (Shared)(to + SCALES + 256 * (needed ? wave : BM / 64)), 4, 0, 0);
+        }
     };
     int ws = 0, us = 0, ws_next = 0, us_next = 0;
     auto fetch_w_scales = [&](int step) {
