@@ -54,18 +54,20 @@ __global__ __launch_bounds__(64 * WN * WM) __attribute__((amdgpu_waves_per_eu(EA
     }
     // (of the last step the pieces behind the rows' end are not read: the row's first of the step in their place, which zeros overwrite)
     const int behind = last * STEP + place < a.k_bytes ? 0 : place;
-    auto fetch = [&](uint8_t* to, int step) {
+    constexpr int LOADS = W_LOADS + X_LOADS;
+    auto fetch = [&](uint8_t* to, int step, int from_load, int to_load) {
         const int back = step == last ? behind : 0;
 #pragma unroll
-        for (int i = 0; i < W_LOADS; ++i) {
-            const int row = 8 * (WAVES * i + wave);
-            const uint8_t* from = (GATED && row / 16 % 2 ? a.w_up : a.w) + w0 + step * STEP;
-            __builtin_amdgcn_global_load_lds((Global)(from + (w_at[i] - back)), (Shared)(to + row * STEP), 16, 0, 0);
-        }
-#pragma unroll
-        for (int i = 0; i < X_LOADS; ++i) {
-            const uint8_t* from = a.x + x0 * a.x_row + step * STEP;
-            __builtin_amdgcn_global_load_lds((Global)(from + (x_at[i] - back)), (Shared)(to + (BN + 8 * (WAVES * i + wave)) * STEP), 16, 0, 0);
+        for (int k = from_load; k < to_load; ++k) {
+            if (k < W_LOADS) {
+                const int row = 8 * (WAVES * k + wave);
+                const uint8_t* from = (GATED && row / 16 % 2 ? a.w_up : a.w) + w0 + step * STEP;
+                __builtin_amdgcn_global_load_lds((Global)(from + (w_at[k < W_LOADS ? k : 0] - back)), (Shared)(to + row * STEP), 16, 0, 0);
+            } else {
+                const int i = k - W_LOADS;
+                const uint8_t* from = a.x + x0 * a.x_row + step * STEP;
+                __builtin_amdgcn_global_load_lds((Global)(from + (x_at[i < 0 ? 0 : i] - back)), (Shared)(to + (BN + 8 * (WAVES * i + wave)) * STEP), 16, 0, 0);
+            }
         }
     };
     // scales: those of the rows go through LDS, the words that have a step's bytes; the weights' are the wavefront's
@@ -128,6 +130,8 @@ __global__ __launch_bounds__(64 * WN * WM) __attribute__((amdgpu_waves_per_eu(EA
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
+    static_assert(MS % 2 == 0 && MS >= 4, "rows of 16");
+    constexpr int AT_ONCE = LOADS / 2, LATER = 2;   // of a step's loads: those beside the last products of the step before the last; sets of products that the others are beside
     // In rows of 16: a step's first is in place ODD of x, the next one in the other, and so on in turn; the last in place 2, so that the next step's first has the place of
     // the last but two.
     auto step = [&](uint8_t* now, uint8_t* next, int s, auto odd) {
@@ -136,6 +140,8 @@ __global__ __launch_bounds__(64 * WN * WM) __attribute__((amdgpu_waves_per_eu(EA
         fetch_w_scales(after);
 #pragma unroll
         for (int j = 0; j + 2 < MS; ++j) {
+            // the rest of the next step's loads, a few beside each of the first products: a wavefront waits where it gives more than are taken
+            if (j < LATER) fetch(next, after, AT_ONCE + (LOADS - AT_ONCE) * j / LATER, AT_ONCE + (LOADS - AT_ONCE) * (j + 1) / LATER);
             read_x(now, s, j + 1, (j + 1) % 2 ^ ODD);
             if (j + 3 == MS) read_x(now, s, MS - 1, 2);
 #pragma unroll
@@ -143,26 +149,25 @@ __global__ __launch_bounds__(64 * WN * WM) __attribute__((amdgpu_waves_per_eu(EA
             __builtin_amdgcn_sched_barrier(0);   // (else all reads go first, and their registers are too many)
         }
         meet();
-        fetch(now, min(s + 2, last));
-        fetch_x_scales(now, min(s + 2, last));
         read_x(next, after, 0, 1 - ODD);
 #pragma unroll
         for (int i = 0; i < NS; ++i) {
             product(i, MS - 2, ODD);
             product(i, MS - 1, 2);
             read_w(next, i);
+            fetch(now, min(s + 2, last), AT_ONCE * i / NS, AT_ONCE * (i + 1) / NS);
+            if (i == 0) fetch_x_scales(now, min(s + 2, last));
         }
         __builtin_amdgcn_sched_barrier(0);
         ws = ws_next;
         us = us_next;
     };
-    static_assert(MS % 2 == 0 && MS >= 4, "");
     fetch_w_scales(0);
-    fetch(s0, 0);
+    fetch(s0, 0, 0, LOADS);
     fetch_x_scales(s0, 0);
     if (steps) {
         meet();
-        fetch(s1, 1);
+        fetch(s1, 1, 0, AT_ONCE);
         fetch_x_scales(s1, 1);
         ws = ws_next;
         us = us_next;
@@ -173,8 +178,9 @@ __global__ __launch_bounds__(64 * WN * WM) __attribute__((amdgpu_waves_per_eu(EA
             step(s0, s1, s, std::integral_constant<int, 0>());
             step(s1, s0, s + 1, std::integral_constant<int, 1>());
         }
+        fetch(s1, min(steps + 1, last), AT_ONCE, LOADS);
     } else {
-        fetch(s1, min(1, last));
+        fetch(s1, min(1, last), 0, LOADS);
         fetch_x_scales(s1, min(1, last));
     }
     // What is left, which has set out already.  Behind the rows' end it becomes zeros, of both operands (a code there may be no number).
