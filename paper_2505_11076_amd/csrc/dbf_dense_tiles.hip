@@ -131,7 +131,8 @@ __global__ __launch_bounds__(64 * WN * WM) __attribute__((amdgpu_waves_per_eu(EA
         asm volatile("" ::: "memory");
     };
     static_assert(MS % 2 == 0 && MS >= 4, "rows of 16");
-    constexpr int AT_ONCE = LOADS / 2, LATER = 2;   // of a step's loads: those beside the last products of the step before the last; sets of products that the others are beside
+    constexpr int AT_ONCE = LOADS / 4, LATER = MS > 4 ? 3 : 2;   // of a step's loads: those beside the last products of the step before the last; sets of products that the others are beside
+    static_assert(LATER <= MS - 2, "all loads are given out");
     // In rows of 16: a step's first is in place ODD of x, the next one in the other, and so on in turn; the last in place 2, so that the next step's first has the place of
     // the last but two.
     auto step = [&](uint8_t* now, uint8_t* next, int s, auto odd) {
@@ -243,9 +244,12 @@ int launch(const DenseArgs& a, hipStream_t stream) {
                        (int)m_tiles);
     return hipGetLastError() == hipSuccess ? DBF_OK : DBF_EHIP;
 }
-// What a launch costs, in us a step, by how many tiles it has: `full` where all places of the chip have one, `alone` for the first; measured with 4096 values in 8 bits (24 .. 2048 rows by 4096 and
-// 16384 outputs).  256 x 256: 512 rows by 16384 53 us, 1024 63, 2048 120.  128 x 128: 27 / 75 / 143 (512 rows 40).  128 x 64: 64 rows by 16384 26, 256 28, 512 52.  64 x 64: 64 rows by 4096 13,
-// 512 21, 1024 34, 128 rows by 16384 22.  Of a group's last tile half is taken to be empty.
+// What a launch costs, in us a step, by how many tiles it has: `full` where all places of the chip have one, `alone` for the first; from these times (us, rows by outputs, 4096 values in 8 bits):
+//   256 x 256   64 x 4096 39    512 x 16384 49   1024 x 16384 60   2048 x 16384 118  2048 x 4096 51
+//   128 x 128   64 x 4096 21    256 x 16384 32    512 x 16384 37   1024 x 16384 73   2048 x 16384 140   2048 x 4096 38
+//   128 x 64    64 x 4096 16    256 x 16384 26    512 x 16384 49   512 x 4096 23     1024 x 4096 26     2048 x 4096 51
+//   64 x 64     64 x 4096 14    256 x 16384 30    512 x 16384 66   512 x 4096 23     1024 x 4096 29     2048 x 4096 66
+// Of a group's last tile half is taken to be empty (16384 rows of 32 experts, fp32 scales, gated, 396 us, with 128 x 128 476).
 double cost_of(const DenseArgs& a, int outs, int rows, int places, double alone, double full) {
     const double groups = a.starts ? std::min(a.n_groups, a.n_rows) : 1, each = a.n_rows / groups;
     const double m_tiles = groups * (a.starts ? std::max(1.0, each / rows + 0.5) : std::ceil(each / rows));
@@ -255,8 +259,8 @@ double cost_of(const DenseArgs& a, int outs, int rows, int places, double alone,
 template <int TYPE, bool FLOAT, bool GATED, bool EXACT>
 int launch(const DenseArgs& a, hipStream_t stream) {
     constexpr int OF = GATED ? 2 : 1;
-    const double large = EXACT ? 1e30 : cost_of(a, 256 / OF, 256, 256, 1.5, 1.85), square = cost_of(a, 128 / OF, 128, 512, 0.75, 1.2);
-    const double low = cost_of(a, 128 / OF, 64, 768, 0.62, 1.1), small = cost_of(a, 64 / OF, 64, 1024, 0.4, 1.0);
+    const double large = EXACT ? 1e30 : cost_of(a, 256 / OF, 256, 256, 1.2, 1.85), square = cost_of(a, 128 / OF, 128, 512, 0.68, 1.15);
+    const double low = cost_of(a, 128 / OF, 64, 768, 0.45, 1.13), small = cost_of(a, 64 / OF, 64, 1024, 0.43, 0.92);
     const double least = std::min({large, square, low, small});
     if constexpr (!EXACT)   // (in fp16 its operands have no registers)
         if (large <= least) return launch<TYPE, FLOAT, GATED, EXACT, 256, 256, 4, 2, 2>(a, stream);
