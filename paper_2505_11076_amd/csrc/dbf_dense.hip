@@ -145,7 +145,9 @@ __global__ __launch_bounds__(64 * KW) void dbf_dense_few_kernel(const DenseArgs 
 template <int TYPE, bool FLOAT, bool GATED, bool EXACT, int NS, int MS, int KW>
 int launch(const DenseArgs& a, hipStream_t stream) {
     const long long tiles = (a.n_rows + 16LL * MS - 1) / (16 * MS) + (a.starts ? std::min(a.n_groups, a.n_rows) : 0);
-    const dim3 grid((unsigned)((a.n_out + 16 * NS - 1) / (16 * NS)), (unsigned)std::min(tiles, 4096LL));
+    const long long outs = (a.n_out + 16 * NS - 1) / (16 * NS);
+    // (a grid holds less than 2^32 threads; tiles that it has no workgroup for are taken in turn)
+    const dim3 grid((unsigned)outs, (unsigned)std::min({tiles, 4096LL, (1LL << 31) / (outs * 64 * KW)}));
     hipLaunchKernelGGL((dbf_dense_few_kernel<TYPE, FLOAT, GATED, EXACT, NS, MS, KW>), grid, dim3(64 * KW), 0, stream, a);
     return hipGetLastError() == hipSuccess ? DBF_OK : DBF_EHIP;
 }

@@ -55,6 +55,13 @@ def test_few_rows_of_small_weights(rec):
     assert product(rec, 3, 256, 64, 5)[:2] == ("few", (4, 1 + 3, 1))
 
 
+def test_launches_stay_below_what_a_grid_may_hold(rec):
+    # 2^32 threads: 65536 workgroups of outputs and as many rows of groups as there are
+    for kw in (dict(rows=4096, n_in=24, n_out=1 << 20, groups=1024), dict(rows=1024, n_in=1 << 20, n_out=1 << 20, groups=1024, w_group_stride=0), dict(rows=1 << 22, n_in=1, n_out=16, groups=1024)):
+        name, grid, threads = product(rec, **kw)
+        assert grid[0] * grid[1] * grid[2] * threads < 1 << 32 and grid[1] >= 1, (name, kw)
+
+
 def test_tiles_are_chosen_by_what_a_launch_costs(rec):
     def tiles(*a, **kw):
         name, grid, threads = product(rec, *a, **kw)
