@@ -528,7 +528,7 @@ int dbf_grouped_gemm(const dbf_dense* product, void* workspace_dev, size_t works
  *   token_rows int32 [n_tokens][n_top]: the row of each choice; -1 where there is none
  * starts and row_token are what dbf_grouped_gemm takes as starts and x_rows, token_rows what dbf_combine does.  n_tokens 0 only clears starts.
  * workspace_dev: 256-byte aligned, dbf_route_workspace_bytes bytes (may be 0).
- * Errors: DBF_EINVAL (null, misaligned, types, n_tokens < 0, n_top not in 1 .. 32 or above n_experts, n_tokens * n_top above 2^31 - 1, row_stride), DBF_ESHAPE (n_experts
+ * Errors: DBF_EINVAL (null, misaligned, types, n_tokens not in 0 .. 2^27 - 32, n_top not in 1 .. 32 or above n_experts, n_tokens * n_top above 2^31 - 1, row_stride), DBF_ESHAPE (n_experts
  * not in 1 .. DBF_MAX_GROUPS), DBF_EWORKSPACE, DBF_EHIP. */
 enum { DBF_SCORE_SOFTMAX = 0, DBF_SCORE_SIGMOID = 1 };
 typedef struct dbf_router {

@@ -14,6 +14,7 @@ typedef unsigned long long u64;
 // ---- the choice ------------------------------------------------------------------------------------------------
 
 constexpr int THREADS = 1024, CHOOSERS = 512, CHUNK = 32, MOST_TOP = 32;   // CHUNK: tokens of a workgroup; a bit of a word for each
+constexpr int MOST_TOKENS = CHUNK * ((1 << 22) - 1);   // of 2^32 threads or more only the remainder would run: chunks of THREADS
 constexpr int MOST_CHUNKS = 256;   // whose counts every workgroup of the second launch adds up itself; from more a launch between makes sums
 
 struct RouteArgs {
@@ -317,8 +318,8 @@ __global__ __launch_bounds__(THREADS) void dbf_route_place_kernel(const RouteArg
 }
 
 bool sizes_ok(const dbf_router* r) {
-    return r->n_tokens >= 0 && r->n_experts >= 1 && r->n_experts <= DBF_MAX_GROUPS && r->n_top >= 1 && r->n_top <= MOST_TOP && r->n_top <= r->n_experts &&
-           (long long)r->n_tokens * r->n_top <= INT_MAX;
+    return r->n_tokens >= 0 && r->n_tokens <= MOST_TOKENS && r->n_experts >= 1 && r->n_experts <= DBF_MAX_GROUPS && r->n_top >= 1 && r->n_top <= MOST_TOP &&
+           r->n_top <= r->n_experts && (long long)r->n_tokens * r->n_top <= INT_MAX;
 }
 struct Room {
     size_t counts, before;
@@ -444,8 +445,6 @@ extern "C" int dbf_route(const dbf_router* r, void* workspace_dev, size_t worksp
     a.padded = (r->n_experts + 3) / 4 * 4;
     a.renormalise = r->renormalise;
     a.scale = r->scale;
-    // (of 2^32 threads or more only the remainder would run: 2^23 chunks are 2^28 tokens)
-    if (chunks >= 1 << 23) return DBF_EINVAL;
     const dim3 grid((unsigned)chunks);
     if (r->dtype == DBF_F16) choose<_Float16>(a, r->score, grid, stream);
     else if (r->dtype == DBF_BF16) choose<dbf_bf16>(a, r->score, grid, stream);

@@ -114,6 +114,15 @@ def test_a_router_refuses():
     assert B.dbf_route_workspace_bytes(_router(n_top=0)) == 0
 
 
+def test_a_router_refuses_more_tokens_than_a_launch_has_workgroups_for():
+    # 32 tokens to a workgroup of 1024 threads, of which a launch has less than 2^32
+    most = (1 << 27) - 32
+    assert B.dbf_route_workspace_bytes(_router(n_tokens=most, n_top=1)) >= most // 32 * 64
+    for n in (most + 1, 1 << 30):
+        assert B.dbf_route_workspace_bytes(_router(n_tokens=n, n_top=1)) == 0
+        _refused(B.DBF_EINVAL, B.dbf_route, _router(n_tokens=n, n_top=1), P, 1 << 60)
+
+
 def test_a_sum_of_rows_refuses():
     def sums(**kw):
         return B.Combine(**{**dict(rows=P, token_rows=P, weights=P, residual=P, out=P, row_stride=10, residual_stride=10, out_stride=10, dtype=B.F16, n_rows=4, n_tokens=3, n_top=2, n_cols=10), **kw})
