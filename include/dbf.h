@@ -493,6 +493,7 @@ int dbf_quantize(const void* x, int dtype, long long x_stride, int n_rows, int n
  *   w_scale, w_up_scale  DBF_E4M3: [ceil(n_out / 128)][ceil(n_in / 128)] of w_scale_type (DBF_E8M0 or DBF_F32), rows w_scale_stride scales apart
  *   y        [n_rows][n_out] of out_dtype (DBF_F16, DBF_BF16, DBF_F32), rows y_stride values apart, any alignment of the type
  * x, w and w_up are 16-byte aligned, and their rows a multiple of 16 bytes apart (what lies between n_in and the next row is not used).
+ * Rows of x, w and x_scale are 2^22 values apart at most, of y 2^32; with x_rows x has 2^32 bytes in all at most, and x_scale as many.  y overlaps nothing that is read.
  * For dbf_grouped_gemm: n_groups matrices, w_group_stride values (w_scale_group_stride scales) from one to the next, in w_up too; starts: device int32
  * [n_groups + 1], rows starts[g] .. starts[g + 1] - 1 of y are of matrix g (held to 0 .. n_rows; a group that ends before it begins has none; a row may be of one group
  * only).  Rows before starts[0] or behind starts[n_groups] are left as they were. */

@@ -170,8 +170,8 @@ int launch(const DenseArgs& a, hipStream_t stream) {
     return a.w_up ? launch<TYPE, FLOAT, true>(a, stream) : launch<TYPE, FLOAT, false>(a, stream);
 }
 
-constexpr long long MOST_STRIDE = 1 << 22;   // values of a row of x or weights: a tile's bytes have 32-bit offsets
-constexpr long long MOST_GATHERED = 1LL << 32;   // bytes of x whose rows are given: the same
+constexpr long long MOST_STRIDE = 1 << 22;   // values of a row of x, weights or x's scales: a tile's bytes have 32-bit offsets
+constexpr long long MOST_GATHERED = 1LL << 32;   // bytes of x whose rows are given, or of its scales: the same
 
 bool types_ok(const dbf_dense* p) {
     if (p->dtype != DBF_E4M3 && p->dtype != DBF_F16 && p->dtype != DBF_BF16) return false;
@@ -185,10 +185,10 @@ int check(const dbf_dense* p, bool grouped) {
     if (p->n_in < 1 || p->n_in > DBF_MAX_DIM || p->n_out < 1 || p->n_out > DBF_MAX_DIM) return DBF_ESHAPE;
     if (p->n_rows < 0 || p->n_x_rows < 0 || (!p->x_rows && p->n_x_rows < p->n_rows) || (p->n_rows && !p->n_x_rows)) return DBF_EINVAL;
     if (grouped ? !p->starts || p->n_groups < 1 || p->n_groups > DBF_MAX_GROUPS : p->starts || p->n_groups) return DBF_EINVAL;
-    if (p->x_rows && (p->n_x_rows * p->x_stride * (p->dtype == DBF_E4M3 ? 1 : 2) > MOST_GATHERED || p->n_x_rows * p->x_scale_stride > MOST_GATHERED)) return DBF_EINVAL;
     const int per = p->dtype == DBF_E4M3 ? 16 : 8, kb = (p->n_in + DBF_SCALE_BLOCK - 1) / DBF_SCALE_BLOCK;
     if (p->x_stride < p->n_in || p->x_stride % per || p->w_stride < p->n_in || p->w_stride % per || p->y_stride < p->n_out) return DBF_EINVAL;
-    if (p->x_stride > MOST_STRIDE || p->w_stride > MOST_STRIDE || p->y_stride > (1LL << 32)) return DBF_EINVAL;
+    if (p->x_stride > MOST_STRIDE || p->w_stride > MOST_STRIDE || p->x_scale_stride > MOST_STRIDE || p->y_stride > (1LL << 32)) return DBF_EINVAL;
+    if (p->x_rows && (p->n_x_rows * p->x_stride * (p->dtype == DBF_E4M3 ? 1 : 2) > MOST_GATHERED || p->n_x_rows * p->x_scale_stride > MOST_GATHERED)) return DBF_EINVAL;
     if (grouped && (p->w_group_stride < 0 || p->w_group_stride % per)) return DBF_EINVAL;
     if (dbf_misaligned(p->x, 16) || dbf_misaligned(p->w, 16) || dbf_misaligned(p->w_up, 16) || dbf_misaligned(p->x_rows, 4) || dbf_misaligned(p->starts, 4)) return DBF_EINVAL;
     if (dbf_misaligned(p->y, p->out_dtype == DBF_F32 ? 4 : 2)) return DBF_EINVAL;

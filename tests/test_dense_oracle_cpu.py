@@ -73,6 +73,19 @@ def test_products_refuse_shapes(kw):
     _refused(B.DBF_ESHAPE, B.dbf_grouped_gemm, _grouped(**kw))
 
 
+def test_products_refuse_rows_further_apart_than_offsets_reach():
+    # 2^22 values; a gathered x, whose rows may be any, has 2^32 bytes in all, its scales as many
+    far = 1 << 22
+    for f, make in ((B.dbf_dense_gemm, _dense), (B.dbf_grouped_gemm, _grouped)):
+        for kw in (dict(x_stride=far + 16), dict(w_stride=far + 16), dict(x_scale_stride=far + 4), dict(x_scale_stride=1 << 62), dict(y_stride=(1 << 32) + 1)):
+            _refused(B.DBF_EINVAL, f, make(**kw))
+            _refused(B.DBF_EINVAL, f, make(n_x_rows=1 << 20, x_rows=P, **kw))
+            _refused(B.DBF_EINVAL, f, make(n_rows=0, **kw))
+        _refused(B.DBF_EINVAL, f, make(x_rows=P, n_x_rows=1025, x_stride=far))
+        _refused(B.DBF_EINVAL, f, make(x_rows=P, n_x_rows=1025, x_scale_stride=far))
+        f(make(n_rows=0, x_rows=P, n_x_rows=1024, x_stride=far, x_scale_stride=far, w_stride=far, y_stride=1 << 32))
+
+
 def test_groups_are_refused_where_they_do_not_belong():
     for kw in (dict(starts=0), dict(starts=P + 2), dict(n_groups=0), dict(n_groups=B.MAX_GROUPS + 1), dict(w_group_stride=-16), dict(w_group_stride=8), dict(w_scale_group_stride=-1)):
         _refused(B.DBF_EINVAL, B.dbf_grouped_gemm, _grouped(**kw))
