@@ -13,6 +13,11 @@ typedef __attribute__((address_space(3))) unsigned* Shared;
 // A wavefront has its weights of a step in registers and its rows of x in pairs of 16.  Before a step's last pair all have read what the step has in LDS: there they meet,
 // the next step but one sets out for its place, and as each of the weights has done its last product the next step's comes from LDS into its registers: reads and loads are
 // under way beside products at all times.
+// Bound by the matrix cores and by what feeds them: 2047 rows through 2 x 11008 x 4096 in 8 bits (gated; 369 GFLOP, 140 us at a library's rate for 8192^3) in 171 us, 2.2 PFLOP/s, the
+// matrix cores busy for half the time.  The first form, whose scales were loaded to registers, took 246; scales through LDS 206; next weights in place 194; scales in the step's own buffer
+// 181; loads given out beside the products of two steps and more 171.  Its 688 tiles are 2.7 rounds of 256 compute units.  fp32 scales cost four operations beside each matrix
+// instruction: 16384 rows of 32 experts, 550 GFLOP, 369 us.  Four wavefronts of 128 x 128 with sums in the second half of the registers took 257 for the same, weights straight to
+// registers did not fit.  A wavefront's sums are all of its 128 accumulators at two wavefronts a SIMD: hence 256 x 256 by eight.
 template <int TYPE, bool FLOAT, bool GATED, bool EXACT, int BN, int BM, int WN, int WM, int EACH>
 __global__ __launch_bounds__(64 * WN * WM) __attribute__((amdgpu_waves_per_eu(EACH, EACH))) void dbf_dense_tiles_kernel(const DenseArgs a, int n_tiles, int m_tiles) {
     constexpr int WAVES = WN * WM, NS = BN / WN / 16, MS = BM / WM / 16, OUTS = GATED ? BN / 2 : BN;

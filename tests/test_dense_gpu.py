@@ -340,6 +340,26 @@ def test_rows_and_groups_beyond_4_gib():
 # ---- rounding to 8 bits ---------------------------------------------------------------------------------------
 
 
+def test_more_small_tiles_than_a_launch_has_workgroups_for():
+    """1024 rows of as many groups through 2^20 outputs: 32768 workgroups of outputs, of which a launch has 256 times as many at most; group g's weights begin 8 g rows in."""
+    g, groups, n_out, n_in = gen(53), 1024, 1 << 20, 12
+    x = Operand(groups, n_in, B.F16, g)
+    w = Operand(n_out + 8 * (groups - 1), n_in, B.F16, g)
+    starts = torch.arange(groups + 1, dtype=torch.int32, device="cuda")
+    y = torch.full((groups, n_out), float("nan"), dtype=torch.float16, device="cuda")
+    d = B.Dense(x=x.data.data_ptr(), x_stride=x.stride, n_x_rows=groups, w=w.data.data_ptr(), w_stride=w.stride, w_group_stride=8 * w.stride, y=y.data_ptr(), y_stride=n_out, dtype=B.F16,
+                out_dtype=B.F16, n_rows=groups, n_in=n_in, n_out=n_out, starts=starts.data_ptr(), n_groups=groups)
+    B.dbf_grouped_gemm(d, 0, 0, G.stream_handle())
+    torch.cuda.synchronize()
+    for part in y.split(64):
+        assert torch.isfinite(part).all()
+    cols = torch.cat([torch.randint(0, n_out, (200,), generator=g, device="cuda"), torch.tensor([0, 15, 16, n_out - 17, n_out - 1], device="cuda")])
+    for r in range(groups):
+        want, off = expected(x.values[0, r : r + 1], w.values[0, 8 * r + cols], None, True, B.F16)
+        far = ((y[r, cols].double() - want[0]).abs() / off[0]).max().item()
+        assert far <= 1, (r, far)
+
+
 @pytest.mark.parametrize("dtype", [B.F16, B.BF16, B.F32])
 @pytest.mark.parametrize("block_rows", [1, 128])
 @pytest.mark.parametrize("rows,cols,extra", [(1, 1, 0), (1, 128, 3), (7, 130, 0), (33, 1000, 1), (129, 257, 7), (300, 640, 0), (128, 16, 0), (2, 5000, 13)])
