@@ -10,8 +10,9 @@ namespace {
 
 // Few rows: a workgroup has 16 NS weights (gated: of each matrix) and 16 MS rows; its wavefronts have every KW-th four steps of them, and their sums meet in LDS.  Operands come
 // straight from memory as the matrix cores take them: of four steps 512 bytes of a row, four steps' loads under way at a time.
-// Bound by latencies: of a row through 4096 x 4096 in 8 bits (16.8 MB, which the caches hold: 2.4 us at a bare read's rate) 5.4 us, where the rounding of 7 rows
-// to 8 bits, a launch with next to nothing to do, takes 2.8; eight share the 32 steps of a workgroup's 16 weights, so that each waits for memory once.  Through LDS there is nothing to gain: no operand is used twice.
+// Bound by latencies: of a row through 4096 x 4096 in 8 bits (16.8 MB: 2.4 us at a bare read's rate) 5.6 us, where the rounding of 7 rows
+// to 8 bits, a launch with next to nothing to do, takes 2.8;
+// eight share the 32 steps of a workgroup's 16 weights, so that each waits for memory once.  Through LDS there is nothing to gain: no operand is used twice.
 constexpr int GROUP = 4;   // steps
 template <int TYPE, bool FLOAT, bool GATED, bool EXACT, int NS, int MS, int KW>
 __global__ __launch_bounds__(64 * KW) void dbf_dense_few_kernel(const DenseArgs a) {

@@ -13,7 +13,7 @@ typedef __attribute__((address_space(3))) unsigned* Shared;
 // (Weights straight to registers, 16 lanes a row each: every 16 bytes were an access of their own to the first cache, and these took two thirds of the time.  Here eight
 // lanes have 128 bytes of a row.  In LDS a row's piece p is at place p ^ (row % 8), so that 16 rows' pieces lie in all banks evenly.)
 // Bound by memory: 13 rows through a head of 4096 x 128256 in 8 bits, 529 MB, 81 us = 6.5 TB/s, beside the 7.0 of a bare read, for 103 with weights straight to registers,
-// 98 with loads that leave their lines in the caches and 97 with two places; the kernel for few rows 151.  Experts of few rows (147 MB, 26.5 us, 5.4 TB/s) wait besides at the
+// 98 with loads that leave their lines in the caches and 97 with two places; the kernel for few rows 151.  Experts of few rows (147 MB, 28 us, 5.2 TB/s) wait besides at the
 // start of each share, where rows have to be there before the first product.
 constexpr int KW = 8;
 template <int TYPE, bool FLOAT, bool GATED, bool EXACT, int SPAN, int C>

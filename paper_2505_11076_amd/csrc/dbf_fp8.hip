@@ -2,7 +2,7 @@
 //
 // A block's scale is the smallest power of two that brings its largest value to 448 or less, so a value over its scale is exact in fp32 and the conversion to the
 // type is its only rounding: codes do not hang on how a quotient is made.
-// Bound by memory where there is much (8191 rows of 11008 bf16: 271 MB in 39.7 us, 6.8 TB/s beside the 7.0 of a bare read) and by the launch where there is little (7 rows of 4096 in
+// Bound by memory where there is much (8191 rows of 11008 bf16: 271 MB in 47.4 us, 5.7 TB/s beside the 5.1 of a copy) and by the launch where there is little (7 rows of 4096 in
 // 2.8 us).  Eight lanes have a block, so that its largest value takes three moves between lanes and no memory; a lane's sixteen values are loads and a store of 16 bytes, and x is
 // read once.  A square of 128 x 128 stays in registers between its largest value and its codes (four turns
 // of 256 lanes), for the same reason.

@@ -364,7 +364,8 @@ struct CombineArgs {
     int n_rows, n_tokens, n_top, n_cols;
 };
 
-// N neighbouring values of a token to a thread.  Bound by memory: 4095 tokens, a residual and four rows each of 4096 fp16 values, 201 MB in 30.6 us (6.6 TB/s); a token's rows
+// N neighbouring values of a token to a thread.  Bound by memory: 4095 tokens, a residual and four rows each of 4096 fp16 values, 201 MB in 41.2 us (4.9 TB/s,
+// where a copy has 5.1; 30.6 where the last cache holds them); a token's rows
 // are n_top loads that do not wait for each other, and nothing is read twice but ids and weights, which the caches hold.
 constexpr int SUM_THREADS = 256;
 template <typename T, int N>
