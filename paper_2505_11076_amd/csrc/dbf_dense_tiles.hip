@@ -221,23 +221,64 @@ __global__ __launch_bounds__(64 * WN * WM) __attribute__((amdgpu_waves_per_eu(EA
     if (steps < all_steps) left(s0, steps);
     if (steps + 1 < all_steps) left(s1, steps + 1);
     __builtin_amdgcn_s_waitcnt(0x0070);
+    // outputs of rows 16 (MS wm + j) .. + 15: lane c's row, four columns for each i
+    auto output = [&](int i, int j, bool known) -> dbf_f4 {
+        dbf_f4 v = acc[i][j];
+        if constexpr (GATED) {
 #pragma unroll
-    for (int j = 0; j < MS; ++j) {
-        const int r = 16 * (MS * wm + j) + c, row = tile.row + r;
-        if (r >= tile.rows) continue;
-        const bool known = !a.x_rows || (unsigned)a.x_rows[row] < (unsigned)a.n_x_rows;
-#pragma unroll
-        for (int i = 0; i < NS; i += GATED ? 2 : 1) {
-            const int n = out0 + (GATED ? 8 * NS * wn + 8 * i : 16 * (NS * wn + i)) + 4 * q;
-            dbf_f4 v = acc[i][j];
-            if constexpr (GATED) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = gate(v[e], acc[i + 1][j][e]);
-            }
-            if (!known) v = (dbf_f4){0.f, 0.f, 0.f, 0.f};
-            if (n < a.n_out) store4(a, row, n, v);
+            for (int e = 0; e < 4; ++e) v[e] = gate(v[e], acc[i + 1][j][e]);
         }
+        return known ? v : (dbf_f4){0.f, 0.f, 0.f, 0.f};
+    };
+    auto is_known = [&](int r) { return !a.x_rows || r >= tile.rows || (unsigned)a.x_rows[tile.row + r] < (unsigned)a.n_x_rows; };
+    constexpr int COLS = GATED ? 8 * NS : 16 * NS;   // of a wavefront
+    if (a.quads) {
+#pragma unroll
+        for (int j = 0; j < MS; ++j) {
+            const int r = 16 * (MS * wm + j) + c, n0 = out0 + COLS * wn + 4 * q;
+            const bool known = is_known(r);
+            if (r >= tile.rows) continue;
+#pragma unroll
+            for (int i = 0; i < NS; i += GATED ? 2 : 1) {
+                const int n = n0 + 16 * (GATED ? i / 2 : i);
+                const dbf_f4 v = output(i, j, known);
+                if (n < a.n_out) store4(a, tile.row + r, n, v);
+            }
+        }
+        return;
     }
+    // Where four outputs are no word that can be stored, each goes by itself: through LDS, so that a wavefront's 64 are neighbours and not four of sixteen rows.
+    __syncthreads();
+    auto one_by_one = [&](auto type) {
+        typedef decltype(type) T;
+        constexpr int PITCH = COLS + 16 / sizeof(T);
+        static_assert(16 * PITCH * sizeof(T) * WAVES <= SCALES, "a part of LDS for each wavefront");
+        T* mine = reinterpret_cast<T*>(s0 + wave * (SCALES / WAVES / 16 * 16));
+#pragma unroll
+        for (int j = 0; j < MS; ++j) {
+            const bool known = is_known(16 * (MS * wm + j) + c);
+#pragma unroll
+            for (int i = 0; i < NS; i += GATED ? 2 : 1) {
+                const dbf_f4 v = output(i, j, known);
+                T* to = mine + c * PITCH + 16 * (GATED ? i / 2 : i) + 4 * q;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) to[e] = dbf_from_float<T>(v[e]);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int k = 0; k < COLS / 4; ++k) {
+                const int at = 64 * k + lane, r = 16 * (MS * wm + j) + at / COLS, n = out0 + COLS * wn + at % COLS;
+                const T v = mine[at / COLS * PITCH + at % COLS];
+                if (r < tile.rows && n < a.n_out) static_cast<T*>(a.y)[(tile.row + r) * a.y_stride + n] = v;
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+    };
+    if (a.out_dtype == DBF_F16) one_by_one(_Float16());
+    else if (a.out_dtype == DBF_BF16) one_by_one(dbf_bf16());
+    else one_by_one(float());
 }
 
 template <int TYPE, bool FLOAT, bool GATED, bool EXACT, int BN, int BM, int WN, int WM, int EACH>
