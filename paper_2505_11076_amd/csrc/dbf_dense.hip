@@ -203,6 +203,19 @@ int check(const dbf_dense* p, bool grouped) {
     return DBF_OK;
 }
 
+// Whether rows, `each` to a matrix, are few enough that operands come straight from memory, and not by tiles.  Of few rows tiles are few too and walk the long axis one step behind the other,
+// half a microsecond each and more the more there are, where eight wavefronts share it here; but here each 32 rows read the weights again, at 2.8 TB/s.  us, few rows for tiles, weights that no cache holds:
+//   4096 x 4096, 8 bits     24 rows 9.6 / 10.0   64 rows 15.3 / 24.1   128 rows 27.1 / 23.9        4096 x 16384, 8 bits    24 rows 24.4 / 23.7   64 rows 50.0 / 25.9
+//   11008 x 4096, 8 bits    24 rows 17.0 / 53.6  64 rows 32.6 / 55.9   128 rows 61.7 / 56.3        11008 x 4096, bf16      24 rows 35 / 118      96 rows 94 / 118
+//   8192 x 8192, bf16       24 rows 48 / 93      64 rows 96 / 96                                   28672 x 8192, 8 bits    24 rows 79 / 182      64 rows 170 / 192
+// (to fp32 from 8 bits, by instructions for fp16, tiles take half as long again: 8192 x 8192, 64 rows 52 / 66)
+bool few_rows(const DenseArgs& a, long long each, double weights, bool eight_bits) {
+    if (each <= (a.starts ? 4 : 16) || (each <= 32 && weights <= (32 << 20))) return true;
+    const double steps = a.k_bytes / (double)STEP, tiles = (double)(a.starts ? std::min(a.n_groups, a.n_rows) : 1) * ((a.n_out + 63) / 64) * (a.w_up ? 2 : 1);
+    const double by_tiles = 5 + steps * (0.5 + tiles / 1024) * (eight_bits && a.out_dtype == DBF_F32 ? 1.5 : 1), straight = 2.5 + (each + 31) / 32 * weights / 2.8e6;
+    return each <= 128 && straight < by_tiles;
+}
+
 int run(const dbf_dense* p, bool grouped, hipStream_t stream) {
     const int wrong = check(p, grouped);
     if (wrong != DBF_OK) return wrong;
@@ -238,8 +251,7 @@ int run(const dbf_dense* p, bool grouped, hipStream_t stream) {
     // average some have more than 16, whose weights are read twice: 268 MB of 64 groups with 4 rows each 44.2 for 43.8 by tiles, with 8 49 for 45, with 1 26.5 for 28 (147 MB).
     const long long each = a.starts ? (a.n_rows + a.n_groups - 1LL) / a.n_groups : a.n_rows;
     if (each <= (a.starts ? 4 : 16) && weights >= (64 << 20) && dbf_dense_streams(a.k_bytes)) return dbf_dense_stream(&a, p->dtype, fp32_scales, stream);
-    // Few rows' operands straight from memory: 24 rows of 4096 x 4096 9.4 for 11.7 by tiles, 48 rows 13.0 for 12.3, 24 rows of 16384 x 4096 23.4 for 19.9.
-    if (each > 32 || (each > 16 && weights > (32 << 20)) || (a.starts && each > 4 && weights > (32 << 20))) return dbf_dense_tiles(&a, p->dtype, fp32_scales, stream);
+    if (!few_rows(a, each, weights, p->dtype == DBF_E4M3)) return dbf_dense_tiles(&a, p->dtype, fp32_scales, stream);
     if (p->dtype == DBF_F16) return launch<DBF_F16, false>(a, stream);
     if (p->dtype == DBF_BF16) return launch<DBF_BF16, false>(a, stream);
     return fp32_scales ? launch<DBF_E4M3, true>(a, stream) : launch<DBF_E4M3, false>(a, stream);

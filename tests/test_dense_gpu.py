@@ -118,7 +118,8 @@ def run_dense(x, w, w_up, n_in, n_out, out, n_rows, x_rows=None, starts=None, sc
 
 # rows, n_in, n_out: on the sides of the rules that choose a kernel, lengths that end inside a step, a piece, a byte behind one
 SIZES = [(1, 1, 1), (1, 16, 16), (1, 128, 5), (3, 127, 33), (16, 129, 64), (2, 1000, 100), (16, 4096, 256), (17, 520, 70), (32, 1040, 130), (33, 300, 200), (64, 2048, 64), (65, 143, 129),
-         (100, 640, 257), (129, 256, 300), (200, 1999, 100), (257, 384, 513), (300, 1, 40), (520, 900, 1100), (1030, 272, 520)]
+         (100, 640, 257), (129, 256, 300), (200, 1999, 100), (257, 384, 513), (300, 1, 40), (520, 900, 1100), (1030, 272, 520),
+         (129, 16, 16), (130, 128, 5), (131, 143, 129), (150, 127, 33), (140, 1040, 130), (160, 300, 200), (192, 2048, 64)]
 KINDS = [(B.E4M3, B.E8M0, B.F16), (B.E4M3, B.F32, B.BF16), (B.E4M3, B.E8M0, B.F32), (B.E4M3, B.F32, B.F32), (B.F16, B.E8M0, B.F16), (B.BF16, B.E8M0, B.F32)]
 
 
@@ -181,7 +182,8 @@ def split(rows, groups, g):
 @pytest.mark.parametrize("kind", KINDS, ids=lambda k: "%d-%d-%d" % k)
 @pytest.mark.parametrize("rows,groups,n_in,n_out,gated,gathered", [(1, 1, 64, 17, False, False), (8, 64, 512, 96, True, True), (50, 16, 333, 129, True, True), (200, 5, 1000, 65, False, False),
                                                                    (700, 60, 272, 300, False, True), (700, 3, 700, 130, True, False), (1500, 4, 512, 520, True, True), (40, 1000, 144, 40, False, True),
-                                                                   (64, 70, 2048, 512, True, True)])
+                                                                   (64, 70, 2048, 512, True, True), (600, 4, 333, 129, True, True), (900, 6, 1000, 65, False, False), (1100, 8, 144, 40, False, True),
+                                                                   (270, 2, 64, 17, False, False), (2000, 12, 272, 300, True, True)])
 def test_a_product_by_groups(rows, groups, n_in, n_out, gated, gathered, kind):
     dtype, scale_type, out = kind
     g = gen(rows + groups)

@@ -34,7 +34,7 @@ def test_few_rows_stream_weights_that_no_cache_holds(rec):
         assert product(rec, rows, 4096, 16384)[0] == "stream"          # 64 MB
         assert product(rec, rows, 4096, 16383)[0] == "few"
         assert product(rec, rows, 4096, 8192, w_up=T.P, w_up_scale=T.P)[0] == "stream"
-    assert product(rec, 17, 4096, 16384)[0] == "tiles"
+    assert product(rec, 17, 4096, 16384)[0] == "few" and product(rec, 33, 4096, 16384)[0] == "tiles"
     # rows of up to 8192 bytes, of whole pieces of 16
     assert product(rec, 4, 8192, 32000)[0] == "stream" and product(rec, 4, 8208, 32000)[0] == "few" and product(rec, 4, 8191, 32000)[0] == "few"
     assert product(rec, 4, 4096, 32000, dtype=B.F16)[0] == "stream" and product(rec, 4, 4104, 32000, dtype=B.F16)[0] == "few"
@@ -49,7 +49,13 @@ def test_few_rows_of_small_weights(rec):
     assert product(rec, 3, 1024, 32768) == ("few", (1024, 1, 1), 256)
     assert product(rec, 3, 512, 32768, w_up=T.P, w_up_scale=T.P) == ("few", (2048, 1, 1), 256)
     assert product(rec, 17, 4096, 4096) == ("few", (256, 1, 1), 256) and product(rec, 32, 4096, 4096)[0] == "few"
-    assert product(rec, 33, 4096, 4096)[0] == "tiles" and product(rec, 17, 4096, 8193)[0] == "tiles"
+    # more rows read the weights again for each 32, but tiles of few outputs are too few for a long axis
+    assert product(rec, 33, 4096, 4096)[0] == "few" and product(rec, 96, 4096, 4096)[0] == "few" and product(rec, 97, 4096, 4096)[0] == "tiles"
+    assert product(rec, 32, 4096, 8193)[0] == "few" and product(rec, 33, 4096, 8193)[0] == "tiles" and product(rec, 64, 11008, 4096)[0] == "few" and product(rec, 128, 11008, 4096)[0] == "tiles"
+    assert product(rec, 32, 28672, 8192) == ("few", (512, 1, 1), 256) and product(rec, 96, 11008, 4096, dtype=B.BF16) == ("few", (256, 3, 1), 256)
+    assert product(rec, 128, 128, 16)[0] == "few" and product(rec, 129, 128, 16)[0] == "tiles"
+    assert product(rec, 64, 8192, 8192)[0] == "tiles" and product(rec, 64, 8192, 8192, out_dtype=B.F32)[0] == "few"
+    assert product(rec, 300 * 8, 2048, 1024, 64, w_up=T.P, w_up_scale=T.P)[0] == "tiles" and product(rec, 32, 11008, 4096, 2)[0] == "few"
     # rows of groups: tiles of 16, one at least for each that may have some
     assert product(rec, 12, 256, 64, 5)[:2] == ("few", (4, 1 + 5, 1))
     assert product(rec, 3, 256, 64, 5)[:2] == ("few", (4, 1 + 3, 1))
@@ -71,7 +77,7 @@ def test_tiles_are_chosen_by_what_a_launch_costs(rec):
     assert tiles(2048, 4096, 16384) == (8 * 64, 512)      # 256 x 256
     assert tiles(2048, 4096, 4096) == (16 * 32, 256)      # 128 x 128
     assert tiles(256, 4096, 16384)[0] in (2 * 128, 4 * 128)
-    assert tiles(64, 4096, 4096) == (64, 128)             # 64 x 64
+    assert tiles(160, 4096, 4096) == (3 * 64, 128)        # 64 x 64
     assert tiles(2047, 4096, 11008, w_up=T.P, w_up_scale=T.P) == (8 * 86, 512)
     # fp32 outputs of 8 bits go through fp16, whose operands leave no registers for the largest
     assert tiles(2048, 4096, 16384, out_dtype=B.F32) == (16 * 128, 256)
