@@ -99,6 +99,16 @@ __global__ __launch_bounds__(64 * KW) void dbf_dense_stream_kernel(const DenseAr
                 const int s = min(step_of(i, 0), kb - 1);
                 xs[i] = *reinterpret_cast<const unsigned*>(a.x_scale + from * a.x_scale_row + (s & ~3)) >> (8 * (s & 3));
             }
+            // A step behind the row's end, whose values are zeros, has the last block's scale where it is its part's first, else 1: what lies behind that block's byte may be 255, no
+            // number, and so would be its products.
+            if constexpr (C > 1) {
+                static_assert(C == 2, "a part's second step is its last");
+#pragma unroll
+                for (int i = 0; i < PARTS; ++i) {
+                    const bool there = step_of(i, 1) < kb;
+                    xs[i] = (xs[i] & (there ? ~0u : 255u)) | (there ? 0u : 127u << 8);
+                }
+            }
         }
         dbf_f4 acc[N];
         auto products = [&](int place, int part) {
