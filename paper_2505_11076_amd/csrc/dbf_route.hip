@@ -337,7 +337,7 @@ Room room_of(const dbf_router* r) {
 
 template <typename T, int L, int PER>
 void choose(const RouteArgs& a, int score, dim3 grid, hipStream_t stream) {
-    const dim3 threads(std::min(CHOOSERS, std::max(64, (a.n_tokens * L + 63) / 64 * 64)));   // (no more wavefronts than tokens)
+    const dim3 threads(std::min(CHOOSERS, (std::min(a.n_tokens, CHUNK) * L + 63) / 64 * 64));   // (no more wavefronts than a chunk's tokens need)
     if (score == DBF_SCORE_SIGMOID) hipLaunchKernelGGL((dbf_route_choose_kernel<T, L, PER, true>), grid, threads, 0, stream, a);
     else hipLaunchKernelGGL((dbf_route_choose_kernel<T, L, PER, false>), grid, threads, 0, stream, a);
 }
