@@ -132,10 +132,21 @@ __device__ __forceinline__ void multiply_exactly(dbf_f4& acc, v8i w, v8i x, int 
     dbf_f4 p = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int k = 0; k < 4; ++k) p = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen(w, k), widen(x, k), p, 0, 0, 0);
-    // (the smaller scale first: the other way round a sum of 2^25 leaves fp32's range where the result does not.  Sums are multiples of 2^-18, so 2^-127 of one is exact)
-    const float by = FLOAT ? __builtin_bit_cast(float, w_scale) : scale_of(w_scale), of_row = scale_of(x_scale);
-    const bool first = fabsf(by) < of_row;
-    const float a = first ? by : of_row, b = first ? of_row : by;
+    // Sums are multiples of 2^-18, so that each times the first factor, a power of two, is exact, and what rounds is the addition alone.
+    float a, b;
+    if constexpr (FLOAT) {
+        // The power of two of a number goes together with the row's, and half of both comes on the sum first: neither alone takes it out of fp32's range where the result does not leave
+        // it (with all of a number below 2^-126, or of a sum of small codes by one near it, first, digits were lost that the row's scale brings back into range)
+        const float number = __builtin_bit_cast(float, w_scale);
+        const int power = __builtin_amdgcn_frexp_expf(number) + x_scale - 127, half = power >> 1;
+        a = x_scale == 255 ? scale_of(255) : __builtin_ldexpf(1.f, half);
+        b = __builtin_ldexpf(__builtin_amdgcn_frexp_mantf(number), power - half);
+    } else {
+        // (the smaller one first: the other way round a sum of 2^25 leaves fp32's range where the result does not; 2^-127 of a sum is exact)
+        const float by = scale_of(w_scale), of_row = scale_of(x_scale);
+        const bool first = by < of_row;   // (not a minimum: no number has to stay one)
+        a = first ? by : of_row, b = first ? of_row : by;
+    }
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[e] = fmaf(p[e] * a, b, acc[e]);
 }

@@ -1,4 +1,6 @@
-"""Scales of products with ordinary weights at their edges: what lies behind a row's last block.  Bounds are those of tests/test_dense_gpu.py."""
+"""Scales of products with ordinary weights at their edges: what lies behind a row's last block, and the ends of their range.  Bounds are those of
+tests/test_dense_gpu.py; fp32 outputs have nothing of the 8-bit instructions' beside theirs, whatever the scales are."""
+import numpy as np
 import pytest
 import torch
 
@@ -92,3 +94,50 @@ def test_rounded_rows_in_a_buffer_of_no_numbers(rows, n_out):
     xv = torch.from_numpy(O.values(*O.quantize(t.double().cpu().numpy(), 1), 1)).cuda()
     want, off = D.expected(xv, w.values[0], None, True, B.F32)
     D.near(y, want, off, "%d rows" % rows)
+
+
+# Scales of rows (bytes) and of weights that meet within fp32: numbers near 2^-126 and below it, whose sums with the smallest codes leave fp32's normal range on the way
+ENDS = [(240, 1.7 * 2.0 ** -126), (247, 1.3 * 2.0 ** -100), (254, -1.9 * 2.0 ** -120), (253, 1.625 * 2.0 ** -140), (254, 3 * 2.0 ** -149), (200, 1.1 * 2.0 ** -126), (0, 1.3 * 2.0 ** 112),
+        (1, -1.7 * 2.0 ** 120), (0, 1.9 * 2.0 ** 127), (127, 1.0), (100, 3.1e7), (140, 0.0)]
+
+
+@pytest.mark.parametrize("rows,n_in,n_out", [(3, 128, 20), (3, 640, 20), (70, 640, 20), (200, 384, 130), (2, 1024, 66000)])
+@pytest.mark.parametrize("codes", ["smallest", "all"])
+def test_fp32_scales_at_the_ends_of_their_range_cost_no_precision(rows, n_in, n_out, codes):
+    g = D.gen(rows + n_in)
+    x, w = D.Operand(rows, n_in, B.E4M3, g), D.Operand(n_out, n_in, B.E4M3, g, 128, B.F32)
+    if codes == "smallest":   # (subnormal codes, of either sign: products of 2^-18 and some of them)
+        for o in (x, w):
+            o.data &= 0x83
+    xv, wv = D.table()[x.data[0, :, :n_in].int()], D.table()[w.data[0, :, :n_in].int()]
+    v, size = xv @ wv.t().contiguous(), xv.abs() @ wv.abs().t().contiguous()
+    for a, b in ENDS:
+        x.scale[:], w.scale[:] = a, b
+        b = float(np.float32(b))
+        y = D.run_dense(x, w, None, n_in, n_out, B.F32, rows, scale_type=B.F32)
+        torch.cuda.synchronize()
+        s = 2.0 ** (a - 127) * b
+        want = v * s
+        # (a sum in chains of K + 3 additions, the scale, the output; what is subnormal as a result is off by half of 2^-149 for each block)
+        off = (n_in + 4) * D.U * size * abs(s) + D.U * want.abs() + 2.0 ** -150 * (kb_of(n_in) + 1)
+        keep = size * abs(s) < 3e38
+        far = torch.where(keep, (y.double() - want).abs() / off, 0).max().item()
+        G.say("%d x %d -> %d, scales 2^%d and %g: %.3g of the bound" % (rows, n_in, n_out, a - 127, b, far))
+        assert torch.isfinite(y[keep]).all() and far <= 1, (a, b)
+
+
+@pytest.mark.parametrize("rows,n_in,n_out", [(3, 640, 20), (70, 640, 20), (200, 384, 130), (2, 1024, 66000)])
+def test_powers_of_two_at_the_ends_of_their_range_cost_no_precision(rows, n_in, n_out):
+    g = D.gen(rows + n_in)
+    x, w = D.Operand(rows, n_in, B.E4M3, g), D.Operand(n_out, n_in, B.E4M3, g, 128)
+    for o in (x, w):
+        o.data &= 0x83
+    xv, wv = D.table()[x.data[0, :, :n_in].int()], D.table()[w.data[0, :, :n_in].int()]
+    v, size = xv @ wv.t().contiguous(), xv.abs() @ wv.abs().t().contiguous()
+    for a, b in ((0, 240), (240, 0), (1, 253), (0, 0), (100, 140), (254, 120)):
+        x.scale[:], w.scale[:] = a, b
+        y = D.run_dense(x, w, None, n_in, n_out, B.F32, rows)
+        torch.cuda.synchronize()
+        s = 2.0 ** (a + b - 254)
+        off = (n_in + 4) * D.U * size * s + D.U * (v * s).abs() + 2.0 ** -150 * (kb_of(n_in) + 1)
+        assert torch.isfinite(y).all() and ((y.double() - v * s).abs() <= off).all(), (a, b)
