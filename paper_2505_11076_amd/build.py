@@ -201,6 +201,60 @@ def _wait_states_report(code: str):
     return seen, bad
 
 
+# The fourth guard, for loads into LDS that are waited for by their number.  A part of the weights is taken to be there once no more loads are under way than AHEAD parts behind it have: that
+# holds where each of these has as many as the kernel counts, and where parts set out in order.  One load less (two made one, one made scalar) would be a race without a fault.  The source
+# marks where a part's loads begin and end, and the build counts the vector loads between the marks.
+PARTS_SRC = "dbf_dense_stream.hip"
+PART_MARKS = ("; loads of a part", "; end of a part's loads")
+
+
+def _part_loads_report(code: str, ahead: int):
+    """(kernels seen, [complaints]) for the assembly text `code` of PARTS_SRC: each part's loads in one piece of straight code, as many as the kernel's arguments ask for, and behind
+    each part but the first `ahead` a wait for all but those of `ahead` parts."""
+    import re
+    bad, seen = [], 0
+    for m in re.finditer(r"^(_ZN\w*dbf_dense_stream_kernelILi(\d)ELb\dELb(\d)ELb\dELi(\d)ELi(\d)E\w*):", code, re.M):
+        name, eight_bits, n, span, c = m.group(1), m.group(2) == "3", 1 + int(m.group(3)), int(m.group(4)), int(m.group(5))
+        want = 2 * n * c + (n if eight_bits else 0)
+        parts, loads, waited = 0, None, True
+        for line in code[m.end():code.index("s_endpgm", m.end())].splitlines():
+            line = line.strip()
+            if line == PART_MARKS[0]:
+                if not waited:
+                    bad.append("%s: no wait for all but %d loads behind part %d" % (name, ahead * want, parts))
+                loads = 0
+            elif line == PART_MARKS[1]:
+                parts += 1
+                waited = parts <= ahead   # (those before the loop are waited for behind the first ones in it)
+                if loads is None or loads < want:
+                    bad.append("%s: %s loads in part %d, of %d" % (name, loads, parts, want))
+                loads = None
+            elif line.startswith(("global_load", "buffer_load", "flat_load")):
+                loads = None if loads is None else loads + 1
+            elif line.startswith("s_waitcnt"):
+                count = re.search(r"vmcnt\((\d+)\)", line)
+                waited = waited or bool(count) and int(count.group(1)) <= ahead * want
+            elif loads is not None and (line.startswith(("s_cbranch", "s_branch")) or re.match(r"[.\w]+:", line)):
+                bad.append("%s: a part's loads are not one piece of straight code" % name)
+        if not waited:
+            bad.append("%s: no wait for all but %d loads behind part %d" % (name, ahead * want, parts))
+        rounds = max(span // c, ahead + 1)
+        if parts != ahead + rounds:
+            bad.append("%s: %d parts, of %d before the loop and %d in it" % (name, parts, ahead, rounds))
+        seen += 1
+    return seen, bad
+
+
+def _check_part_loads() -> None:
+    import re
+    ahead = int(re.search(r"AHEAD = (\d+)", open(os.path.join(CSRC, PARTS_SRC)).read()).group(1))
+    seen, bad = _part_loads_report(_assembly(PARTS_SRC), ahead)
+    if not seen:
+        raise RuntimeError("%s: no kernel found in the assembly (has it been renamed?)" % PARTS_SRC)
+    if bad:
+        raise RuntimeError("%s: the loads that a wait counts on are not there:\n  %s" % (PARTS_SRC, "\n  ".join(bad)))
+
+
 def _check_wait_states() -> None:
     seen, bad = _wait_states_report(_assembly(WAITS_SRC))
     if not seen:
@@ -302,8 +356,8 @@ def build_route_recorder(runtime_cpp: str) -> str:
 
 def build(verbose: bool = True) -> str:
     os.makedirs(OBJ, exist_ok=True)
-    with ThreadPoolExecutor(max_workers=min(8, len(SOURCES) + 2)) as pool:
-        checks = [pool.submit(_check_ring_homes), pool.submit(_check_wait_states)]
+    with ThreadPoolExecutor(max_workers=min(8, len(SOURCES) + 3)) as pool:
+        checks = [pool.submit(_check_ring_homes), pool.submit(_check_wait_states), pool.submit(_check_part_loads)]
         objs = list(pool.map(_compile, SOURCES))
         for c in checks:
             c.result()

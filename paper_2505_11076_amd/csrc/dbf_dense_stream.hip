@@ -45,7 +45,9 @@ __global__ __launch_bounds__(64 * KW) void dbf_dense_stream_kernel(const DenseAr
         const int last_n = to_n - 1;
         int scale[PLACES][N];   // of the weights; lane s has step s's
         // (behind the last of the rows' pieces of work one address for all lanes, so that no round has other loads under way than another)
+        // What wait() counts on is that a part is LOADS loads at least and that parts set out one behind the other: nothing passes the two marks, and the build counts what is between them.
         auto fetch = [&](int place, int n, int part) {
+            asm volatile("; loads of a part" ::: "memory");
             unsigned live = n <= last_n ? ~0u : 0u;
             asm("" : "+v"(live));   // (as a number: no branches beside the loads)
             n = min(n, last_n);
@@ -67,6 +69,7 @@ __global__ __launch_bounds__(64 * KW) void dbf_dense_stream_kernel(const DenseAr
                         __builtin_amdgcn_global_load_lds((Global)((i ? a.w_up : a.w) + base + ((row + at[part * C + s]) & live)), (Shared)(to + wave * (N * C * 2048) + (i * C + s) * 2048 + 1024 * half),
                                                          16, 0, 2);   // (2: read once, so it need not stay in the caches: 96 -> 81 us for 525 MB)
             }
+            asm volatile("; end of a part's loads" ::: "memory");
         };
         // the loads before those of the last three parts have arrived; what was read from LDS is in registers
         auto wait = [&]() {
