@@ -119,8 +119,12 @@ __device__ __forceinline__ void multiply(dbf_f4& acc, const v8i& w, const v8i& x
 __device__ __forceinline__ float scale_of(int byte) {
     return __builtin_bit_cast(float, byte == 255 ? 0x7FC00000u : byte ? (unsigned)byte << 23 : 0x00400000u);
 }
-// The same of values in 8 bits where the result is to have 32: the instructions for 8 bits cut off what is below 2^-13 of the largest of sixteen neighbouring products (1.5e-5 of the
-// result for random values of one size, 6e-5 where they span 2^12: a tenth and a third of what rounding to fp16 costs); in fp16 the values are exact, and so are the products.
+// The same of values in 8 bits where the result is to have 32: of each of sixteen neighbouring products the instructions for 8 bits cut off, towards zero, what lies below 2^-13 of the
+// largest, so a sum is off by 16 * 2^-13 of the largest of each sixteen at most, relative to its terms and not to itself (of random values of one size it measures 1.5e-5 of the results'
+// size, 6e-5 where they span 2^12: a tenth and a third of what rounding to fp16 costs); in fp16 the values are exact, and so are the products.  For results of 16 bits it is not taken, so that a
+// row has the same precision among few and among many: beside weights from memory it would cost 0 to 9 % (us, 8-bit instructions / these: 13 rows of 128256 x 4096 with fp32 scales 82.5 / 84.2, 16 of
+// 32064 x 4096 25.2 / 26.4, 64 of 4096 x 4096 14.3 / 15.7, one of 16384 x 4096 14.1 / 15.4), but where there are many rows the matrix cores do a third as much (2047 rows of 11008 x 4096: 310
+// us; with 8-bit instructions 180 for two such matrices).
 template <bool FLOAT>
 __device__ __forceinline__ void multiply_exactly(dbf_f4& acc, v8i w, v8i x, int w_scale, int x_scale) {
     auto widen = [](v8i v, int k) -> dbf_h8 {   // codes 8 k .. 8 k + 7

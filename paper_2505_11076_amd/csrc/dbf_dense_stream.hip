@@ -12,9 +12,10 @@ typedef __attribute__((address_space(3))) unsigned* Shared;
 // their sums meet in LDS, where one wavefront, each in turn, adds them up in order.
 // (Weights straight to registers, 16 lanes a row each: every 16 bytes were an access of their own to the first cache, and these took two thirds of the time.  Here eight
 // lanes have 128 bytes of a row.  In LDS a row's piece p is at place p ^ (row % 8), so that 16 rows' pieces lie in all banks evenly.)
-// Bound by memory: 13 rows through a head of 4096 x 128256 in 8 bits, 529 MB, 81 us = 6.5 TB/s, beside the 7.0 of a bare read, for 103 with weights straight to registers,
-// 98 with loads that leave their lines in the caches and 97 with two places; the kernel for few rows 151.  Experts of few rows (147 MB, 28 us, 5.2 TB/s) wait besides at the
-// start of each share, where rows have to be there before the first product.
+// Bound by memory: 13 rows through a head of 4096 x 128256 in 8 bits, 529 MB, 82 us = 6.4 TB/s, beside the 7.0 of a bare read, for 103 with weights straight to registers,
+// 98 with loads that leave their lines in the caches and 97 with two places; the kernel for few rows 112.  Experts of few rows (147 MB, 28.5 us, 5.2 TB/s) wait besides at the
+// start of each share, where rows have to be there before the first product.  (Scales of a byte are widened in the round of the loop that loads them, for which the compiler waits for all
+// loads once a round; it does not show: with fp32 scales, which have no such wait, the head takes 82.5 for 82.7, the experts 28.4 for 28.7.)
 constexpr int KW = 8;
 template <int TYPE, bool FLOAT, bool GATED, bool EXACT, int SPAN, int C>
 __global__ __launch_bounds__(64 * KW) void dbf_dense_stream_kernel(const DenseArgs a) {

@@ -13,10 +13,11 @@ typedef __attribute__((address_space(3))) unsigned* Shared;
 // A wavefront has its weights of a step in registers and its rows of x in pairs of 16.  Before a step's last pair all have read what the step has in LDS: there they meet,
 // the next step but one sets out for its place, and as each of the weights has done its last product the next step's comes from LDS into its registers: reads and loads are
 // under way beside products at all times.
-// Bound by the matrix cores and by what feeds them: 2047 rows through 2 x 11008 x 4096 in 8 bits (gated; 369 GFLOP, 140 us at a library's rate for 8192^3) in 171 us, 2.2 PFLOP/s, the
-// matrix cores busy for half the time.  The first form, whose scales were loaded to registers, took 246; scales through LDS 206; next weights in place 194; scales in the step's own buffer
-// 181; loads given out beside the products of two steps and more 171.  Its 688 tiles are 2.7 rounds of 256 compute units.  fp32 scales cost four operations beside each matrix
-// instruction: 16384 rows of 32 experts, 550 GFLOP, 369 us.  Four wavefronts of 128 x 128 with sums in the second half of the registers took 257 for the same, weights straight to
+// Bound by the matrix cores and by what feeds them: 2047 rows through 2 x 11008 x 4096 in 8 bits (gated; 369 GFLOP, 140 us at a library's rate for 8192^3) in 171 to 182 us by passes in
+// turn, under a profiler 196 in the median and 177 at least (the clock falls as it goes on): 1.9 to 2.2 PFLOP/s, the
+// matrix cores busy for half the time.  Steps, timed when each was made: the first form, whose scales were loaded to registers, 246; scales through LDS 206; next weights in place 194; scales in
+// the step's own buffer 181; loads given out beside the products of two steps and more 171.  Its 688 tiles are 2.7 rounds of 256 compute units.  fp32 scales cost four operations beside each matrix
+// instruction: the same with them 208 us for 180, 16384 rows of 32 experts, 550 GFLOP, 365 to 391.  Four wavefronts of 128 x 128 with sums in the second half of the registers took 257 for the same, weights straight to
 // registers did not fit.  A wavefront's sums are all of its 128 accumulators at two wavefronts a SIMD: hence 256 x 256 by eight.
 template <int TYPE, bool FLOAT, bool GATED, bool EXACT, int BN, int BM, int WN, int WM, int EACH>
 __global__ __launch_bounds__(64 * WN * WM) __attribute__((amdgpu_waves_per_eu(EACH, EACH))) void dbf_dense_tiles_kernel(const DenseArgs a, int n_tiles, int m_tiles) {
@@ -248,7 +249,7 @@ __global__ __launch_bounds__(64 * WN * WM) __attribute__((amdgpu_waves_per_eu(EA
         return;
     }
     // Where four outputs are no word that can be stored, each goes by itself: through LDS, so that a wavefront's 64 are neighbours and not four of sixteen rows (6126 rows of 60 experts,
-    // 1000 x 2047 in bf16, 101 us for 107; with 128 values a row 27 for 37).
+    // 1000 x 2047 in bf16, 111 us for 117; with 128 values a row 26 for 36).
     __syncthreads();
     auto one_by_one = [&](auto type) {
         typedef decltype(type) T;
@@ -296,7 +297,9 @@ int launch(const DenseArgs& a, hipStream_t stream) {
 //   128 x 128   64 x 4096 21    256 x 16384 32    512 x 16384 37   1024 x 16384 73   2048 x 16384 140   2048 x 4096 38
 //   128 x 64    64 x 4096 16    256 x 16384 26    512 x 16384 49   512 x 4096 23     1024 x 4096 26     2048 x 4096 51
 //   64 x 64     64 x 4096 14    256 x 16384 30    512 x 16384 66   512 x 4096 23     1024 x 4096 29     2048 x 4096 66
-// Of a group's last tile half is taken to be empty (16384 rows of 32 experts, fp32 scales, gated, 396 us, with 128 x 128 476).
+// Of a group's last tile half is taken to be empty (16384 rows of 32 experts, fp32 scales, gated, 366 us, with 128 x 128 455).
+// They are 8 bits' with scales of a byte.  16 bits, fp32 scales and fp16 instructions cost more a step and go by the same, as the order of the four is much the same: 60 experts, 1000 x 2047 in bf16,
+// 6126 rows 111 us by 128 x 64 for 109 by 128 x 128, 1800 rows 67 for 75.
 double cost_of(const DenseArgs& a, int outs, int rows, int places, double alone, double full) {
     const double groups = a.starts ? std::min(a.n_groups, a.n_rows) : 1, each = a.n_rows / groups;
     const double m_tiles = groups * (a.starts ? std::max(1.0, each / rows + 0.5) : std::ceil(each / rows));
